@@ -16,7 +16,10 @@
  *  - the scores, batch selection and stopping rule of the multi-pass Bayesian
  *    optimisation (Section 4.3, Algorithm 1);
  *  - the launch-timing frontier of two operation sequences (Appendix B);
- *  - the evaluation's frontier comparison metrics (Section 6.1).
+ *  - the evaluation's frontier comparison metrics (Section 6.1);
+ *  - the compute kernels of a transformer block's partition on this card, so that a plan
+ *    can be made from measured times: norm with the residual's addition, gated
+ *    projection, their backward passes, and the forward form in 8-bit integers.
  *
  * Conventions for every entry point
  *  - Array arguments are DEVICE pointers unless marked "host".  The caller owns and
@@ -490,6 +493,69 @@ kr_status kr_launch_timing_frontier(int64_t n_inst, int32_t I, int32_t J, const 
 kr_status kr_decode_candidates(const kr_space *space, const int32_t *idx, int64_t n,
                                int32_t *f_out, int32_t *pos_out, int32_t *sm_out,
                                void *stream);
+
+/*
+ * Transformer-block operators.
+ *
+ * The compute kernels that a partition of a transformer block is made of (Section 4.2:
+ * norms are its memory-bound rows, projections its compute-bound ones).  The conventions
+ * above on pointers, streams, workspaces and return codes hold; these differ:
+ *  - Values are KR_F32, KR_F16 or KR_BF16; sums, norms and products are held in 32 bits
+ *    (fused multiply-adds allowed) and every stored value is rounded once, unless the call
+ *    says otherwise.  Results do not depend on other work on the device: no atomics.
+ *  - A matrix is rows of contiguous elements, `ld` elements apart (ld >= the row's length,
+ *    64-bit offsets throughout), aligned to its element.  Any size and alignment is taken;
+ *    rows that are 16-byte aligned and a multiple of 16 bytes long are fastest (products
+ *    copy others into the workspace first).
+ *  - NaN and infinite inputs are allowed and give what the formulas give.
+ *  - A call without rows does nothing but the zero weight gradients it owes.
+ */
+#define KR_F32 0
+#define KR_F16 1
+#define KR_BF16 2
+
+/*
+ * kr_add_rms_norm -- sum of input and residual, and its root-mean-square norm:
+ *   s = x + residual,  rstd = 1 / sqrt(mean(s^2) + eps),  out = s * rstd * weight
+ *   type              of x, residual, weight, sum and out
+ *   rows, width       rows >= 0, 1 <= width <= 2^30
+ *   residual          NULL: s = x
+ *   sum               s, rounded to the type (the norm uses the unrounded s), or NULL
+ *   rstd              [rows] or NULL: what the backward pass takes
+ * sum and out may be x or residual themselves (same rows and ld), not each other.
+ * KR_EINVAL for a negative, infinite or NaN eps.  No workspace.
+ */
+kr_status kr_add_rms_norm(int32_t type, int64_t rows, int64_t width, const void *x, int64_t ldx,
+                          const void *residual, int64_t ldr, const void *weight, float eps,
+                          void *sum, int64_t lds, void *out, int64_t ldo, float *rstd,
+                          void *stream);
+
+/*
+ * kr_add_rms_norm_bytes -- the same with the norm n (32 bits, not rounded to the type) held
+ * in 8-bit integers: with a = the row's largest |n|,
+ *   scale = a / 127,  q = round(n * (127 / a)), halves to even
+ * A row with a < 2^-100 gives q = 0 and scale = 0; a row with a NaN or an infinity gives
+ * q = 0 and scale = NaN.  q is what kr_byte_matmul takes, its rows ldq bytes apart.
+ */
+kr_status kr_add_rms_norm_bytes(int32_t type, int64_t rows, int64_t width, const void *x,
+                                int64_t ldx, const void *residual, int64_t ldr,
+                                const void *weight, float eps, void *sum, int64_t lds, int8_t *q,
+                                int64_t ldq, float *scale, float *rstd, void *stream);
+
+/*
+ * kr_add_rms_norm_backward -- gradients of kr_add_rms_norm, given the sum s and rstd that
+ * it returned.  With h = s * rstd and g = dout * weight,
+ *   dx = rstd * (g - h * mean(g * h)) + dsum,  dweight = sum over rows of dout * h
+ *   dsum     gradient that reaches s by the residual's path, or NULL: 0
+ *   dx       gradient of x and, being the same, of residual; may be dout or dsum itself
+ *   dweight  float [width]; 0 where there are no rows
+ */
+kr_status kr_add_rms_norm_backward(int32_t type, int64_t rows, int64_t width, const void *dout,
+                                   int64_t ldo, const void *sum, int64_t lds, const void *weight,
+                                   const float *rstd, const void *dsum, int64_t ldd, void *dx,
+                                   int64_t ldx, float *dweight, void *ws, size_t ws_bytes,
+                                   void *stream);
+size_t kr_add_rms_norm_backward_workspace(int32_t type, int64_t rows, int64_t width);
 
 /*
  * kr_set_phase_events -- instrumentation for profilers and benchmarks (not part of the

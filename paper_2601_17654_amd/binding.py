@@ -34,6 +34,7 @@ class KrSpace(ctypes.Structure):
 
 _vp, _i32, _i64, _f64, _sz = (ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64,
                               ctypes.c_double, ctypes.c_size_t)
+_f32 = ctypes.c_float
 _SP = ctypes.POINTER(KrSpace)
 _SIGS = {
     "kr_evaluate_partition": (_i32, [_SP, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp]),
@@ -71,6 +72,13 @@ _SIGS = {
     "kr_launch_timing_frontier": (_i32, [_i64, _i32, _i32, _vp, _vp, _f64, _i32, _i32, _vp, _vp,
                                          _vp, _vp, _vp, _vp, _sz, _vp]),
     "kr_launch_timing_frontier_workspace": (_sz, [_i64]),
+    "kr_add_rms_norm": (_i32, [_i32, _i64, _i64, _vp, _i64, _vp, _i64, _vp, _f32, _vp, _i64, _vp,
+                               _i64, _vp, _vp]),
+    "kr_add_rms_norm_bytes": (_i32, [_i32, _i64, _i64, _vp, _i64, _vp, _i64, _vp, _f32, _vp, _i64,
+                                     _vp, _i64, _vp, _vp, _vp]),
+    "kr_add_rms_norm_backward": (_i32, [_i32, _i64, _i64, _vp, _i64, _vp, _i64, _vp, _vp, _vp,
+                                        _i64, _vp, _i64, _vp, _vp, _sz, _vp]),
+    "kr_add_rms_norm_backward_workspace": (_sz, [_i32, _i64, _i64]),
     "kr_status_string": (ctypes.c_char_p, [_i32]),
     "kr_set_phase_events": (_i32, [_i32, _vp, _vp]),
 }
@@ -685,3 +693,142 @@ def launch_timing_frontier(kind1, kind2, ops, p_static: float, kmax: int, out_ca
     if check and int(out.status.item()) != KR_OK:
         raise KrError("kr_launch_timing_frontier", int(out.status.item()))
     return out
+
+
+# ---- transformer-block operators ------------------------------------------------------
+# Values are float32, float16 or bfloat16 tensors on the current device; leading dimensions
+# are rows.  Outputs and workspaces are allocated on the current stream.
+
+_TYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
+
+
+def _type(x: torch.Tensor, name: str, types=tuple(_TYPES)) -> int:
+    if not isinstance(x, torch.Tensor) or x.dtype not in types:
+        raise TypeError("%s must be a tensor of %s, got %s"
+                        % (name, " or ".join(str(t) for t in types),
+                           getattr(x, "dtype", type(x).__name__)))
+    return _TYPES.get(x.dtype, -1)
+
+
+def _on_device(x: torch.Tensor, name: str) -> None:
+    if not x.is_cuda or x.device.index != torch.cuda.current_device():
+        raise ValueError("%s must be on the current device (cuda:%d), got %s"
+                         % (name, torch.cuda.current_device(), x.device))
+
+
+def _rows(x: torch.Tensor, name: str, width: Optional[int] = None):
+    """x as rows: (tensor, rows, ld).  A 2-D view whose rows are contiguous is taken as it
+    is; others are copied."""
+    _on_device(x, name)
+    if x.dim() < 1 or (width is not None and x.shape[-1] != width):
+        raise ValueError("%s must have rows of %s elements, got %s"
+                         % (name, width if width is not None else "some", tuple(x.shape)))
+    w = x.shape[-1]
+    if x.dim() != 2:
+        x = x.reshape(-1, w) if w else x.reshape(0, 0)
+    if (w > 1 and x.stride(1) != 1) or (x.shape[0] > 1 and x.stride(0) < w):
+        x = x.contiguous()
+    return x, x.shape[0], x.stride(0) if x.shape[0] > 1 else w
+
+
+def _vector(x: torch.Tensor, n: int, dtype, name: str) -> torch.Tensor:
+    if not isinstance(x, torch.Tensor) or x.dtype != dtype:
+        raise TypeError("%s must be a tensor of %s, got %s"
+                        % (name, dtype, getattr(x, "dtype", type(x).__name__)))
+    _on_device(x, name)
+    if x.numel() != n:
+        raise ValueError("%s must have %d elements, got %s" % (name, n, tuple(x.shape)))
+    return x.reshape(-1).contiguous()
+
+
+def _scratch(nbytes: int) -> Optional[torch.Tensor]:
+    """A call's own workspace: of the current stream, so calls on several streams may overlap."""
+    return torch.empty(nbytes, dtype=torch.uint8, device="cuda") if nbytes else None
+
+
+@dataclasses.dataclass
+class Normed:
+    out: torch.Tensor              # the norm, like x
+    sum: torch.Tensor              # x + residual, like x (x itself without a residual)
+    rstd: torch.Tensor             # float32, one for each row
+
+
+@dataclasses.dataclass
+class NormedBytes:
+    q: torch.Tensor                # int8, the shape of x
+    scale: torch.Tensor            # float32, one for each row
+    sum: torch.Tensor
+    rstd: torch.Tensor
+
+
+def _norm_inputs(x, weight, residual):
+    t = _type(x, "x")
+    xr, n, ldx = _rows(x, "x")
+    width = xr.shape[1]
+    if width < 1:
+        raise ValueError("x must have rows of one element at least")
+    w = _vector(weight, width, x.dtype, "weight")
+    rr, ldr = None, 0
+    if residual is not None:
+        if residual.dtype != x.dtype or residual.shape != x.shape:
+            raise ValueError("residual must be like x: %s %s" % (x.dtype, tuple(x.shape)))
+        rr, _, ldr = _rows(residual, "residual", width)
+    return t, xr, n, ldx, width, w, rr, ldr
+
+
+def add_rms_norm(x, weight, residual=None, eps: float = 1e-6) -> Normed:
+    """s = x + residual and s * rstd * weight, rstd = 1 / sqrt(mean(s^2) + eps) over the last
+    dimension (kr_add_rms_norm)."""
+    t, xr, n, ldx, width, w, rr, ldr = _norm_inputs(x, weight, residual)
+    out = torch.empty(x.shape, dtype=x.dtype, device="cuda")
+    total = x if residual is None else torch.empty_like(out)
+    rstd = torch.empty(x.shape[:-1], dtype=torch.float32, device="cuda")
+    _check("kr_add_rms_norm",
+           _lib.kr_add_rms_norm(t, n, width, _ptr(xr), ldx, _ptr(rr), ldr, _ptr(w), eps,
+                                None if residual is None else _ptr(total), width, _ptr(out),
+                                width, _ptr(rstd), _stream()))
+    return Normed(out, total, rstd)
+
+
+def add_rms_norm_bytes(x, weight, residual=None, eps: float = 1e-6) -> NormedBytes:
+    """add_rms_norm with the norm held in 8-bit integers and a scale for each row: q * scale
+    (kr_add_rms_norm_bytes)."""
+    t, xr, n, ldx, width, w, rr, ldr = _norm_inputs(x, weight, residual)
+    q = torch.empty(x.shape, dtype=torch.int8, device="cuda")
+    total = x if residual is None else torch.empty(x.shape, dtype=x.dtype, device="cuda")
+    scale, rstd = torch.empty((2,) + x.shape[:-1], dtype=torch.float32, device="cuda").unbind(0)
+    _check("kr_add_rms_norm_bytes",
+           _lib.kr_add_rms_norm_bytes(t, n, width, _ptr(xr), ldx, _ptr(rr), ldr, _ptr(w), eps,
+                                      None if residual is None else _ptr(total), width, _ptr(q),
+                                      width, _ptr(scale), _ptr(rstd), _stream()))
+    return NormedBytes(q, scale, total, rstd)
+
+
+def add_rms_norm_backward(dout, sum, weight, rstd, dsum=None):
+    """(dx, dweight) of add_rms_norm from its sum and rstd; dsum is the gradient that reaches
+    the sum by the residual's path.  dx, like dout, is the gradient of x and of residual;
+    dweight is float32 (kr_add_rms_norm_backward)."""
+    t = _type(dout, "dout")
+    if sum.dtype != dout.dtype or sum.shape != dout.shape:
+        raise ValueError("sum must be like dout: %s %s" % (dout.dtype, tuple(dout.shape)))
+    if dsum is not None and (dsum.dtype != dout.dtype or dsum.shape != dout.shape):
+        raise ValueError("dsum must be like dout: %s %s" % (dout.dtype, tuple(dout.shape)))
+    gr, n, ldo = _rows(dout, "dout")
+    width = gr.shape[1]
+    if width < 1:
+        raise ValueError("dout must have rows of one element at least")
+    sr, _, lds = _rows(sum, "sum", width)
+    w = _vector(weight, width, dout.dtype, "weight")
+    f = _vector(rstd, n, torch.float32, "rstd")
+    dr, ldd = None, 0
+    if dsum is not None:
+        dr, _, ldd = _rows(dsum, "dsum", width)
+    dx = torch.empty(dout.shape, dtype=dout.dtype, device="cuda")
+    dw = torch.empty(width, dtype=torch.float32, device="cuda")
+    wsb = _lib.kr_add_rms_norm_backward_workspace(t, n, width)
+    ws = _scratch(wsb)
+    _check("kr_add_rms_norm_backward",
+           _lib.kr_add_rms_norm_backward(t, n, width, _ptr(gr), ldo, _ptr(sr), lds, _ptr(w),
+                                         _ptr(f), _ptr(dr), ldd, _ptr(dx), width, _ptr(dw),
+                                         _ptr(ws), wsb, _stream()))
+    return dx, dw
