@@ -558,6 +558,67 @@ kr_status kr_add_rms_norm_backward(int32_t type, int64_t rows, int64_t width, co
 size_t kr_add_rms_norm_backward_workspace(int32_t type, int64_t rows, int64_t width);
 
 /*
+ * kr_byte_matmul -- product of 8-bit integers with a scale for each token and channel:
+ *   out[i][j] = sa[i] * sb[j] * sum over k of a[i][k] * b[j][k]
+ * The sum is exact (32-bit integers); the scales are applied in 32 bits, (sum * sa) * sb, and
+ * the result is rounded once to out's type.
+ *   a [m][k], sa [m]   tokens (kr_add_rms_norm_bytes)
+ *   b [n][k], sb [n]   channels: a weight matrix as its rows of inputs
+ *   type               of out
+ * m >= 0, n >= 1, k >= 1; KR_EUNSUPPORTED for m >= 2^31, n > 2^30 or k > 131071.  Strides are
+ * in elements.  The workspace (16-byte aligned) depends on sizes, strides and addresses; 0:
+ * none needed, or an invalid argument.
+ */
+typedef struct kr_bytes {
+    int64_t m, n, k;
+    const int8_t *a, *b;
+    int64_t lda, ldb;
+    const float *sa, *sb;
+} kr_bytes;
+kr_status kr_byte_matmul(const kr_bytes *p, int32_t type, void *out, int64_t ldo, void *ws,
+                         size_t ws_bytes, void *stream);
+size_t kr_byte_matmul_workspace(const kr_bytes *p);
+
+/*
+ * kr_gated_projection -- h = act(x Wg^T) * (x Wu^T), both projections, the activation and the
+ * product in one kernel.
+ *   type        KR_F16 or KR_BF16, of every matrix
+ *   act         KR_SILU: g / (1 + e^-g);  KR_GELU: g / 2 (1 + tanh(sqrt(2 / pi) (g + 0.044715 g^3)))
+ *   x           [rows][width]
+ *   wg, wu      [hidden][width]
+ *   out         [rows][hidden]
+ * rows >= 0, width >= 1, hidden >= 1; KR_EUNSUPPORTED for rows >= 2^31 or more than 2^20
+ * columns.  The workspace (16-byte aligned) depends on sizes, strides and addresses; 0: none
+ * needed, or an invalid argument.
+ */
+#define KR_SILU 0
+#define KR_GELU 1
+typedef struct kr_gated {
+    int32_t type, act;
+    int64_t rows, width, hidden;
+    const void *x, *wg, *wu;
+    int64_t ldx, ldg, ldu;
+} kr_gated;
+kr_status kr_gated_projection(const kr_gated *g, void *out, int64_t ldo, void *ws,
+                              size_t ws_bytes, void *stream);
+size_t kr_gated_projection_workspace(const kr_gated *g);
+
+/*
+ * kr_gated_projection_backward -- gradients of kr_gated_projection from its inputs and the
+ * gradient dh of its output; nothing is kept from the forward call (g and u are computed
+ * again).  With dg = dh * u * act'(g) and du = dh * act(g),
+ *   dx = dg Wg + du Wu,  dwg = dg^T x,  dwu = du^T x
+ * dg and du are rounded to the type between the products (they are the products' operands), in
+ * the workspace; in KR_F16 what leaves its range is infinite or 0 there.  dx, dwg and dwu are
+ * rounded once and overwritten; without rows the weight gradients are 0.  No output may
+ * overlap an input.
+ */
+kr_status kr_gated_projection_backward(const kr_gated *g, const void *dh, int64_t ldh, void *dx,
+                                       int64_t lddx, void *dwg, int64_t lddg, void *dwu,
+                                       int64_t lddu, void *ws, size_t ws_bytes, void *stream);
+size_t kr_gated_projection_backward_workspace(const kr_gated *g);
+
+/*
  * kr_set_phase_events -- instrumentation for profilers and benchmarks (not part of the
  * method).  When both events are non-NULL, later calls record `start_event` on their
  * stream right before the phase's first kernel and `stop_event` right after its last

@@ -36,6 +36,19 @@ _vp, _i32, _i64, _f64, _sz = (ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64,
                               ctypes.c_double, ctypes.c_size_t)
 _f32 = ctypes.c_float
 _SP = ctypes.POINTER(KrSpace)
+
+
+class KrBytes(ctypes.Structure):
+    _fields_ = [("m", _i64), ("n", _i64), ("k", _i64), ("a", _vp), ("b", _vp), ("lda", _i64),
+                ("ldb", _i64), ("sa", _vp), ("sb", _vp)]
+
+
+class KrGated(ctypes.Structure):
+    _fields_ = [("type", _i32), ("act", _i32), ("rows", _i64), ("width", _i64), ("hidden", _i64),
+                ("x", _vp), ("wg", _vp), ("wu", _vp), ("ldx", _i64), ("ldg", _i64), ("ldu", _i64)]
+
+
+_BP, _GP = ctypes.POINTER(KrBytes), ctypes.POINTER(KrGated)
 _SIGS = {
     "kr_evaluate_partition": (_i32, [_SP, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp]),
     "kr_candidates_per_partition": (_i64, [_SP]),
@@ -79,6 +92,13 @@ _SIGS = {
     "kr_add_rms_norm_backward": (_i32, [_i32, _i64, _i64, _vp, _i64, _vp, _i64, _vp, _vp, _vp,
                                         _i64, _vp, _i64, _vp, _vp, _sz, _vp]),
     "kr_add_rms_norm_backward_workspace": (_sz, [_i32, _i64, _i64]),
+    "kr_byte_matmul": (_i32, [_BP, _i32, _vp, _i64, _vp, _sz, _vp]),
+    "kr_byte_matmul_workspace": (_sz, [_BP]),
+    "kr_gated_projection": (_i32, [_GP, _vp, _i64, _vp, _sz, _vp]),
+    "kr_gated_projection_workspace": (_sz, [_GP]),
+    "kr_gated_projection_backward": (_i32, [_GP, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _vp,
+                                            _sz, _vp]),
+    "kr_gated_projection_backward_workspace": (_sz, [_GP]),
     "kr_status_string": (ctypes.c_char_p, [_i32]),
     "kr_set_phase_events": (_i32, [_i32, _vp, _vp]),
 }
@@ -712,8 +732,7 @@ def _type(x: torch.Tensor, name: str, types=tuple(_TYPES)) -> int:
 
 def _on_device(x: torch.Tensor, name: str) -> None:
     if not x.is_cuda or x.device.index != torch.cuda.current_device():
-        raise ValueError("%s must be on the current device (cuda:%d), got %s"
-                         % (name, torch.cuda.current_device(), x.device))
+        raise ValueError("%s must be on the current device, got %s" % (name, x.device))
 
 
 def _rows(x: torch.Tensor, name: str, width: Optional[int] = None):
@@ -832,3 +851,83 @@ def add_rms_norm_backward(dout, sum, weight, rstd, dsum=None):
                                          _ptr(f), _ptr(dr), ldd, _ptr(dx), width, _ptr(dw),
                                          _ptr(ws), wsb, _stream()))
     return dx, dw
+
+
+def byte_matmul(a, sa, b, sb, dtype=torch.bfloat16) -> torch.Tensor:
+    """sa * sb * (a b^T) of int8 rows a [..., k] and b [n][k], a float32 scale for each row of
+    either; the result, [..., n], in dtype (kr_byte_matmul)."""
+    if dtype not in _TYPES:
+        raise TypeError("dtype must be %s, got %s" % (" or ".join(map(str, _TYPES)), dtype))
+    _type(a, "a", (torch.int8,))
+    _type(b, "b", (torch.int8,))
+    ar, m, lda = _rows(a, "a")
+    k = ar.shape[1]
+    if b.dim() != 2 or k < 1 or b.shape[0] < 1:
+        raise ValueError("a and b must have rows of one element at least, b two dimensions")
+    br, n, ldb = _rows(b, "b", k)
+    fa = _vector(sa, m, torch.float32, "sa")
+    fb = _vector(sb, n, torch.float32, "sb")
+    out = torch.empty(a.shape[:-1] + (n,), dtype=dtype, device="cuda")
+    p = KrBytes(m, n, k, ar.data_ptr(), br.data_ptr(), lda, ldb, fa.data_ptr(), fb.data_ptr())
+    wsb = _lib.kr_byte_matmul_workspace(ctypes.byref(p))
+    ws = _scratch(wsb)
+    _check("kr_byte_matmul",
+           _lib.kr_byte_matmul(ctypes.byref(p), _TYPES[dtype], _ptr(out), n, _ptr(ws), wsb,
+                               _stream()))
+    return out
+
+
+_ACTS = {"silu": 0, "gelu": 1}
+
+
+def _gated(x, wg, wu, act):
+    t = _type(x, "x", (torch.float16, torch.bfloat16))
+    if act not in _ACTS:
+        raise ValueError("act must be one of %s, got %r" % (", ".join(_ACTS), act))
+    xr, n, ldx = _rows(x, "x")
+    width = xr.shape[1]
+    for w, name in ((wg, "wg"), (wu, "wu")):
+        if not isinstance(w, torch.Tensor) or w.dtype != x.dtype:
+            raise TypeError("%s must be a tensor of %s" % (name, x.dtype))
+        if w.dim() != 2 or w.shape != wg.shape or w.shape[0] < 1 or width < 1:
+            raise ValueError("wg and wu must be [hidden][%d], got %s" % (width, tuple(w.shape)))
+    gr, hidden, ldg = _rows(wg, "wg", width)
+    ur, _, ldu = _rows(wu, "wu", width)
+    g = KrGated(t, _ACTS[act], n, width, hidden, xr.data_ptr(), gr.data_ptr(), ur.data_ptr(), ldx,
+                ldg, ldu)
+    return g, (xr, gr, ur)
+
+
+def gated_projection(x, wg, wu, act: str = "silu") -> torch.Tensor:
+    """act(x wg^T) * (x wu^T) of x [..., width] and wg, wu [hidden][width], act "silu" or
+    "gelu" (kr_gated_projection)."""
+    g, keep = _gated(x, wg, wu, act)
+    out = torch.empty(x.shape[:-1] + (g.hidden,), dtype=x.dtype, device="cuda")
+    wsb = _lib.kr_gated_projection_workspace(ctypes.byref(g))
+    ws = _scratch(wsb)
+    _check("kr_gated_projection",
+           _lib.kr_gated_projection(ctypes.byref(g), _ptr(out), g.hidden, _ptr(ws), wsb,
+                                    _stream()))
+    return out
+
+
+def gated_projection_backward(dh, x, wg, wu, act: str = "silu"):
+    """(dx, dwg, dwu) of gated_projection from its inputs and the gradient dh of its output
+    (kr_gated_projection_backward)."""
+    g, keep = _gated(x, wg, wu, act)
+    if not isinstance(dh, torch.Tensor) or dh.dtype != x.dtype:
+        raise TypeError("dh must be a tensor of %s" % x.dtype)
+    if dh.shape != x.shape[:-1] + (g.hidden,):
+        raise ValueError("dh must be %s, got %s" % (tuple(x.shape[:-1]) + (g.hidden,),
+                                                    tuple(dh.shape)))
+    hr, _, ldh = _rows(dh, "dh", g.hidden)
+    dx = torch.empty(x.shape, dtype=x.dtype, device="cuda")
+    dwg = torch.empty(wg.shape, dtype=x.dtype, device="cuda")
+    dwu = torch.empty(wg.shape, dtype=x.dtype, device="cuda")
+    wsb = _lib.kr_gated_projection_backward_workspace(ctypes.byref(g))
+    ws = _scratch(wsb)
+    _check("kr_gated_projection_backward",
+           _lib.kr_gated_projection_backward(ctypes.byref(g), _ptr(hr), ldh, _ptr(dx), g.width,
+                                             _ptr(dwg), g.width, _ptr(dwu), g.width, _ptr(ws), wsb,
+                                             _stream()))
+    return dx, dwg, dwu

@@ -1,0 +1,52 @@
+// Launch arguments of the projections.
+#pragma once
+
+#include "kr_mma.h"
+
+namespace kr {
+
+// Rows of `bytes` bytes copied to rows of `to_ld` bytes (a multiple of 16), the rest of each
+// filled with zeros.
+hipError_t launch_pad(const void *from, int64_t from_ld, int64_t rows, int64_t bytes, void *to,
+                      int64_t to_ld, hipStream_t st);
+
+// gated.hip.  x [m][k], wg and wu [n][k] as operands that the tiles take, k_bytes of k a row.
+struct GatedArgs {
+    int type, act;
+    int64_t m, n;             // rows, hidden
+    int64_t k_bytes;
+    Operand x, wg, wu;        // plain
+    void *out;                // [m][n]
+    int64_t ldo;
+    void *part;               // gated_part bytes
+};
+size_t gated_part(int64_t m, int64_t n, int64_t k_bytes);
+hipError_t launch_gated(const GatedArgs &a, hipStream_t st);
+
+struct GatedBackArgs {
+    GatedArgs f;              // out, ldo unused
+    int64_t width;            // k in elements
+    const void *dh;
+    int64_t ldh;
+    char *d;                  // [m][2 n_pad]: dg, du, each padded with zeros to n_pad
+    int64_t n_pad;
+    void *dx, *dwg, *dwu;
+    int64_t lddx, lddg, lddu;
+};
+size_t gated_back_part(int64_t m, int64_t n, int64_t n_pad, int64_t width, int64_t k_bytes);
+hipError_t launch_gated_back(const GatedBackArgs &a, hipStream_t st);
+
+// bytes.hip
+struct BytesArgs {
+    int out_type;
+    int64_t m, n, k_bytes;
+    Operand a, b;
+    const float *sa, *sb;
+    void *out;
+    int64_t ldo;
+    void *part;
+};
+size_t bytes_part(int64_t m, int64_t n, int64_t k_bytes);
+hipError_t launch_bytes(const BytesArgs &a, hipStream_t st);
+
+}  // namespace kr
