@@ -239,6 +239,38 @@ __device__ inline void read_done()
     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
 }
 
+// The block's waves meet; memory accesses are not moved across.
+__device__ inline void block_barrier() { asm volatile("s_barrier" ::: "memory"); }
+
+// A block's sums to the output, or to its split's part.
+template <int BM, int BN, int WM, int WN, typename Out, typename Acc>
+__device__ inline void put_tile(const MmaArgs &a, const Out &out, const Acc (&acc)[BM / WM / 16][BN / WN / 16],
+                                int64_t m0, int64_t n0, int wm, int wn, int split, int lane)
+{
+    constexpr int TM = BM / WM / 16, TN = BN / WN / 16;
+    constexpr bool TWO = Out::PLANES == 2;
+    const int row = lane % 16, col = lane / 16 * 4;
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+        const int64_t m = m0 + wm * (BM / WM) + i * 16 + row;
+        if (m >= a.m) continue;
+#pragma unroll
+        for (int j = 0; j < (TWO ? TN / 2 : TN); ++j) {
+            const int64_t n = n0 + wn * (BN / WN / Out::PLANES) + j * 16 + col;
+            if (n >= out.columns(a.n)) continue;
+            const Acc v0 = acc[i][j], v1 = acc[i][TWO ? j + TN / 2 : j];
+            if (a.splits > 1) {
+                typedef decltype(v0[0] + v0[0]) S;
+                S *p = (S *)a.part + ((int64_t)split * Out::PLANES * a.m + m) * a.n;
+                store4(p, (int)n, a.n, (const S *)&v0);
+                if (TWO) store4(p + (int64_t)a.m * a.n, (int)n, a.n, (const S *)&v1);
+            } else {
+                out.put(m, (int)n, v0, v1);
+            }
+        }
+    }
+}
+
 // One product kernel.  Out says what happens to the sums:
 //   PLANES         1, or 2: B's tile is half of b[0], half of b[1] (same rows), two sums
 //   put(m, n, v0, v1)   four outputs from n on of row m, from the first and second plane
@@ -317,26 +349,135 @@ __global__ __launch_bounds__(WM *WN * 64) void mma_kernel(MmaArgs a, Out out)
         read_done();
     }
 
-    const int row = lane % 16, col = lane / 16 * 4;
+    put_tile<BM, BN, WM, WN>(a, out, acc, m0, n0, wm, wn, split, lane);
+}
+
+// The same for 256 x 256 tiles, with the two waves of each SIMD taking turns: while one waits for
+// its reads of LDS, the other keeps the matrix cores busy.  A step is four phases, one for each
+// quarter of a wave's 128 x 64 sums (64 x 32 each, 16 matrix instructions); a phase is a memory
+// part and a matrix part with a barrier after either, and waves 4 .. 7 run one barrier behind
+// waves 0 .. 3.
+//
+//   phase   reads        sums       slots of waves 0-3 / 4-7 (a slot ends with a barrier)
+//   0       A0, B0       A0 B0      8s,     8s + 1  /  8s + 1, 8s + 2
+//   1       B1           A0 B1      8s + 2, 8s + 3  /  8s + 3, 8s + 4
+//   2       A1           A1 B1      8s + 4, 8s + 5  /  8s + 5, 8s + 6
+//   3       copies of    A1 B0      8s + 6, 8s + 7  /  8s + 7, 8s + 8
+//           step s + 2
+//
+// The last reads of step s's buffer are phase 2's, waited for inside slots 8s + 4 and 8s + 5, so
+// the copies that overwrite it from slot 8s + 6 on come after them.  A wave waits for its own
+// copies of step s + 1 (a whole step old by then) in phase 3's memory part, slots 8s + 6 and
+// 8s + 7; step s + 1's first reads are in slots 8s + 8 and 8s + 9.
+template <typename E, bool A_CROSSED, bool B_CROSSED, typename Out>
+__global__ __launch_bounds__(512) void mma_wide_kernel(MmaArgs a, Out out)
+{
+    constexpr int BM = 256, BN = 256, WM = 2, WN = 4, NW = 8;
+    constexpr bool TWO = Out::PLANES == 2;
+    typedef typename Mma<E>::Acc Acc;
+    __shared__ __align__(1024) char lds[2][(BM + BN) * kStep];
+
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int wm = wave / WN, wn = wave % WN;
+    int tm, tn, split;
+    tile_of(a, &tm, &tn, &split);
+    const int64_t m0 = (int64_t)tm * BM;
+    const int64_t n0 = (int64_t)tn * (TWO ? BN / 2 : BN);
+
+    typedef TileLoader<A_CROSSED, BM, NW> LoadA;
+    typedef TileLoader<B_CROSSED, BN, NW> LoadB;
+    constexpr int COPIES = LoadA::N + LoadB::N;
+    LoadA la;
+    LoadB lb;
+    TileReader<A_CROSSED, BM> ra;
+    TileReader<B_CROSSED, BN> rb;
+    ra.init(lane);
+    rb.init(lane);
+
+    Acc acc[8][4];
 #pragma unroll
-    for (int i = 0; i < TM; ++i) {
-        const int64_t m = m0 + wm * (BM / WM) + i * 16 + row;
-        if (m >= a.m) continue;
+    for (int i = 0; i < 8; ++i)
 #pragma unroll
-        for (int j = 0; j < (TWO ? TN / 2 : TN); ++j) {
-            const int64_t n = n0 + wn * (OUT_N / WN) + j * 16 + col;
-            if (n >= out.columns(a.n)) continue;
-            const Acc v0 = acc[i][j], v1 = acc[i][TWO ? j + TN / 2 : j];
-            if (a.splits > 1) {
-                typedef decltype(v0[0] + v0[0]) S;
-                S *p = (S *)a.part + ((int64_t)split * Out::PLANES * a.m + m) * a.n;
-                store4(p, (int)n, a.n, (const S *)&v0);
-                if (TWO) store4(p + (int64_t)a.m * a.n, (int)n, a.n, (const S *)&v1);
-            } else {
-                out.put(m, (int)n, v0, v1);
-            }
+        for (int j = 0; j < 4; ++j) acc[i][j] = Acc{0, 0, 0, 0};
+
+    const int begin = split * a.per_split, end = min(begin + a.per_split, a.steps * a.pairs);
+    int pair = -1;
+    auto load = [&](int s, int buf) {
+        const int p = s >= a.steps ? 1 : 0;
+        if (p != pair) {
+            pair = p;
+            la.init(a.a[p], m0, wave, lane);
+            const int h = TWO ? wave & 1 : p;  // a wave copies rows of one plane only
+            lb.template init<TWO>(a.b[h], n0, wave, lane);
         }
+        const int t = s - p * a.steps;
+        const int64_t k_left = a.k_bytes - (int64_t)t * kStep;
+        la.load(t, k_left, lds[buf], wave);
+        lb.load(t, k_left, lds[buf] + BM * kStep, wave);
+    };
+
+    i32x4 fa[2][4], fb[2][2][2];  // [half of the step][16 rows]; B: [quarter] in front
+    auto read_a = [&](const char *at, int q) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) fa[h][i] = ra.read(at, wm * 128 + q * 64 + i * 16, h);
+    };
+    auto read_b = [&](const char *at, int q) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+                fb[q][h][j] = rb.read(at + BM * kStep, wn * 64 + q * 32 + j * 16, h);
+    };
+    auto sums = [&](int qa, int qb) {
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+                    acc[qa * 4 + i][qb * 2 + j] =
+                        mma(E(), fb[qb][h][j], fa[h][i], acc[qa * 4 + i][qb * 2 + j]);
+        __builtin_amdgcn_s_setprio(0);
+        __builtin_amdgcn_sched_barrier(0);
+        block_barrier();
+    };
+
+    if (begin < end) load(begin, 0);
+    if (begin + 1 < end) {
+        load(begin + 1, 1);
+        arrived<COPIES>();
+    } else {
+        arrived<0>();
     }
+    if (wm == 1) block_barrier();
+    for (int s = begin; s < end; ++s) {
+        const int buf = (s - begin) & 1;
+        const char *at = lds[buf];
+        read_a(at, 0);
+        read_b(at, 0);
+        block_barrier();
+        sums(0, 0);
+        read_b(at, 1);
+        block_barrier();
+        sums(0, 1);
+        read_a(at, 1);
+        read_done();
+        sums(1, 1);
+        if (s + 2 < end) {
+            load(s + 2, buf);
+            arrived<COPIES>();
+        } else {
+            arrived<0>();
+        }
+        sums(1, 0);
+    }
+    if (wm == 0) block_barrier();
+    put_tile<BM, BN, WM, WN>(a, out, acc, m0, n0, wm, wn, split, lane);
 }
 
 // The splits' sums added in turn, then put: four outputs a thread.
@@ -379,7 +520,7 @@ hipError_t launch_mma(MmaArgs a, const MmaPlan &p, const Out &out, hipStream_t s
     a.per_split = p.per_split;
     const unsigned blocks = (unsigned)(p.tiles_m * p.tiles_n * p.splits);
     if (p.large)
-        mma_kernel<E, A_CROSSED, B_CROSSED, 256, 256, 2, 4, Out><<<blocks, 512, 0, st>>>(a, out);
+        mma_wide_kernel<E, A_CROSSED, B_CROSSED, Out><<<blocks, 512, 0, st>>>(a, out);
     else
         mma_kernel<E, A_CROSSED, B_CROSSED, 128, 128, 2, 2, Out><<<blocks, 256, 0, st>>>(a, out);
     if (p.splits > 1) {
