@@ -121,10 +121,10 @@ struct Laid {
     const void *from;
     int64_t from_ld, bytes;
     bool copy;
-    Laid(const void *p, int64_t ld, int64_t rows, int64_t bytes_, Carve &c)
+    Laid(const void *p, int64_t ld, int64_t rows, int64_t bytes_, Carve &c, bool always = false)
         : from(p), from_ld(rows > 1 ? ld : padded(bytes_)), bytes(bytes_)
     {
-        copy = (uintptr_t)p % 16 || from_ld % 16 || bytes % 16 || from_ld > kLdMost;
+        copy = always || (uintptr_t)p % 16 || from_ld % 16 || bytes % 16 || from_ld > kLdMost;
         if (copy) {
             const int64_t to = padded(bytes);
             op = Operand{c.take(rows * to), to, rows, to};
@@ -153,10 +153,14 @@ bool gated_fits(const kr_gated *g)
 
 struct GatedLaid {
     Laid x, wg, wu;
-    GatedLaid(const kr_gated *g, Carve &c)
-        : x(g->x, g->ldx * 2, g->rows, g->width * 2, c), wg(g->wg, g->ldg * 2, g->hidden, g->width * 2, c),
-          wu(g->wu, g->ldu * 2, g->hidden, g->width * 2, c)
+    // one_ld: both weights' rows the same distance apart (one sum over both takes them)
+    GatedLaid(const kr_gated *g, Carve &c, bool one_ld)
+        : x(g->x, g->ldx * 2, g->rows, g->width * 2, c),
+          wg(g->wg, g->ldg * 2, g->hidden, g->width * 2, c, one_ld && g->ldg != g->ldu),
+          wu(g->wu, g->ldu * 2, g->hidden, g->width * 2, c, one_ld && (wg.copy || g->ldg != g->ldu))
     {
+        if (one_ld && wu.copy && !wg.copy)
+            wg = Laid(g->wg, g->ldg * 2, g->hidden, g->width * 2, c, true);
     }
     GatedArgs args(const kr_gated *g) const
     {
@@ -181,7 +185,7 @@ struct GatedLaid {
 
 kr_status gated_run(const kr_gated *g, void *out, int64_t ldo, Carve &c, hipStream_t st)
 {
-    const GatedLaid l(g, c);
+    const GatedLaid l(g, c, false);
     GatedArgs a = l.args(g);
     a.out = out;
     a.ldo = ldo;
@@ -193,7 +197,7 @@ kr_status gated_run(const kr_gated *g, void *out, int64_t ldo, Carve &c, hipStre
 
 kr_status gated_back_run(const kr_gated *g, GatedBackArgs &b, Carve &c, hipStream_t st)
 {
-    const GatedLaid l(g, c);
+    const GatedLaid l(g, c, true);
     b.f = l.args(g);
     b.width = g->width;
     b.n_pad = (g->hidden + 7) / 8 * 8;

@@ -16,18 +16,18 @@ struct PutScaled {
     int n;
     const float *sa, *sb;
     __device__ __host__ int columns(int c) const { return c; }
-    __device__ void put(int64_t m, int c, i32x4 s, i32x4) const
+    __device__ void put(int64_t m, int c, const int *s, const int *) const
     {
         const float f = sa[m];
-        float v[4];
+        float v[8];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
+        for (int e = 0; e < 8; ++e) {
             v[e] = c + e < n ? (float)s[e] * f * sb[c + e] : 0.0f;
             // the compiler would fold the last product into float16's rounding; kept apart, it
             // is rounded to 32 bits as the contract says, for every type
             asm("" : "+v"(v[e]));
         }
-        store4(out + m * ldo, c, n, v);
+        store8(out + m * ldo, c, n, v);
     }
 };
 

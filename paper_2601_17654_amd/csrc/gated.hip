@@ -37,12 +37,12 @@ struct PutGated {
     int64_t ldo;
     int n, act;
     __device__ __host__ int columns(int c) const { return c; }
-    __device__ void put(int64_t m, int c, f32x4 g, f32x4 u) const
+    __device__ void put(int64_t m, int c, const float *g, const float *u) const
     {
-        float v[4];
+        float v[8];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = g[e] * activation(g[e], act).p * u[e];
-        store4(out + m * ldo, c, n, v);
+        for (int e = 0; e < 8; ++e) v[e] = g[e] * activation(g[e], act).p * u[e];
+        store8(out + m * ldo, c, n, v);
     }
 };
 
@@ -54,30 +54,20 @@ struct PutGatedBack {
     int64_t ldh;
     int n, n_pad, act;
     __device__ __host__ int columns(int) const { return n_pad; }
-    __device__ void put(int64_t m, int c, f32x4 g, f32x4 u) const
+    __device__ void put(int64_t m, int c, const float *g, const float *u) const
     {
-        struct __attribute__((packed)) Loose {
-            T v[4];
-        } h;
-        const T *from = dh + m * ldh;
-        if (c + 4 <= n) {
-            h = *(const Loose *)(from + c);
-        } else {
+        float x[8], dg[8], du[8];
+        floats(load_row(dh + m * ldh, c, n), x);  // zeros past n, and dg and du with them
 #pragma unroll
-            for (int e = 0; e < 4; ++e) h.v[e] = c + e < n ? from[c + e] : (T)0.0f;
-        }
-        float dg[4], du[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
+        for (int e = 0; e < 8; ++e) {
             const Act a = activation(g[e], act);
-            const float x = (float)h.v[e];
             const float slope = a.p + g[e] * a.p * (1.0f - a.p) * a.dz;
-            dg[e] = c + e < n ? x * u[e] * slope : 0.0f;
-            du[e] = c + e < n ? x * (g[e] * a.p) : 0.0f;
+            dg[e] = x[e] * u[e] * slope;
+            du[e] = x[e] * (g[e] * a.p);
         }
         T *to = d + m * 2 * n_pad;
-        store4(to, c, n_pad, dg);
-        store4(to + n_pad, c, n_pad, du);
+        store8(to, c, n_pad, dg);
+        store8(to + n_pad, c, n_pad, du);
     }
 };
 
@@ -88,9 +78,9 @@ struct PutRows {
     int64_t ldo;
     int n;
     __device__ __host__ int columns(int c) const { return c; }
-    __device__ void put(int64_t m, int c, f32x4 v, f32x4) const
+    __device__ void put(int64_t m, int c, const float *v, const float *) const
     {
-        store4(out + m * ldo, c, n, (const float *)&v);
+        store8(out + m * ldo, c, n, v);
     }
 };
 
@@ -102,12 +92,12 @@ struct PutTwoRows {
     int64_t ld_first, ld_second;
     int rows, pad, n;
     __device__ __host__ int columns(int c) const { return c; }
-    __device__ void put(int64_t m, int c, f32x4 v, f32x4) const
+    __device__ void put(int64_t m, int c, const float *v, const float *) const
     {
         const bool two = m >= pad;
         const int64_t r = two ? m - pad : m;
         if (r < rows)
-            store4(two ? second + r * ld_second : first + r * ld_first, c, n, (const float *)&v);
+            store8(two ? second + r * ld_second : first + r * ld_first, c, n, v);
     }
 };
 

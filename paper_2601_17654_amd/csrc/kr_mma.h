@@ -6,18 +6,19 @@
 // contiguous in m ("crossed": row k holds m = 0, 1, ...).  A block computes a BM x BN tile with
 // one wave per (BM / WM) x (BN / WN) part, over k in steps of 128 bytes (64 16-bit values or
 // 128 bytes).  Operand tiles go from memory straight to LDS, 16 bytes a lane, and from there to
-// registers in the matrix instructions' layout: 16 rows x 16 bytes of k for each group of 16
-// lanes.
+// registers in the layout of the 32 x 32 matrix instructions: 32 rows x 16 bytes of k for each
+// half of a wave.  (They take half the operand registers of the 16 x 16 ones for the same
+// products, and with them less power: under full load the clock is what the power leaves.)
 //
 // LDS layout.  A direct copy writes 64 lanes' 16 bytes side by side, so the order within a tile
 // is chosen by what each lane fetches:
-//  - plain: 128 bytes a row; 16-byte chunk c of row r sits at place c ^ (r / 2 % 8).  The 16
-//    rows that a group of lanes reads at once then lie in 16 different 16-byte places of the
-//    256 bytes that the 64 banks hold.
+//  - plain: 128 bytes a row; 16-byte chunk c of row r sits at place c ^ (r / 2 % 8).  16
+//    consecutive rows, read at one c, then lie in 16 different 16-byte places of the 256 bytes
+//    that the 64 banks hold.
 //  - crossed: one k a row; 32-byte block b (16 values) of row k sits at place b ^ f(k), f(k) =
-//    k % 4 + 4 * (k / 8 % 4) (k / 8 % 2 where a row has 8 blocks).  The transposing read takes
-//    4 rows x 32 bytes for each group of 16 lanes, the four groups 8 rows apart: 16 different
-//    places (8).
+//    2 (k % 4) + 8 (k / 8 % 2) (2 (k % 4) where a row has 8 blocks).  The transposing read takes
+//    4 rows x 32 bytes for each group of 16 lanes; two groups read neighbouring blocks of the
+//    same rows, the other two the rows 8 further on: 16 different places (8, twice).
 // Whatever lies outside an operand is read as zero: rows past its end by the buffer's bound, k
 // past the end of a plain row by an offset beyond that bound.
 #pragma once
@@ -36,31 +37,37 @@ constexpr int kStep = 128;               // bytes of k a step
 constexpr uint32_t kNowhere = 1u << 31;  // an offset past every buffer
 constexpr uint32_t kBufferMost = kNowhere - 1;
 
-// An element type's matrix instruction: 16 x 16 outputs, 64 bytes of k.  The first operand's
-// rows become the registers of a lane (4 in a row), the second's the lanes.
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef int i32x16 __attribute__((ext_vector_type(16)));
+
+// An element type's matrix instruction: 32 x 32 outputs, 32 bytes of k.  The second operand's
+// rows become the lanes (row lane % 32), the first's the registers: register r is its row
+// 8 (r / 4) + 4 (lane / 32) + r % 4.
 template <typename E>
 struct Mma {
-    typedef f32x4 Acc;
-    static constexpr int size = 2;
+    typedef f32x16 Acc;
+    typedef f32x4 Quad;
+    typedef float Sum;
 };
 template <>
 struct Mma<int8_t> {
-    typedef i32x4 Acc;
-    static constexpr int size = 1;
+    typedef i32x16 Acc;
+    typedef i32x4 Quad;
+    typedef int Sum;
 };
-__device__ inline f32x4 mma(bf16, i32x4 a, i32x4 b, f32x4 c)
+__device__ inline f32x16 mma(bf16, i32x4 a, i32x4 b, f32x16 c)
 {
-    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a),
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a),
                                                    __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
-__device__ inline f32x4 mma(f16, i32x4 a, i32x4 b, f32x4 c)
+__device__ inline f32x16 mma(f16, i32x4 a, i32x4 b, f32x16 c)
 {
-    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a),
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a),
                                                   __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
 }
-__device__ inline i32x4 mma(int8_t, i32x4 a, i32x4 b, i32x4 c)
+__device__ inline i32x16 mma(int8_t, i32x4 a, i32x4 b, i32x16 c)
 {
-    return __builtin_amdgcn_mfma_i32_16x16x64_i8(a, b, c, 0, 0, 0);
+    return __builtin_amdgcn_mfma_i32_32x32x32_i8(a, b, c, 0, 0, 0);
 }
 
 // One operand as the host describes it: `rows` rows (m, or k where crossed) of `bytes` bytes,
@@ -101,10 +108,10 @@ struct TileLoader {
     int64_t left;       // bytes of the operand from there
     int64_t step;       // bytes from one k step to the next
 
-    // first: the tile's first m.  HALVES (plain): LDS rows are strips of 64, the first 32 of
-    // one operand, the rest of another, both at 32 operand rows a strip.
-    template <bool HALVES = false>
-    __device__ void init(const Operand &o, int64_t first, int wave, int lane)
+    // first: the tile's first m; map: the m, from there, of a row of LDS (runs of 8 rows of LDS,
+    // 16 where crossed, are runs of m).
+    template <typename Map>
+    __device__ void init(const Operand &o, int64_t first, int wave, int lane, Map map)
     {
         if (CROSSED) {
             base = o.p + first * 2;
@@ -121,56 +128,68 @@ struct TileLoader {
             const int i = wave * N + j;
             const int r = i * (64 / LANES) + lane / LANES, c = lane % LANES;
             if (CROSSED) {
-                const int f = LANES == 32 ? (r & 3) | (r >> 3 & 3) << 2 : (r & 3) | (r >> 3 & 1) << 2;
-                off[j] = (uint32_t)r * (uint32_t)o.ld + (uint32_t)(c ^ f << 1) * 16;
+                const int f = (r & 3) << 1 | (LANES == 32 ? (r >> 3 & 1) << 3 : 0);
+                off[j] = (uint32_t)r * (uint32_t)o.ld + (uint32_t)map((c ^ f << 1) * 8) * 2;
             } else {
                 const int at = c ^ (r >> 1 & 7);
-                const int row = HALVES ? (r / 64) * 32 + r % 32 : r;
-                off[j] = (uint32_t)row * (uint32_t)o.ld + (uint32_t)at * 16;
+                off[j] = (uint32_t)map(r) * (uint32_t)o.ld + (uint32_t)at * 16;
                 chunk[j & 1] = (uint32_t)at * 16;
             }
         }
     }
 
-    // Starts the copies of step t; k_left: bytes of k from that step's start (plain).
-    __device__ void load(int t, int64_t k_left, char *lds, int wave) const
+    // The operand from step t on, `by` bytes from the one that init() took (another of its
+    // shape), as a buffer; an empty one where there is no such step.
+    __device__ i32x4 buffer(int t, int64_t by, bool there) const
     {
-        const int64_t rest = left - t * step;
+        const int64_t rest = there ? left - t * step : 0;
         const uint32_t records = rest <= 0 ? 0u : rest > kBufferMost ? kBufferMost : (uint32_t)rest;
-        const uint64_t at = (uint64_t)(base + t * step);
-        const i32x4 rsrc = {(int)at, (int)(at >> 32) & 0xFFFF, (int)records, 0x00020000};
-#pragma unroll
-        for (int j = 0; j < N; ++j) {
-            uint32_t o = off[j];
-            if (!CROSSED) o = (int64_t)chunk[j & 1] < k_left ? o : kNowhere;
-            copy_to_lds(rsrc, o, lds + (wave * N + j) * 1024);
-        }
+        const uint64_t at = (uint64_t)(base + by + t * step);
+        return i32x4{(int)at, (int)(at >> 32) & 0xFFFF, (int)records, 0x00020000};
+    }
+    // Starts the wave's copy j of a step; k_left: bytes of k from its start (plain).
+    __device__ void copy(int j, const i32x4 &rsrc, int64_t k_left, const char *lds, int wave) const
+    {
+        uint32_t o = off[j];
+        if (!CROSSED) o = (int64_t)chunk[j & 1] < k_left ? o : kNowhere;
+        copy_to_lds(rsrc, o, lds + (wave * N + j) * 1024);
     }
 };
 
-// Reads of a tile in LDS: rows (plain) or columns (crossed) first .. first + 15, half h of the
-// step (64 bytes of k).
+// Maps of a tile's rows: as they are;  strips of STRIP rows, one half of either plane.
+struct MapSame {
+    __device__ int operator()(int r) const { return r; }
+};
+template <int STRIP>
+struct MapPlanes {
+    __device__ int operator()(int r) const { return r / STRIP * (STRIP / 2) + r % (STRIP / 2); }
+};
+
+// Reads of a tile in LDS: rows (plain) or columns (crossed) first .. first + 31, quarter h of
+// the step (32 bytes of k).
 template <bool CROSSED, int ROWS>
 struct TileReader {
-    int at[2];  // plain: a lane's byte for either half
+    int at[4];  // plain: a lane's byte for each quarter
     int k0, fl;
 
     __device__ void init(int lane)
     {
-        const int g = lane / 16, i = lane % 16;
         if (CROSSED) {
-            k0 = (g * 8 + i / 4) * ROWS * 2 + (i % 4) * 8;
-            fl = ROWS == 256 ? i / 4 | g << 2 : i / 4 | (g & 1) << 2;
+            const int g = lane / 16, i = lane % 16;
+            k0 = ((g >> 1) * 8 + i / 4) * ROWS * 2 + (i % 4) * 8;
+            fl = (g & 1) ^ ((i / 4) << 1 | (ROWS == 256 ? (g >> 1) << 3 : 0));
         } else {
-            at[0] = i * kStep + ((g ^ i >> 1) << 4);
-            at[1] = i * kStep + (((4 + g) ^ i >> 1) << 4);
+            const int r = lane % 32;
+#pragma unroll
+            for (int h = 0; h < 4; ++h)
+                at[h] = r * kStep + (((h * 2 + lane / 32) ^ (r >> 1 & 7)) << 4);
         }
     }
     __device__ i32x4 read(const char *lds, int first, int h) const
     {
         if (!CROSSED) return *(const i32x4 *)(lds + first * kStep + at[h]);
         typedef __attribute__((address_space(3))) s16x4 *Lds;
-        const char *p = lds + k0 + ((first / 16 ^ fl) << 5) + h * 32 * ROWS * 2;
+        const char *p = lds + k0 + ((first / 16 ^ fl) << 5) + h * 16 * ROWS * 2;
         struct {
             s16x4 lo, hi;
         } x;
@@ -182,7 +201,8 @@ struct TileReader {
 
 // What a product's blocks have in common.
 struct MmaArgs {
-    Operand a[2], b[2];  // second pair: the second half of the sum, or B's second half
+    Operand a[2], b[2];  // second pair: the second half of the sum (of the first one's ld), or
+                         // B's second plane
     int m, n;            // outputs
     int64_t k_bytes;     // bytes of k in one pair (plain operands), rows of it where crossed
     int steps;           // k steps of one pair
@@ -208,64 +228,86 @@ __device__ inline void tile_of(const MmaArgs &a, int *tm, int *tn, int *split)
     *tn = t / size;
 }
 
+// Eight values to columns n .. n + 7 of a row of `width`.
 template <typename T, typename S>
-__device__ inline void store4(T *row, int n, int width, const S *v)
+__device__ inline void store8(T *row, int n, int width, const S *v)
 {
     struct __attribute__((packed)) Loose {
-        T v[4];
+        T v[8];
     };
-    if (n + 4 <= width) {
+    if (n + 8 <= width) {
         Loose x;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) x.v[e] = (T)v[e];
+        for (int e = 0; e < 8; ++e) x.v[e] = (T)v[e];
         *(Loose *)(row + n) = x;
     } else {
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
+        for (int e = 0; e < 8; ++e)
             if (n + e < width) row[n + e] = (T)v[e];
     }
 }
 
-// Waits for all but the last LEFT of the wave's copies to LDS, then for the block.
+// Waits for all but the last LEFT of the wave's copies to LDS and for all its reads of LDS, then
+// for the block: what was copied may be read, what was read may be overwritten.
 template <int LEFT>
-__device__ inline void arrived()
+__device__ inline void block_wait()
 {
-    asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(LEFT) : "memory");
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LEFT) : "memory");
 }
 
-// Waits for the wave's reads of LDS, then for the block: what was read may be overwritten.
-__device__ inline void read_done()
+// A block's sums to the output, or to its split's part.  Each wave takes them through its own
+// share of the LDS, 64 rows at a time: out of the matrix layout into rows of 8 neighbouring
+// columns a lane, so that whole lines are written, in a loop that is short in code (unrolled over
+// the registers, this part was 150 KB of instructions that every block fetched anew, a quarter of
+// a tile's time at 64 steps).  16-byte chunk c of row r lies at place c ^ r % 16.
+template <int BM, int BN, int WM, int WN, typename E, typename Out, typename Acc>
+__device__ inline void put_tile(E, const MmaArgs &a, const Out &out,
+                                const Acc (&acc)[BM / WM / 32][BN / WN / 32], char *lds, int64_t m0,
+                                int64_t n0, int wave, int split, int lane)
 {
-    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-}
-
-// The block's waves meet; memory accesses are not moved across.
-__device__ inline void block_barrier() { asm volatile("s_barrier" ::: "memory"); }
-
-// A block's sums to the output, or to its split's part.
-template <int BM, int BN, int WM, int WN, typename Out, typename Acc>
-__device__ inline void put_tile(const MmaArgs &a, const Out &out, const Acc (&acc)[BM / WM / 16][BN / WN / 16],
-                                int64_t m0, int64_t n0, int wm, int wn, int split, int lane)
-{
-    constexpr int TM = BM / WM / 16, TN = BN / WN / 16;
-    constexpr bool TWO = Out::PLANES == 2;
-    const int row = lane % 16, col = lane / 16 * 4;
+    constexpr int TM = BM / WM / 32, TN = BN / WN / 32, PLANES = Out::PLANES;
+    constexpr int STRIP = BN / WN, COLS = STRIP / PLANES;  // of a wave's sums, of its output
+    constexpr int LANES = COLS / 8;                        // lanes a row
+    typedef typename Mma<E>::Quad Quad;
+    typedef typename Mma<E>::Sum Sum;
+    static_assert(64 * STRIP * 4 <= 2 * (BM + BN) * kStep / (WM * WN), "a wave's share of LDS");
+    char *own = lds + wave * 64 * STRIP * 4;
+    const int wm = wave / WN, wn = wave % WN;
+    const int n = (int)n0 + wn * COLS + lane % LANES * 8;
 #pragma unroll
-    for (int i = 0; i < TM; ++i) {
-        const int64_t m = m0 + wm * (BM / WM) + i * 16 + row;
-        if (m >= a.m) continue;
+    for (int p = 0; p < TM / 2; ++p) {
 #pragma unroll
-        for (int j = 0; j < (TWO ? TN / 2 : TN); ++j) {
-            const int64_t n = n0 + wn * (BN / WN / Out::PLANES) + j * 16 + col;
-            if (n >= out.columns(a.n)) continue;
-            const Acc v0 = acc[i][j], v1 = acc[i][TWO ? j + TN / 2 : j];
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int j = 0; j < TN; ++j)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int row = i * 32 + lane % 32, c = j * 8 + q * 2 + lane / 32;
+                    Quad v;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) v[e] = acc[p * 2 + i][j][q * 4 + e];
+                    *(Quad *)(own + row * STRIP * 4 + ((c ^ row % 16) << 4)) = v;
+                }
+#pragma unroll 1
+        for (int it = 0; it < LANES; ++it) {
+            const int row = it * (64 / LANES) + lane / LANES;
+            const int64_t m = m0 + wm * (BM / WM) + p * 64 + row;
+            Quad v[PLANES][2];
+#pragma unroll
+            for (int k = 0; k < PLANES; ++k)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int c = k * COLS / 4 + lane % LANES * 2 + h;
+                    v[k][h] = *(const Quad *)(own + row * STRIP * 4 + ((c ^ row % 16) << 4));
+                }
+            if (m >= a.m || n >= out.columns(a.n)) continue;
+            const Sum *v0 = (const Sum *)v[0], *v1 = (const Sum *)v[PLANES - 1];
             if (a.splits > 1) {
-                typedef decltype(v0[0] + v0[0]) S;
-                S *p = (S *)a.part + ((int64_t)split * Out::PLANES * a.m + m) * a.n;
-                store4(p, (int)n, a.n, (const S *)&v0);
-                if (TWO) store4(p + (int64_t)a.m * a.n, (int)n, a.n, (const S *)&v1);
+                Sum *to = (Sum *)a.part + ((int64_t)split * PLANES * a.m + m) * a.n;
+                store8(to, n, a.n, v0);
+                if (PLANES == 2) store8(to + (int64_t)a.m * a.n, n, a.n, v1);
             } else {
-                out.put(m, (int)n, v0, v1);
+                out.put(m, n, v0, v1);
             }
         }
     }
@@ -273,107 +315,20 @@ __device__ inline void put_tile(const MmaArgs &a, const Out &out, const Acc (&ac
 
 // One product kernel.  Out says what happens to the sums:
 //   PLANES         1, or 2: B's tile is half of b[0], half of b[1] (same rows), two sums
-//   put(m, n, v0, v1)   four outputs from n on of row m, from the first and second plane
+//   put(m, n, v0, v1)   eight outputs from n on of row m, from the first and second plane
+//
+// Two steps' tiles are in LDS.  A wave's registers hold two quarters of a step: while the matrix
+// instructions of one run, the next is read, so the matrix cores wait for LDS only where a block
+// waits: once a step, after the last reads of its tile.  From there the tile is overwritten with
+// the step after next, whose copies have three quarters of a step to arrive before they are
+// waited for.  One wave per SIMD in the 256 x 256 form: its 128 x 128 sums halve the reads of LDS
+// against 8 waves' 128 x 64.
 template <typename E, bool A_CROSSED, bool B_CROSSED, int BM, int BN, int WM, int WN, typename Out>
 __global__ __launch_bounds__(WM *WN * 64) void mma_kernel(MmaArgs a, Out out)
 {
-    constexpr int NW = WM * WN, TM = BM / WM / 16, TN = BN / WN / 16;
+    constexpr int NW = WM * WN, TM = BM / WM / 32, TN = BN / WN / 32;
     constexpr bool TWO = Out::PLANES == 2;
-    constexpr int OUT_N = TWO ? BN / 2 : BN;  // output columns of a tile
-    static_assert(!TWO || BN / WN == 64, "a strip of both planes is 64 wide");
-    typedef typename Mma<E>::Acc Acc;
-    __shared__ __align__(1024) char lds[2][(BM + BN) * kStep];
-
-    const int lane = threadIdx.x & 63;
-    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-    const int wm = wave / WN, wn = wave % WN;
-    int tm, tn, split;
-    tile_of(a, &tm, &tn, &split);
-    const int64_t m0 = (int64_t)tm * BM;
-    const int64_t n0 = (int64_t)tn * OUT_N;
-
-    typedef TileLoader<A_CROSSED, BM, NW> LoadA;
-    typedef TileLoader<B_CROSSED, BN, NW> LoadB;
-    LoadA la;
-    LoadB lb;
-    TileReader<A_CROSSED, BM> ra;
-    TileReader<B_CROSSED, BN> rb;
-    ra.init(lane);
-    rb.init(lane);
-
-    Acc acc[TM][TN];
-#pragma unroll
-    for (int i = 0; i < TM; ++i)
-#pragma unroll
-        for (int j = 0; j < TN; ++j) acc[i][j] = Acc{0, 0, 0, 0};
-
-    const int begin = split * a.per_split, end = min(begin + a.per_split, a.steps * a.pairs);
-    int pair = -1;
-    auto load = [&](int s, int buf) {
-        const int p = s >= a.steps ? 1 : 0;
-        if (p != pair) {
-            pair = p;
-            la.init(a.a[p], m0, wave, lane);
-            // a wave copies rows of one half only: N * 8 = 32 of a strip's 64
-            const int h = TWO ? (wave * LoadB::N / 4) & 1 : p;
-            lb.template init<TWO>(a.b[h], n0, wave, lane);
-        }
-        const int t = s - p * a.steps;
-        const int64_t k_left = a.k_bytes - (int64_t)t * kStep;
-        la.load(t, k_left, lds[buf], wave);
-        lb.load(t, k_left, lds[buf] + BM * kStep, wave);
-    };
-
-    if (begin < end) load(begin, 0);
-    for (int s = begin; s < end; ++s) {
-        const int buf = (s - begin) & 1;
-        if (s + 1 < end) {
-            load(s + 1, buf ^ 1);
-            arrived<LoadA::N + LoadB::N>();  // all but the next step's
-        } else {
-            arrived<0>();
-        }
-        const char *sa = lds[buf], *sb = lds[buf] + BM * kStep;
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            i32x4 fa[TM], fb[TN];
-#pragma unroll
-            for (int i = 0; i < TM; ++i) fa[i] = ra.read(sa, wm * (BM / WM) + i * 16, h);
-#pragma unroll
-            for (int j = 0; j < TN; ++j) fb[j] = rb.read(sb, wn * (BN / WN) + j * 16, h);
-#pragma unroll
-            for (int i = 0; i < TM; ++i)
-#pragma unroll
-                for (int j = 0; j < TN; ++j) acc[i][j] = mma(E(), fb[j], fa[i], acc[i][j]);
-        }
-        read_done();
-    }
-
-    put_tile<BM, BN, WM, WN>(a, out, acc, m0, n0, wm, wn, split, lane);
-}
-
-// The same for 256 x 256 tiles, with the two waves of each SIMD taking turns: while one waits for
-// its reads of LDS, the other keeps the matrix cores busy.  A step is four phases, one for each
-// quarter of a wave's 128 x 64 sums (64 x 32 each, 16 matrix instructions); a phase is a memory
-// part and a matrix part with a barrier after either, and waves 4 .. 7 run one barrier behind
-// waves 0 .. 3.
-//
-//   phase   reads        sums       slots of waves 0-3 / 4-7 (a slot ends with a barrier)
-//   0       A0, B0       A0 B0      8s,     8s + 1  /  8s + 1, 8s + 2
-//   1       B1           A0 B1      8s + 2, 8s + 3  /  8s + 3, 8s + 4
-//   2       A1           A1 B1      8s + 4, 8s + 5  /  8s + 5, 8s + 6
-//   3       copies of    A1 B0      8s + 6, 8s + 7  /  8s + 7, 8s + 8
-//           step s + 2
-//
-// The last reads of step s's buffer are phase 2's, waited for inside slots 8s + 4 and 8s + 5, so
-// the copies that overwrite it from slot 8s + 6 on come after them.  A wave waits for its own
-// copies of step s + 1 (a whole step old by then) in phase 3's memory part, slots 8s + 6 and
-// 8s + 7; step s + 1's first reads are in slots 8s + 8 and 8s + 9.
-template <typename E, bool A_CROSSED, bool B_CROSSED, typename Out>
-__global__ __launch_bounds__(512) void mma_wide_kernel(MmaArgs a, Out out)
-{
-    constexpr int BM = 256, BN = 256, WM = 2, WN = 4, NW = 8;
-    constexpr bool TWO = Out::PLANES == 2;
+    constexpr int STRIP = BN / WN;
     typedef typename Mma<E>::Acc Acc;
     __shared__ __align__(1024) char lds[2][(BM + BN) * kStep];
 
@@ -387,7 +342,8 @@ __global__ __launch_bounds__(512) void mma_wide_kernel(MmaArgs a, Out out)
 
     typedef TileLoader<A_CROSSED, BM, NW> LoadA;
     typedef TileLoader<B_CROSSED, BN, NW> LoadB;
-    constexpr int COPIES = LoadA::N + LoadB::N;
+    constexpr int COPIES = LoadA::N + LoadB::N, BLOCK = TM * TN;
+    static_assert(!TWO || LoadB::N * 8 == STRIP / 2, "a wave copies rows of one plane only");
     LoadA la;
     LoadB lb;
     TileReader<A_CROSSED, BM> ra;
@@ -395,109 +351,102 @@ __global__ __launch_bounds__(512) void mma_wide_kernel(MmaArgs a, Out out)
     ra.init(lane);
     rb.init(lane);
 
-    Acc acc[8][4];
+    Acc acc[TM][TN];
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
+    for (int i = 0; i < TM; ++i)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) acc[i][j] = Acc{0, 0, 0, 0};
+        for (int j = 0; j < TN; ++j)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[i][j][e] = 0;
 
     const int begin = split * a.per_split, end = min(begin + a.per_split, a.steps * a.pairs);
-    int pair = -1;
-    auto load = [&](int s, int buf) {
-        const int p = s >= a.steps ? 1 : 0;
-        if (p != pair) {
-            pair = p;
-            la.init(a.a[p], m0, wave, lane);
-            const int h = TWO ? wave & 1 : p;  // a wave copies rows of one plane only
-            lb.template init<TWO>(a.b[h], n0, wave, lane);
+    la.init(a.a[0], m0, wave, lane, MapSame());
+    if (TWO)
+        lb.init(a.b[wave & 1], n0, wave, lane, MapPlanes<STRIP>());
+    else
+        lb.init(a.b[0], n0, wave, lane, MapSame());
+    const int64_t to_second_a = a.a[1].p - a.a[0].p, to_second_b = a.b[1].p - a.b[0].p;
+    i32x4 rsrc_a, rsrc_b;
+    int64_t k_left = 0;
+    auto aim = [&](int s) {  // the copies at step s
+        const bool second = s >= a.steps;
+        const int t = second ? s - a.steps : s;
+        k_left = a.k_bytes - (int64_t)t * kStep;
+        rsrc_a = la.buffer(t, second ? to_second_a : 0, s < end);
+        rsrc_b = lb.buffer(t, second ? to_second_b : 0, s < end);
+    };
+    auto copy = [&](int j, const char *to) {
+        if (j < LoadA::N)
+            la.copy(j, rsrc_a, k_left, to, wave);
+        else
+            lb.copy(j - LoadA::N, rsrc_b, k_left, to + BM * kStep, wave);
+    };
+
+    i32x4 fa[2][TM], fb[2][TN];
+    auto read = [&](int j, const char *at, int h) {
+        if (j < TN)
+            fb[h & 1][j] = rb.read(at + BM * kStep, wn * STRIP + j * 32, h);
+        else
+            fa[h & 1][j - TN] = ra.read(at, wm * (BM / WM) + (j - TN) * 32, h);
+    };
+    // The products of quarter h, with the reads of the next and, where asked for, copies between
+    // them: one of each in front of a matrix instruction.
+    auto quarter = [&](int h, const char *next, bool copies, const char *to) {
+#pragma unroll
+        for (int x = 0; x < BLOCK; ++x) {
+            if (x < TM + TN) read(x, next, h + 1 & 3);
+            if (copies) {
+#pragma unroll
+                for (int j = x * COPIES / BLOCK; j < (x + 1) * COPIES / BLOCK; ++j) copy(j, to);
+            }
+            const int i = x / TN, j = x % TN;
+            acc[i][j] = mma(E(), fb[h & 1][j], fa[h & 1][i], acc[i][j]);
+            __builtin_amdgcn_sched_barrier(0);
         }
-        const int t = s - p * a.steps;
-        const int64_t k_left = a.k_bytes - (int64_t)t * kStep;
-        la.load(t, k_left, lds[buf], wave);
-        lb.load(t, k_left, lds[buf] + BM * kStep, wave);
     };
 
-    i32x4 fa[2][4], fb[2][2][2];  // [half of the step][16 rows]; B: [quarter] in front
-    auto read_a = [&](const char *at, int q) {
+    // Past the last step the copies are of an empty buffer, zeros that nothing uses: every step
+    // is the same, and the waits too.
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
+    for (int k = 0; k < 2; ++k) {
+        aim(begin + k);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) fa[h][i] = ra.read(at, wm * 128 + q * 64 + i * 16, h);
-    };
-    auto read_b = [&](const char *at, int q) {
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int j = 0; j < 2; ++j)
-                fb[q][h][j] = rb.read(at + BM * kStep, wn * 64 + q * 32 + j * 16, h);
-    };
-    auto sums = [&](int qa, int qb) {
-        __builtin_amdgcn_sched_barrier(0);
-        __builtin_amdgcn_s_setprio(1);
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int j = 0; j < 2; ++j)
-                    acc[qa * 4 + i][qb * 2 + j] =
-                        mma(E(), fb[qb][h][j], fa[h][i], acc[qa * 4 + i][qb * 2 + j]);
-        __builtin_amdgcn_s_setprio(0);
-        __builtin_amdgcn_sched_barrier(0);
-        block_barrier();
-    };
-
-    if (begin < end) load(begin, 0);
-    if (begin + 1 < end) {
-        load(begin + 1, 1);
-        arrived<COPIES>();
-    } else {
-        arrived<0>();
+        for (int j = 0; j < COPIES; ++j) copy(j, lds[k]);
     }
-    if (wm == 1) block_barrier();
+    block_wait<COPIES>();
+#pragma unroll
+    for (int j = 0; j < TM + TN; ++j) read(j, lds[0], 0);
     for (int s = begin; s < end; ++s) {
         const int buf = (s - begin) & 1;
         const char *at = lds[buf];
-        read_a(at, 0);
-        read_b(at, 0);
-        block_barrier();
-        sums(0, 0);
-        read_b(at, 1);
-        block_barrier();
-        sums(0, 1);
-        read_a(at, 1);
-        read_done();
-        sums(1, 1);
-        if (s + 2 < end) {
-            load(s + 2, buf);
-            arrived<COPIES>();
-        } else {
-            arrived<0>();
-        }
-        sums(1, 0);
+        quarter(0, at, false, nullptr);
+        quarter(1, at, false, nullptr);
+        quarter(2, at, false, nullptr);
+        aim(s + 2);
+        block_wait<0>();
+        quarter(3, lds[buf ^ 1], true, at);
     }
-    if (wm == 0) block_barrier();
-    put_tile<BM, BN, WM, WN>(a, out, acc, m0, n0, wm, wn, split, lane);
+    block_wait<0>();  // the tiles' LDS is free, and no copy will write to it
+    put_tile<BM, BN, WM, WN>(E(), a, out, acc, lds[0], m0, n0, wave, split, lane);
 }
 
-// The splits' sums added in turn, then put: four outputs a thread.
+// The splits' sums added in turn, then put: eight outputs a thread.
 template <typename E, typename Out>
 __global__ __launch_bounds__(256) void mma_join_kernel(MmaArgs a, Out out)
 {
-    typedef typename Mma<E>::Acc Acc;
-    typedef decltype(Acc{}[0] + Acc{}[0]) S;
-    const int quads = (out.columns(a.n) + 3) / 4;
+    typedef typename Mma<E>::Sum Sum;
+    const int per = (out.columns(a.n) + 7) / 8;
     const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (id >= (int64_t)a.m * quads) return;
-    const int64_t m = id / quads;
-    const int n = (int)(id - m * quads) * 4;
-    Acc v[2] = {Acc{0, 0, 0, 0}, Acc{0, 0, 0, 0}};
+    if (id >= (int64_t)a.m * per) return;
+    const int64_t m = id / per;
+    const int n = (int)(id - m * per) * 8;
+    Sum v[2][8] = {};
     for (int s = 0; s < a.splits; ++s)
 #pragma unroll
         for (int p = 0; p < Out::PLANES; ++p) {
-            const S *q = (const S *)a.part + (((int64_t)s * Out::PLANES + p) * a.m + m) * a.n;
+            const Sum *q = (const Sum *)a.part + (((int64_t)s * Out::PLANES + p) * a.m + m) * a.n;
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
+            for (int e = 0; e < 8; ++e)
                 if (n + e < a.n) v[p][e] += q[n + e];
         }
     out.put(m, n, v[0], v[Out::PLANES - 1]);
@@ -505,7 +454,7 @@ __global__ __launch_bounds__(256) void mma_join_kernel(MmaArgs a, Out out)
 
 // How a product is cut into tiles.
 struct MmaPlan {
-    bool large;   // 256 x 256 tiles of 8 waves, else 128 x 128 of 4
+    bool large;   // 256 x 256 tiles, else 128 x 128
     int tiles_m, tiles_n, splits, per_split;
     int64_t part_bytes;
 };
@@ -520,12 +469,12 @@ hipError_t launch_mma(MmaArgs a, const MmaPlan &p, const Out &out, hipStream_t s
     a.per_split = p.per_split;
     const unsigned blocks = (unsigned)(p.tiles_m * p.tiles_n * p.splits);
     if (p.large)
-        mma_wide_kernel<E, A_CROSSED, B_CROSSED, Out><<<blocks, 512, 0, st>>>(a, out);
+        mma_kernel<E, A_CROSSED, B_CROSSED, 256, 256, 2, 2, Out><<<blocks, 256, 0, st>>>(a, out);
     else
         mma_kernel<E, A_CROSSED, B_CROSSED, 128, 128, 2, 2, Out><<<blocks, 256, 0, st>>>(a, out);
     if (p.splits > 1) {
-        const int64_t quads = (int64_t)a.m * ((out.columns(a.n) + 3) / 4);
-        mma_join_kernel<E, Out><<<(unsigned)((quads + 255) / 256), 256, 0, st>>>(a, out);
+        const int64_t threads = (int64_t)a.m * ((out.columns(a.n) + 7) / 8);
+        mma_join_kernel<E, Out><<<(unsigned)((threads + 255) / 256), 256, 0, st>>>(a, out);
     }
     return hipGetLastError();
 }

@@ -157,6 +157,22 @@ def test_strides_and_what_lies_beside(kr, dtype, gap, start):
     assert all(torch.equal(p, q) for p, q in zip(a, b))
 
 
+@pytest.mark.parametrize("at", [0, 1])
+def test_weights_of_unlike_strides(kr, at):
+    """One weight matrix inside a larger one, aligned and not, the other by itself."""
+    x, wg, wu, dh = make(90, 64, 48, torch.bfloat16, 2)
+    want = kr.gated_projection_backward(dh, x, wg, wu)
+    for start, gap in ((8, 8), (3, 2)):
+        big = torch.full((50, 64 + start + gap), float("nan"), dtype=torch.bfloat16, device="cuda")
+        view = big[1:-1, start:start + 64]
+        view.copy_((wg, wu)[at])
+        w = [wg, wu]
+        w[at] = view
+        got = kr.gated_projection_backward(dh, x, *w)
+        assert all(torch.equal(p, q) for p, q in zip(got, want))
+        assert torch.equal(kr.gated_projection(x, *w), kr.gated_projection(x, wg, wu))
+
+
 def test_outputs_inside_larger_matrices(kr):
     """The C entry points write their rows and nothing between them."""
     rows, width, hidden = 70, 40, 52
