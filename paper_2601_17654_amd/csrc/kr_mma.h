@@ -82,13 +82,13 @@ struct Operand {
 // Starts the copy of 16 bytes a lane to LDS, from byte `off` of a buffer; 64 lanes side by side.
 // Written out because the compiler, where it knows of such a copy, waits for all of them before
 // any read of LDS; here the waits are arrived() below.  There is no output register, and the
-// copies' LDS is read only after such a wait.  The five idle states cover what the compiler
-// cannot see inside: a scalar register that a vector instruction wrote, and m0.
+// copies' LDS is read only after such a wait.  The idle state stands between m0 and its use.  The
+// buffer's registers come from scalar arithmetic (a vector instruction's result would need five).
 __device__ inline void copy_to_lds(i32x4 rsrc, uint32_t off, const char *lds)
 {
     const uint32_t to = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char *)lds;
     asm volatile("s_mov_b32 m0, %0\n\t"
-                 "s_nop 4\n\t"
+                 "s_nop 0\n\t"
                  "buffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(off), "s"(rsrc)
                  : "memory", "m0");
 }
@@ -103,7 +103,8 @@ struct TileLoader {
     static_assert(N * 8 * NW == ROWS && (CROSSED || N % 2 == 0), "copies do not divide");
 
     uint32_t off[N];
-    uint32_t chunk[2];  // plain: byte of k that copies of either parity fetch
+    int chunk[2];       // plain: byte of k that copies of either parity fetch
+    uint32_t past[2];   //        kNowhere where that is past the end
     const char *base;   // of the tile's first row (column)
     int64_t left;       // bytes of the operand from there
     int64_t step;       // bytes from one k step to the next
@@ -133,7 +134,7 @@ struct TileLoader {
             } else {
                 const int at = c ^ (r >> 1 & 7);
                 off[j] = (uint32_t)map(r) * (uint32_t)o.ld + (uint32_t)at * 16;
-                chunk[j & 1] = (uint32_t)at * 16;
+                chunk[j & 1] = at * 16;
             }
         }
     }
@@ -147,12 +148,19 @@ struct TileLoader {
         const uint64_t at = (uint64_t)(base + by + t * step);
         return i32x4{(int)at, (int)(at >> 32) & 0xFFFF, (int)records, 0x00020000};
     }
-    // Starts the wave's copy j of a step; k_left: bytes of k from its start (plain).
-    __device__ void copy(int j, const i32x4 &rsrc, int64_t k_left, const char *lds, int wave) const
+    // Says how many bytes of k there are from the step's start (plain).
+    __device__ void bound(int64_t k_left)
     {
-        uint32_t o = off[j];
-        if (!CROSSED) o = (int64_t)chunk[j & 1] < k_left ? o : kNowhere;
-        copy_to_lds(rsrc, o, lds + (wave * N + j) * 1024);
+        if (!CROSSED) {
+            const int most = k_left < kStep ? (int)k_left : kStep;
+#pragma unroll
+            for (int j = 0; j < 2; ++j) past[j] = chunk[j] < most ? 0 : kNowhere;
+        }
+    }
+    // Starts the wave's copy j of a step.
+    __device__ void copy(int j, const i32x4 &rsrc, const char *lds, int wave) const
+    {
+        copy_to_lds(rsrc, CROSSED ? off[j] : off[j] | past[j & 1], lds + (wave * N + j) * 1024);
     }
 };
 
@@ -247,13 +255,16 @@ __device__ inline void store8(T *row, int n, int width, const S *v)
     }
 }
 
-// Waits for all but the last LEFT of the wave's copies to LDS and for all its reads of LDS, then
-// for the block: what was copied may be read, what was read may be overwritten.
+// Waits for all but the last LEFT of the wave's copies to LDS, then for the block: what was
+// copied may be read.
 template <int LEFT>
-__device__ inline void block_wait()
+__device__ inline void arrived()
 {
-    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LEFT) : "memory");
+    asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(LEFT) : "memory");
 }
+
+// Waits for the wave's reads of LDS, then for the block: what was read may be overwritten.
+__device__ inline void read_done() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
 // A block's sums to the output, or to its split's part.  Each wave takes them through its own
 // share of the LDS, 64 rows at a time: out of the matrix layout into rows of 8 neighbouring
@@ -288,7 +299,7 @@ __device__ inline void put_tile(E, const MmaArgs &a, const Out &out,
                     for (int e = 0; e < 4; ++e) v[e] = acc[p * 2 + i][j][q * 4 + e];
                     *(Quad *)(own + row * STRIP * 4 + ((c ^ row % 16) << 4)) = v;
                 }
-#pragma unroll 1
+#pragma unroll 4
         for (int it = 0; it < LANES; ++it) {
             const int row = it * (64 / LANES) + lane / LANES;
             const int64_t m = m0 + wm * (BM / WM) + p * 64 + row;
@@ -317,12 +328,31 @@ __device__ inline void put_tile(E, const MmaArgs &a, const Out &out,
 //   PLANES         1, or 2: B's tile is half of b[0], half of b[1] (same rows), two sums
 //   put(m, n, v0, v1)   eight outputs from n on of row m, from the first and second plane
 //
-// Two steps' tiles are in LDS.  A wave's registers hold two quarters of a step: while the matrix
-// instructions of one run, the next is read, so the matrix cores wait for LDS only where a block
-// waits: once a step, after the last reads of its tile.  From there the tile is overwritten with
-// the step after next, whose copies have three quarters of a step to arrive before they are
-// waited for.  One wave per SIMD in the 256 x 256 form: its 128 x 128 sums halve the reads of LDS
-// against 8 waves' 128 x 64.
+// Two steps' tiles are in LDS, and a wave's registers hold one more: the matrix instructions of
+// a step (4 quarters of TM x TN) run on what was read before them, and between them, one or two in
+// front of each, are
+//   the reads of quarters 1 to 3, from the step's beginning;
+//   from instruction T::free on, when every wave has its step in registers (a barrier): the
+//     copies of the step after next, over this one's tile;
+//   from T::next on, when every wave's copies of the next step have arrived (a barrier): the
+//     reads of its quarter 0.
+// The 256 x 256 form has one wave per SIMD: its 128 x 128 sums halve the reads of LDS against
+// 8 waves' 128 x 64.  There a copy follows every second matrix instruction: a CU takes 16 cycles
+// to address one, its four waves start theirs at the same time, and what they wait for each other
+// the matrix cores wait too (one after every instruction: 2 % slower).
+template <int BLOCK>
+struct Timing;  // copies(x): those started before instruction x;  reads: of quarter 0 each
+template <>
+struct Timing<16> {
+    static constexpr int free = 28, next = 52, reads = 1;
+    static constexpr int copies(int x) { return x - free < 32 ? (x - free + 1) / 2 : 16; }
+};
+template <>
+struct Timing<4> {
+    static constexpr int free = 12, next = 14, reads = 2;
+    static constexpr int copies(int x) { return (x - free) * 2; }
+};
+
 template <typename E, bool A_CROSSED, bool B_CROSSED, int BM, int BN, int WM, int WN, typename Out>
 __global__ __launch_bounds__(WM *WN * 64) void mma_kernel(MmaArgs a, Out out)
 {
@@ -342,7 +372,11 @@ __global__ __launch_bounds__(WM *WN * 64) void mma_kernel(MmaArgs a, Out out)
 
     typedef TileLoader<A_CROSSED, BM, NW> LoadA;
     typedef TileLoader<B_CROSSED, BN, NW> LoadB;
-    constexpr int COPIES = LoadA::N + LoadB::N, BLOCK = TM * TN;
+    constexpr int COPIES = LoadA::N + LoadB::N, BLOCK = TM * TN, READS = TM + TN;
+    typedef Timing<BLOCK> T;
+    static_assert(T::free >= 3 * READS && T::next + READS / T::reads <= 4 * BLOCK &&
+                      T::copies(T::free) == 0 && T::copies(4 * BLOCK) == COPIES,
+                  "the timing fits the tile");
     static_assert(!TWO || LoadB::N * 8 == STRIP / 2, "a wave copies rows of one plane only");
     LoadA la;
     LoadB lb;
@@ -367,42 +401,27 @@ __global__ __launch_bounds__(WM *WN * 64) void mma_kernel(MmaArgs a, Out out)
         lb.init(a.b[0], n0, wave, lane, MapSame());
     const int64_t to_second_a = a.a[1].p - a.a[0].p, to_second_b = a.b[1].p - a.b[0].p;
     i32x4 rsrc_a, rsrc_b;
-    int64_t k_left = 0;
     auto aim = [&](int s) {  // the copies at step s
         const bool second = s >= a.steps;
         const int t = second ? s - a.steps : s;
-        k_left = a.k_bytes - (int64_t)t * kStep;
+        la.bound(a.k_bytes - (int64_t)t * kStep);
+        lb.bound(a.k_bytes - (int64_t)t * kStep);
         rsrc_a = la.buffer(t, second ? to_second_a : 0, s < end);
         rsrc_b = lb.buffer(t, second ? to_second_b : 0, s < end);
     };
     auto copy = [&](int j, const char *to) {
         if (j < LoadA::N)
-            la.copy(j, rsrc_a, k_left, to, wave);
+            la.copy(j, rsrc_a, to, wave);
         else
-            lb.copy(j - LoadA::N, rsrc_b, k_left, to + BM * kStep, wave);
+            lb.copy(j - LoadA::N, rsrc_b, to + BM * kStep, wave);
     };
 
-    i32x4 fa[2][TM], fb[2][TN];
+    i32x4 fa[4][TM], fb[4][TN];
     auto read = [&](int j, const char *at, int h) {
         if (j < TN)
-            fb[h & 1][j] = rb.read(at + BM * kStep, wn * STRIP + j * 32, h);
+            fb[h][j] = rb.read(at + BM * kStep, wn * STRIP + j * 32, h);
         else
-            fa[h & 1][j - TN] = ra.read(at, wm * (BM / WM) + (j - TN) * 32, h);
-    };
-    // The products of quarter h, with the reads of the next and, where asked for, copies between
-    // them: one of each in front of a matrix instruction.
-    auto quarter = [&](int h, const char *next, bool copies, const char *to) {
-#pragma unroll
-        for (int x = 0; x < BLOCK; ++x) {
-            if (x < TM + TN) read(x, next, h + 1 & 3);
-            if (copies) {
-#pragma unroll
-                for (int j = x * COPIES / BLOCK; j < (x + 1) * COPIES / BLOCK; ++j) copy(j, to);
-            }
-            const int i = x / TN, j = x % TN;
-            acc[i][j] = mma(E(), fb[h & 1][j], fa[h & 1][i], acc[i][j]);
-            __builtin_amdgcn_sched_barrier(0);
-        }
+            fa[h][j - TN] = ra.read(at, wm * (BM / WM) + (j - TN) * 32, h);
     };
 
     // Past the last step the copies are of an empty buffer, zeros that nothing uses: every step
@@ -413,20 +432,33 @@ __global__ __launch_bounds__(WM *WN * 64) void mma_kernel(MmaArgs a, Out out)
 #pragma unroll
         for (int j = 0; j < COPIES; ++j) copy(j, lds[k]);
     }
-    block_wait<COPIES>();
+    arrived<COPIES>();
 #pragma unroll
     for (int j = 0; j < TM + TN; ++j) read(j, lds[0], 0);
     for (int s = begin; s < end; ++s) {
         const int buf = (s - begin) & 1;
-        const char *at = lds[buf];
-        quarter(0, at, false, nullptr);
-        quarter(1, at, false, nullptr);
-        quarter(2, at, false, nullptr);
+        const char *at = lds[buf], *next = lds[buf ^ 1];
         aim(s + 2);
-        block_wait<0>();
-        quarter(3, lds[buf ^ 1], true, at);
+#pragma unroll
+        for (int x = 0; x < 4 * BLOCK; ++x) {
+            if (x < 3 * READS) read(x % READS, at, 1 + x / READS);
+            if (x == T::free) read_done();
+            if (x == T::next) arrived<T::copies(T::next)>();
+            if (x >= T::free) {
+#pragma unroll
+                for (int j = T::copies(x); j < T::copies(x + 1); ++j) copy(j, at);
+            }
+            if (x >= T::next && x < T::next + READS / T::reads) {
+#pragma unroll
+                for (int j = 0; j < T::reads; ++j) read((x - T::next) * T::reads + j, next, 0);
+            }
+            const int h = x / BLOCK, i = x % BLOCK / TN, j = x % TN;
+            acc[i][j] = mma(E(), fb[h][j], fa[h][i], acc[i][j]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
     }
-    block_wait<0>();  // the tiles' LDS is free, and no copy will write to it
+    read_done();
+    arrived<0>();  // the tiles' LDS is free, and no copy will write to it
     put_tile<BM, BN, WM, WN>(E(), a, out, acc, lds[0], m0, n0, wave, split, lane);
 }
 
