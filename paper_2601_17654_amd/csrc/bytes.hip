@@ -16,13 +16,26 @@ struct PutScaled {
     int n;
     const float *sa, *sb;
     __device__ __host__ int columns(int c) const { return c; }
-    __device__ void put(int64_t m, int c, const int *s, const int *) const
+    struct Mine {
+        float f[8];
+    };
+    struct Fetched {
+        float f;
+    };
+    __device__ Mine mine(int c) const
     {
-        const float f = sa[m];
+        Mine x;
+        floats(load_row(sb, c, n), x.f);
+        floats(load_row(sb, c + 4, n), x.f + 4);
+        return x;
+    }
+    __device__ Fetched fetch(bool there, int64_t m, int) const { return {sa[there ? m : 0]}; }
+    __device__ void put(int64_t m, int c, const int *s, const int *, Mine b, Fetched a) const
+    {
         float v[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            v[e] = c + e < n ? (float)s[e] * f * sb[c + e] : 0.0f;
+            v[e] = (float)s[e] * a.f * b.f[e];
             // the compiler would fold the last product into float16's rounding; kept apart, it
             // is rounded to 32 bits as the contract says, for every type
             asm("" : "+v"(v[e]));

@@ -31,13 +31,13 @@ __device__ inline Act activation(float g, int act)
 }
 
 template <typename T>
-struct PutGated {
+struct PutGated : Plain {
     static constexpr int PLANES = 2;
     T *out;
     int64_t ldo;
     int n, act;
     __device__ __host__ int columns(int c) const { return c; }
-    __device__ void put(int64_t m, int c, const float *g, const float *u) const
+    __device__ void put(int64_t m, int c, const float *g, const float *u, Mine, Fetched) const
     {
         float v[8];
 #pragma unroll
@@ -54,10 +54,18 @@ struct PutGatedBack {
     int64_t ldh;
     int n, n_pad, act;
     __device__ __host__ int columns(int) const { return n_pad; }
-    __device__ void put(int64_t m, int c, const float *g, const float *u) const
+    typedef Pack<T, 8> Fetched;
+    struct Mine {
+    };
+    __device__ Mine mine(int) const { return {}; }
+    __device__ Fetched fetch(bool there, int64_t m, int c) const
+    {
+        return load_row(dh + (there ? m : 0) * ldh, there ? c : n, n);  // zeros past n
+    }
+    __device__ void put(int64_t m, int c, const float *g, const float *u, Mine, Fetched h) const
     {
         float x[8], dg[8], du[8];
-        floats(load_row(dh + m * ldh, c, n), x);  // zeros past n, and dg and du with them
+        floats(h, x);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             const Act a = activation(g[e], act);
@@ -72,13 +80,13 @@ struct PutGatedBack {
 };
 
 template <typename T>
-struct PutRows {
+struct PutRows : Plain {
     static constexpr int PLANES = 1;
     T *out;
     int64_t ldo;
     int n;
     __device__ __host__ int columns(int c) const { return c; }
-    __device__ void put(int64_t m, int c, const float *v, const float *) const
+    __device__ void put(int64_t m, int c, const float *v, const float *, Mine, Fetched) const
     {
         store8(out + m * ldo, c, n, v);
     }
@@ -86,13 +94,13 @@ struct PutRows {
 
 // Rows [0, rows) to one matrix, [pad, pad + rows) to another.
 template <typename T>
-struct PutTwoRows {
+struct PutTwoRows : Plain {
     static constexpr int PLANES = 1;
     T *first, *second;
     int64_t ld_first, ld_second;
     int rows, pad, n;
     __device__ __host__ int columns(int c) const { return c; }
-    __device__ void put(int64_t m, int c, const float *v, const float *) const
+    __device__ void put(int64_t m, int c, const float *v, const float *, Mine, Fetched) const
     {
         const bool two = m >= pad;
         const int64_t r = two ? m - pad : m;
@@ -121,7 +129,7 @@ MmaArgs two_planes(const GatedArgs &a)
 template <typename T>
 hipError_t forward(const GatedArgs &a, hipStream_t st)
 {
-    const PutGated<T> out{(T *)a.out, a.ldo, (int)a.n, a.act};
+    const PutGated<T> out{{}, (T *)a.out, a.ldo, (int)a.n, a.act};
     const MmaArgs x = two_planes(a);
     return launch_mma<T, false, false>(x, mma_plan(a.m, a.n, 2, x.steps), out, st);
 }
@@ -157,7 +165,7 @@ hipError_t backward(const GatedBackArgs &a, hipStream_t st)
         y.steps = steps_of(y.k_bytes);
         y.pairs = 2;
         y.part = (float *)a.f.part;
-        const PutRows<T> dx{(T *)a.dx, a.lddx, (int)a.width};
+        const PutRows<T> dx{{}, (T *)a.dx, a.lddx, (int)a.width};
         if (const hipError_t e = launch_mma<T, false, true>(y, plan_dx(m, a.n_pad, a.width), dx, st);
             e != hipSuccess)
             return e;
@@ -171,7 +179,7 @@ hipError_t backward(const GatedBackArgs &a, hipStream_t st)
     z.steps = (int)((m + 63) / 64);
     z.pairs = 1;
     z.part = (float *)a.f.part;
-    const PutTwoRows<T> dw{(T *)a.dwg, (T *)a.dwu, a.lddg, a.lddu, (int)n, (int)a.n_pad, (int)a.width};
+    const PutTwoRows<T> dw{{}, (T *)a.dwg, (T *)a.dwu, a.lddg, a.lddu, (int)n, (int)a.n_pad, (int)a.width};
     return launch_mma<T, true, true>(z, plan_dw(m, a.n_pad, a.width), dw, st);
 }
 

@@ -236,6 +236,16 @@ __device__ inline void tile_of(const MmaArgs &a, int *tm, int *tn, int *split)
     *tn = t / size;
 }
 
+// Nothing that a lane needs or reads.
+struct Plain {
+    struct Mine {
+    };
+    struct Fetched {
+    };
+    __device__ Mine mine(int) const { return {}; }
+    __device__ Fetched fetch(bool, int64_t, int) const { return {}; }
+};
+
 // Eight values to columns n .. n + 7 of a row of `width`.
 template <typename T, typename S>
 __device__ inline void store8(T *row, int n, int width, const S *v)
@@ -279,12 +289,14 @@ __device__ inline void put_tile(E, const MmaArgs &a, const Out &out,
     constexpr int TM = BM / WM / 32, TN = BN / WN / 32, PLANES = Out::PLANES;
     constexpr int STRIP = BN / WN, COLS = STRIP / PLANES;  // of a wave's sums, of its output
     constexpr int LANES = COLS / 8;                        // lanes a row
+    constexpr int TOGETHER = 4;                            // rows a lane has in hand
     typedef typename Mma<E>::Quad Quad;
     typedef typename Mma<E>::Sum Sum;
     static_assert(64 * STRIP * 4 <= 2 * (BM + BN) * kStep / (WM * WN), "a wave's share of LDS");
     char *own = lds + wave * 64 * STRIP * 4;
     const int wm = wave / WN, wn = wave % WN;
-    const int n = (int)n0 + wn * COLS + lane % LANES * 8;
+    const int n = (int)n0 + wn * COLS + lane % LANES * 8, columns = out.columns(a.n);
+    const typename Out::Mine mine = out.mine(n);
 #pragma unroll
     for (int p = 0; p < TM / 2; ++p) {
 #pragma unroll
@@ -299,26 +311,36 @@ __device__ inline void put_tile(E, const MmaArgs &a, const Out &out,
                     for (int e = 0; e < 4; ++e) v[e] = acc[p * 2 + i][j][q * 4 + e];
                     *(Quad *)(own + row * STRIP * 4 + ((c ^ row % 16) << 4)) = v;
                 }
-#pragma unroll 4
-        for (int it = 0; it < LANES; ++it) {
-            const int row = it * (64 / LANES) + lane / LANES;
-            const int64_t m = m0 + wm * (BM / WM) + p * 64 + row;
-            Quad v[PLANES][2];
+#pragma unroll 1
+        for (int it = 0; it < LANES; it += TOGETHER) {
+            const int64_t m1 = m0 + wm * (BM / WM) + p * 64 + lane / LANES;
+            typename Out::Fetched f[TOGETHER];
 #pragma unroll
-            for (int k = 0; k < PLANES; ++k)
+            for (int u = 0; u < TOGETHER; ++u) {
+                const int64_t m = m1 + (it + u) * (64 / LANES);
+                f[u] = out.fetch(m < a.m && n < columns, m, n);
+            }
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const int c = k * COLS / 4 + lane % LANES * 2 + h;
-                    v[k][h] = *(const Quad *)(own + row * STRIP * 4 + ((c ^ row % 16) << 4));
+            for (int u = 0; u < TOGETHER; ++u) {
+                const int row = (it + u) * (64 / LANES) + lane / LANES;
+                const int64_t m = m1 + (it + u) * (64 / LANES);
+                Quad v[PLANES][2];
+#pragma unroll
+                for (int k = 0; k < PLANES; ++k)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const int c = k * COLS / 4 + lane % LANES * 2 + h;
+                        v[k][h] = *(const Quad *)(own + row * STRIP * 4 + ((c ^ row % 16) << 4));
+                    }
+                if (m >= a.m || n >= columns) continue;
+                const Sum *v0 = (const Sum *)v[0], *v1 = (const Sum *)v[PLANES - 1];
+                if (a.splits > 1) {
+                    Sum *to = (Sum *)a.part + ((int64_t)split * PLANES * a.m + m) * a.n;
+                    store8(to, n, a.n, v0);
+                    if (PLANES == 2) store8(to + (int64_t)a.m * a.n, n, a.n, v1);
+                } else {
+                    out.put(m, n, v0, v1, mine, f[u]);
                 }
-            if (m >= a.m || n >= out.columns(a.n)) continue;
-            const Sum *v0 = (const Sum *)v[0], *v1 = (const Sum *)v[PLANES - 1];
-            if (a.splits > 1) {
-                Sum *to = (Sum *)a.part + ((int64_t)split * PLANES * a.m + m) * a.n;
-                store8(to, n, a.n, v0);
-                if (PLANES == 2) store8(to + (int64_t)a.m * a.n, n, a.n, v1);
-            } else {
-                out.put(m, n, v0, v1);
             }
         }
     }
@@ -326,7 +348,11 @@ __device__ inline void put_tile(E, const MmaArgs &a, const Out &out,
 
 // One product kernel.  Out says what happens to the sums:
 //   PLANES         1, or 2: B's tile is half of b[0], half of b[1] (same rows), two sums
-//   put(m, n, v0, v1)   eight outputs from n on of row m, from the first and second plane
+//   columns(n)     columns to put, n or more
+//   Mine mine(n)   what a lane needs for its columns n .. n + 7 in every row
+//   Fetched fetch(there, m, n)   what it reads for them of row m, asked for several rows ahead
+//   put(m, n, v0, v1, mine, fetched)   eight outputs from n on of row m, from the first and second
+//                                      plane
 //
 // Two steps' tiles are in LDS, and a wave's registers hold one more: the matrix instructions of
 // a step (4 quarters of TM x TN) run on what was read before them, and between them, one or two in
@@ -481,7 +507,7 @@ __global__ __launch_bounds__(256) void mma_join_kernel(MmaArgs a, Out out)
             for (int e = 0; e < 8; ++e)
                 if (n + e < a.n) v[p][e] += q[n + e];
         }
-    out.put(m, n, v[0], v[Out::PLANES - 1]);
+    out.put(m, n, v[0], v[Out::PLANES - 1], out.mine(n), out.fetch(true, m, n));
 }
 
 // How a product is cut into tiles.
