@@ -717,9 +717,13 @@ def launch_timing_frontier(kind1, kind2, ops, p_static: float, kmax: int, out_ca
 
 # ---- transformer-block operators ------------------------------------------------------
 # Values are float32, float16 or bfloat16 tensors on the current device; leading dimensions
-# are rows.  Outputs and workspaces are allocated on the current stream.
+# are rows.  Outputs and workspaces are allocated on the current stream: calls on several
+# streams may overlap.  A single token's call takes about as long here as on the device, so
+# these functions hand over plain integers and ask for each thing once.
 
 _TYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+    lambda dev: torch.cuda.current_stream(dev).cuda_stream)
 
 
 def _type(x: torch.Tensor, name: str, types=tuple(_TYPES)) -> int:
@@ -730,39 +734,60 @@ def _type(x: torch.Tensor, name: str, types=tuple(_TYPES)) -> int:
     return _TYPES.get(x.dtype, -1)
 
 
-def _on_device(x: torch.Tensor, name: str) -> None:
-    if not x.is_cuda or x.device.index != torch.cuda.current_device():
+def _here(x: torch.Tensor, name: str) -> int:
+    """The current device, which x must be on."""
+    if not x.is_cuda or x.get_device() != torch.cuda.current_device():
         raise ValueError("%s must be on the current device, got %s" % (name, x.device))
+    return x.get_device()
 
 
-def _rows(x: torch.Tensor, name: str, width: Optional[int] = None):
+def _rows(x: torch.Tensor, name: str, dev: int, width: Optional[int] = None):
     """x as rows: (tensor, rows, ld).  A 2-D view whose rows are contiguous is taken as it
     is; others are copied."""
-    _on_device(x, name)
-    if x.dim() < 1 or (width is not None and x.shape[-1] != width):
-        raise ValueError("%s must have rows of %s elements, got %s"
-                         % (name, width if width is not None else "some", tuple(x.shape)))
-    w = x.shape[-1]
-    if x.dim() != 2:
-        x = x.reshape(-1, w) if w else x.reshape(0, 0)
-    if (w > 1 and x.stride(1) != 1) or (x.shape[0] > 1 and x.stride(0) < w):
+    if x.get_device() != dev:
+        raise ValueError("%s must be on the current device, got %s" % (name, x.device))
+    shape = x.shape
+    if len(shape) < 1 or shape[-1] < 1 or (width is not None and shape[-1] != width):
+        raise ValueError("%s must have rows of %s, got %s"
+                         % (name, "%d elements" % width if width is not None
+                            else "one element at least", tuple(shape)))
+    w = shape[-1]
+    if len(shape) != 2:
+        x = x.reshape(-1, w)
+    n = x.shape[0]
+    ld, step = x.stride()
+    if (step != 1 and w > 1) or (ld < w and n > 1):
         x = x.contiguous()
-    return x, x.shape[0], x.stride(0) if x.shape[0] > 1 else w
+        ld = w
+    return x, n, ld if n > 1 else w
 
 
-def _vector(x: torch.Tensor, n: int, dtype, name: str) -> torch.Tensor:
+def _vector(x: torch.Tensor, n: int, dtype, name: str, dev: int) -> torch.Tensor:
     if not isinstance(x, torch.Tensor) or x.dtype != dtype:
         raise TypeError("%s must be a tensor of %s, got %s"
                         % (name, dtype, getattr(x, "dtype", type(x).__name__)))
-    _on_device(x, name)
+    if x.get_device() != dev:
+        raise ValueError("%s must be on the current device, got %s" % (name, x.device))
     if x.numel() != n:
         raise ValueError("%s must have %d elements, got %s" % (name, n, tuple(x.shape)))
-    return x.reshape(-1).contiguous()
+    return x if x.is_contiguous() else x.contiguous()
 
 
-def _scratch(nbytes: int) -> Optional[torch.Tensor]:
-    """A call's own workspace: of the current stream, so calls on several streams may overlap."""
-    return torch.empty(nbytes, dtype=torch.uint8, device="cuda") if nbytes else None
+def _like(x: torch.Tensor, other: torch.Tensor, name: str, of: str) -> None:
+    if not isinstance(x, torch.Tensor) or x.dtype != other.dtype or x.shape != other.shape:
+        raise ValueError("%s must be like %s: %s %s" % (name, of, other.dtype, tuple(other.shape)))
+
+
+def _new(shape, dtype) -> torch.Tensor:
+    return torch.empty(shape, dtype=dtype, device="cuda")
+
+
+def _scratch(nbytes: int):
+    """A call's own workspace and its address."""
+    if not nbytes:
+        return None, None
+    ws = torch.empty(nbytes, dtype=torch.uint8, device="cuda")
+    return ws, ws.data_ptr()
 
 
 @dataclasses.dataclass
@@ -782,44 +807,45 @@ class NormedBytes:
 
 def _norm_inputs(x, weight, residual):
     t = _type(x, "x")
-    xr, n, ldx = _rows(x, "x")
+    dev = _here(x, "x")
+    xr, n, ldx = _rows(x, "x", dev)
     width = xr.shape[1]
-    if width < 1:
-        raise ValueError("x must have rows of one element at least")
-    w = _vector(weight, width, x.dtype, "weight")
+    w = _vector(weight, width, x.dtype, "weight", dev)
     rr, ldr = None, 0
     if residual is not None:
-        if residual.dtype != x.dtype or residual.shape != x.shape:
-            raise ValueError("residual must be like x: %s %s" % (x.dtype, tuple(x.shape)))
-        rr, _, ldr = _rows(residual, "residual", width)
-    return t, xr, n, ldx, width, w, rr, ldr
+        _like(residual, x, "residual", "x")
+        rr, _, ldr = _rows(residual, "residual", dev, width)
+    return t, dev, xr, n, ldx, width, w, rr, ldr
 
 
 def add_rms_norm(x, weight, residual=None, eps: float = 1e-6) -> Normed:
     """s = x + residual and s * rstd * weight, rstd = 1 / sqrt(mean(s^2) + eps) over the last
     dimension (kr_add_rms_norm)."""
-    t, xr, n, ldx, width, w, rr, ldr = _norm_inputs(x, weight, residual)
-    out = torch.empty(x.shape, dtype=x.dtype, device="cuda")
-    total = x if residual is None else torch.empty_like(out)
-    rstd = torch.empty(x.shape[:-1], dtype=torch.float32, device="cuda")
+    t, dev, xr, n, ldx, width, w, rr, ldr = _norm_inputs(x, weight, residual)
+    out = _new(x.shape, x.dtype)
+    total = x if rr is None else _new(x.shape, x.dtype)
+    rstd = _new(x.shape[:-1], torch.float32)
     _check("kr_add_rms_norm",
-           _lib.kr_add_rms_norm(t, n, width, _ptr(xr), ldx, _ptr(rr), ldr, _ptr(w), eps,
-                                None if residual is None else _ptr(total), width, _ptr(out),
-                                width, _ptr(rstd), _stream()))
+           _lib.kr_add_rms_norm(t, n, width, xr.data_ptr(), ldx,
+                                None if rr is None else rr.data_ptr(), ldr, w.data_ptr(), eps,
+                                None if rr is None else total.data_ptr(), width, out.data_ptr(),
+                                width, rstd.data_ptr(), _raw_stream(dev)))
     return Normed(out, total, rstd)
 
 
 def add_rms_norm_bytes(x, weight, residual=None, eps: float = 1e-6) -> NormedBytes:
     """add_rms_norm with the norm held in 8-bit integers and a scale for each row: q * scale
     (kr_add_rms_norm_bytes)."""
-    t, xr, n, ldx, width, w, rr, ldr = _norm_inputs(x, weight, residual)
-    q = torch.empty(x.shape, dtype=torch.int8, device="cuda")
-    total = x if residual is None else torch.empty(x.shape, dtype=x.dtype, device="cuda")
-    scale, rstd = torch.empty((2,) + x.shape[:-1], dtype=torch.float32, device="cuda").unbind(0)
+    t, dev, xr, n, ldx, width, w, rr, ldr = _norm_inputs(x, weight, residual)
+    q = _new(x.shape, torch.int8)
+    total = x if rr is None else _new(x.shape, x.dtype)
+    scale, rstd = _new(x.shape[:-1], torch.float32), _new(x.shape[:-1], torch.float32)
     _check("kr_add_rms_norm_bytes",
-           _lib.kr_add_rms_norm_bytes(t, n, width, _ptr(xr), ldx, _ptr(rr), ldr, _ptr(w), eps,
-                                      None if residual is None else _ptr(total), width, _ptr(q),
-                                      width, _ptr(scale), _ptr(rstd), _stream()))
+           _lib.kr_add_rms_norm_bytes(t, n, width, xr.data_ptr(), ldx,
+                                      None if rr is None else rr.data_ptr(), ldr, w.data_ptr(),
+                                      eps, None if rr is None else total.data_ptr(), width,
+                                      q.data_ptr(), width, scale.data_ptr(), rstd.data_ptr(),
+                                      _raw_stream(dev)))
     return NormedBytes(q, scale, total, rstd)
 
 
@@ -828,28 +854,27 @@ def add_rms_norm_backward(dout, sum, weight, rstd, dsum=None):
     the sum by the residual's path.  dx, like dout, is the gradient of x and of residual;
     dweight is float32 (kr_add_rms_norm_backward)."""
     t = _type(dout, "dout")
-    if sum.dtype != dout.dtype or sum.shape != dout.shape:
-        raise ValueError("sum must be like dout: %s %s" % (dout.dtype, tuple(dout.shape)))
-    if dsum is not None and (dsum.dtype != dout.dtype or dsum.shape != dout.shape):
-        raise ValueError("dsum must be like dout: %s %s" % (dout.dtype, tuple(dout.shape)))
-    gr, n, ldo = _rows(dout, "dout")
+    _like(sum, dout, "sum", "dout")
+    dev = _here(dout, "dout")
+    gr, n, ldo = _rows(dout, "dout", dev)
     width = gr.shape[1]
-    if width < 1:
-        raise ValueError("dout must have rows of one element at least")
-    sr, _, lds = _rows(sum, "sum", width)
-    w = _vector(weight, width, dout.dtype, "weight")
-    f = _vector(rstd, n, torch.float32, "rstd")
+    sr, _, lds = _rows(sum, "sum", dev, width)
+    w = _vector(weight, width, dout.dtype, "weight", dev)
+    f = _vector(rstd, n, torch.float32, "rstd", dev)
     dr, ldd = None, 0
     if dsum is not None:
-        dr, _, ldd = _rows(dsum, "dsum", width)
-    dx = torch.empty(dout.shape, dtype=dout.dtype, device="cuda")
-    dw = torch.empty(width, dtype=torch.float32, device="cuda")
+        _like(dsum, dout, "dsum", "dout")
+        dr, _, ldd = _rows(dsum, "dsum", dev, width)
+    dx = _new(dout.shape, dout.dtype)
+    dw = _new(width, torch.float32)
     wsb = _lib.kr_add_rms_norm_backward_workspace(t, n, width)
-    ws = _scratch(wsb)
+    ws, at = _scratch(wsb)
     _check("kr_add_rms_norm_backward",
-           _lib.kr_add_rms_norm_backward(t, n, width, _ptr(gr), ldo, _ptr(sr), lds, _ptr(w),
-                                         _ptr(f), _ptr(dr), ldd, _ptr(dx), width, _ptr(dw),
-                                         _ptr(ws), wsb, _stream()))
+           _lib.kr_add_rms_norm_backward(t, n, width, gr.data_ptr(), ldo, sr.data_ptr(), lds,
+                                         w.data_ptr(), f.data_ptr(),
+                                         None if dr is None else dr.data_ptr(), ldd,
+                                         dx.data_ptr(), width, dw.data_ptr(), at, wsb,
+                                         _raw_stream(dev)))
     return dx, dw
 
 
@@ -860,20 +885,21 @@ def byte_matmul(a, sa, b, sb, dtype=torch.bfloat16) -> torch.Tensor:
         raise TypeError("dtype must be %s, got %s" % (" or ".join(map(str, _TYPES)), dtype))
     _type(a, "a", (torch.int8,))
     _type(b, "b", (torch.int8,))
-    ar, m, lda = _rows(a, "a")
+    dev = _here(a, "a")
+    ar, m, lda = _rows(a, "a", dev)
     k = ar.shape[1]
-    if b.dim() != 2 or k < 1 or b.shape[0] < 1:
-        raise ValueError("a and b must have rows of one element at least, b two dimensions")
-    br, n, ldb = _rows(b, "b", k)
-    fa = _vector(sa, m, torch.float32, "sa")
-    fb = _vector(sb, n, torch.float32, "sb")
-    out = torch.empty(a.shape[:-1] + (n,), dtype=dtype, device="cuda")
-    p = KrBytes(m, n, k, ar.data_ptr(), br.data_ptr(), lda, ldb, fa.data_ptr(), fb.data_ptr())
-    wsb = _lib.kr_byte_matmul_workspace(ctypes.byref(p))
-    ws = _scratch(wsb)
+    if b.dim() != 2 or b.shape[0] < 1:
+        raise ValueError("b must be [n][%d], got %s" % (k, tuple(b.shape)))
+    br, n, ldb = _rows(b, "b", dev, k)
+    fa = _vector(sa, m, torch.float32, "sa", dev)
+    fb = _vector(sb, n, torch.float32, "sb", dev)
+    out = _new(a.shape[:-1] + (n,), dtype)
+    p = ctypes.byref(KrBytes(m, n, k, ar.data_ptr(), br.data_ptr(), lda, ldb, fa.data_ptr(),
+                             fb.data_ptr()))
+    wsb = _lib.kr_byte_matmul_workspace(p)
+    ws, at = _scratch(wsb)
     _check("kr_byte_matmul",
-           _lib.kr_byte_matmul(ctypes.byref(p), _TYPES[dtype], _ptr(out), n, _ptr(ws), wsb,
-                               _stream()))
+           _lib.kr_byte_matmul(p, _TYPES[dtype], out.data_ptr(), n, at, wsb, _raw_stream(dev)))
     return out
 
 
@@ -884,50 +910,51 @@ def _gated(x, wg, wu, act):
     t = _type(x, "x", (torch.float16, torch.bfloat16))
     if act not in _ACTS:
         raise ValueError("act must be one of %s, got %r" % (", ".join(_ACTS), act))
-    xr, n, ldx = _rows(x, "x")
+    dev = _here(x, "x")
+    xr, n, ldx = _rows(x, "x", dev)
     width = xr.shape[1]
     for w, name in ((wg, "wg"), (wu, "wu")):
         if not isinstance(w, torch.Tensor) or w.dtype != x.dtype:
             raise TypeError("%s must be a tensor of %s" % (name, x.dtype))
-        if w.dim() != 2 or w.shape != wg.shape or w.shape[0] < 1 or width < 1:
+        if w.dim() != 2 or w.shape != wg.shape or w.shape[0] < 1:
             raise ValueError("wg and wu must be [hidden][%d], got %s" % (width, tuple(w.shape)))
-    gr, hidden, ldg = _rows(wg, "wg", width)
-    ur, _, ldu = _rows(wu, "wu", width)
+    gr, hidden, ldg = _rows(wg, "wg", dev, width)
+    ur, _, ldu = _rows(wu, "wu", dev, width)
     g = KrGated(t, _ACTS[act], n, width, hidden, xr.data_ptr(), gr.data_ptr(), ur.data_ptr(), ldx,
                 ldg, ldu)
-    return g, (xr, gr, ur)
+    return g, dev, (xr, gr, ur)
 
 
 def gated_projection(x, wg, wu, act: str = "silu") -> torch.Tensor:
     """act(x wg^T) * (x wu^T) of x [..., width] and wg, wu [hidden][width], act "silu" or
     "gelu" (kr_gated_projection)."""
-    g, keep = _gated(x, wg, wu, act)
-    out = torch.empty(x.shape[:-1] + (g.hidden,), dtype=x.dtype, device="cuda")
-    wsb = _lib.kr_gated_projection_workspace(ctypes.byref(g))
-    ws = _scratch(wsb)
+    g, dev, keep = _gated(x, wg, wu, act)
+    out = _new(x.shape[:-1] + (g.hidden,), x.dtype)
+    p = ctypes.byref(g)
+    wsb = _lib.kr_gated_projection_workspace(p)
+    ws, at = _scratch(wsb)
     _check("kr_gated_projection",
-           _lib.kr_gated_projection(ctypes.byref(g), _ptr(out), g.hidden, _ptr(ws), wsb,
-                                    _stream()))
+           _lib.kr_gated_projection(p, out.data_ptr(), g.hidden, at, wsb, _raw_stream(dev)))
     return out
 
 
 def gated_projection_backward(dh, x, wg, wu, act: str = "silu"):
     """(dx, dwg, dwu) of gated_projection from its inputs and the gradient dh of its output
     (kr_gated_projection_backward)."""
-    g, keep = _gated(x, wg, wu, act)
+    g, dev, keep = _gated(x, wg, wu, act)
     if not isinstance(dh, torch.Tensor) or dh.dtype != x.dtype:
         raise TypeError("dh must be a tensor of %s" % x.dtype)
     if dh.shape != x.shape[:-1] + (g.hidden,):
         raise ValueError("dh must be %s, got %s" % (tuple(x.shape[:-1]) + (g.hidden,),
                                                     tuple(dh.shape)))
-    hr, _, ldh = _rows(dh, "dh", g.hidden)
-    dx = torch.empty(x.shape, dtype=x.dtype, device="cuda")
-    dwg = torch.empty(wg.shape, dtype=x.dtype, device="cuda")
-    dwu = torch.empty(wg.shape, dtype=x.dtype, device="cuda")
-    wsb = _lib.kr_gated_projection_backward_workspace(ctypes.byref(g))
-    ws = _scratch(wsb)
+    hr, _, ldh = _rows(dh, "dh", dev, g.hidden)
+    dx = _new(x.shape, x.dtype)
+    dwg, dwu = _new(wg.shape, x.dtype), _new(wg.shape, x.dtype)
+    p = ctypes.byref(g)
+    wsb = _lib.kr_gated_projection_backward_workspace(p)
+    ws, at = _scratch(wsb)
     _check("kr_gated_projection_backward",
-           _lib.kr_gated_projection_backward(ctypes.byref(g), _ptr(hr), ldh, _ptr(dx), g.width,
-                                             _ptr(dwg), g.width, _ptr(dwu), g.width, _ptr(ws), wsb,
-                                             _stream()))
+           _lib.kr_gated_projection_backward(p, hr.data_ptr(), ldh, dx.data_ptr(), g.width,
+                                             dwg.data_ptr(), g.width, dwu.data_ptr(), g.width, at,
+                                             wsb, _raw_stream(dev)))
     return dx, dwg, dwu

@@ -183,8 +183,28 @@ struct GatedLaid {
     }
 };
 
+// A matrix as it is.
+Operand as_is(const void *p, int64_t ld, int64_t rows, int64_t bytes)
+{
+    return {(const char *)p, ld, rows, bytes};
+}
+
 kr_status gated_run(const kr_gated *g, void *out, int64_t ldo, Carve &c, hipStream_t st)
 {
+    if (g->rows <= kFewRows) {
+        if (!out) return KR_OK;
+        GatedArgs a{};
+        a.type = g->type;
+        a.act = g->act;
+        a.m = g->rows;
+        a.n = g->hidden;
+        a.x = as_is(g->x, g->ldx * 2, g->rows, g->width * 2);
+        a.wg = as_is(g->wg, g->ldg * 2, g->hidden, g->width * 2);
+        a.wu = as_is(g->wu, g->ldu * 2, g->hidden, g->width * 2);
+        a.out = out;
+        a.ldo = ldo;
+        return said(launch_gated_few(a, st));
+    }
     const GatedLaid l(g, c, false);
     GatedArgs a = l.args(g);
     a.out = out;
@@ -218,6 +238,12 @@ bool bytes_fits(const kr_bytes *p) { return p->m <= kRowsMost && p->n <= kWidthM
 
 kr_status bytes_run(const kr_bytes *p, int32_t type, void *out, int64_t ldo, Carve &c, hipStream_t st)
 {
+    if (p->m <= kFewRows) {
+        if (!out) return KR_OK;
+        const BytesArgs x{type, p->m, p->n, p->k, as_is(p->a, p->lda, p->m, p->k),
+                          as_is(p->b, p->ldb, p->n, p->k), p->sa, p->sb, out, ldo, nullptr};
+        return said(launch_bytes_few(x, st));
+    }
     const Laid a(p->a, p->lda, p->m, p->k, c), b(p->b, p->ldb, p->n, p->k, c);
     BytesArgs x{};
     x.out_type = type;

@@ -62,7 +62,21 @@ hipError_t typed(const BytesArgs &a, hipStream_t st)
     return launch_mma<int8_t, false, false>(x, mma_plan(a.m, a.n, 1, x.steps), out, st);
 }
 
+template <typename T>
+hipError_t few(const BytesArgs &a, hipStream_t st)
+{
+    const FewArgs x{a.a.p, {a.b.p, nullptr}, a.a.ld, {a.b.ld, 0}, (int)a.m, (int)a.n, (int)a.a.bytes};
+    return launch_few<int8_t>(x, PutScaled<T>{(T *)a.out, a.ldo, (int)a.n, a.sa, a.sb}, st);
+}
+
 }  // namespace
+
+hipError_t launch_bytes_few(const BytesArgs &a, hipStream_t st)
+{
+    if (a.out_type == KR_F32) return few<float>(a, st);
+    if (a.out_type == KR_F16) return few<f16>(a, st);
+    return few<bf16>(a, st);
+}
 
 size_t bytes_part(int64_t m, int64_t n, int64_t k_bytes)
 {

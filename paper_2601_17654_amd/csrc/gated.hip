@@ -134,6 +134,14 @@ hipError_t forward(const GatedArgs &a, hipStream_t st)
     return launch_mma<T, false, false>(x, mma_plan(a.m, a.n, 2, x.steps), out, st);
 }
 
+template <typename T>
+hipError_t few(const GatedArgs &a, hipStream_t st)
+{
+    const FewArgs x{a.x.p, {a.wg.p, a.wu.p}, a.x.ld, {a.wg.ld, a.wu.ld}, (int)a.m, (int)a.n,
+                    (int)a.x.bytes};
+    return launch_few<T>(x, PutGated<T>{{}, (T *)a.out, a.ldo, (int)a.n, a.act}, st);
+}
+
 // The three products of the backward pass, in turn: their plans share the workspace.
 MmaPlan plan_dx(int64_t m, int64_t n_pad, int64_t width)
 {
@@ -215,6 +223,11 @@ size_t gated_part(int64_t m, int64_t n, int64_t k_bytes)
 hipError_t launch_gated(const GatedArgs &a, hipStream_t st)
 {
     return a.type == KR_F16 ? forward<f16>(a, st) : forward<bf16>(a, st);
+}
+
+hipError_t launch_gated_few(const GatedArgs &a, hipStream_t st)
+{
+    return a.type == KR_F16 ? few<f16>(a, st) : few<bf16>(a, st);
 }
 
 size_t gated_back_part(int64_t m, int64_t n, int64_t n_pad, int64_t width, int64_t k_bytes)

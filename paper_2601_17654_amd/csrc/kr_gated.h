@@ -1,7 +1,7 @@
 // Launch arguments of the projections.
 #pragma once
 
-#include "kr_mma.h"
+#include "kr_few.h"
 
 namespace kr {
 
@@ -21,6 +21,8 @@ struct GatedArgs {
     void *part;               // gated_part bytes
 };
 size_t gated_part(int64_t m, int64_t n, int64_t k_bytes);
+// x, wg, wu as they are: any alignment, a.x.bytes of k; no workspace.
+hipError_t launch_gated_few(const GatedArgs &a, hipStream_t st);
 hipError_t launch_gated(const GatedArgs &a, hipStream_t st);
 
 struct GatedBackArgs {
@@ -47,6 +49,7 @@ struct BytesArgs {
     void *part;
 };
 size_t bytes_part(int64_t m, int64_t n, int64_t k_bytes);
+hipError_t launch_bytes_few(const BytesArgs &a, hipStream_t st);
 hipError_t launch_bytes(const BytesArgs &a, hipStream_t st);
 
 }  // namespace kr
