@@ -132,9 +132,10 @@ struct Laid {
             op = Operand{(const char *)p, from_ld, rows, bytes};
         }
     }
-    hipError_t fill(hipStream_t st) const
+    void add_to(PadArgs &a) const
     {
-        return copy ? launch_pad(from, from_ld, op.rows, bytes, (void *)op.p, op.ld, st) : hipSuccess;
+        if (copy)
+            a.m[a.count++] = {(const char *)from, from_ld, op.rows, bytes, (char *)op.p, op.ld};
     }
 };
 
@@ -177,9 +178,11 @@ struct GatedLaid {
     }
     hipError_t fill(hipStream_t st) const
     {
-        hipError_t e = x.fill(st);
-        if (e == hipSuccess) e = wg.fill(st);
-        return e == hipSuccess ? wu.fill(st) : e;
+        PadArgs a{};
+        x.add_to(a);
+        wg.add_to(a);
+        wu.add_to(a);
+        return launch_pad(a, st);
     }
 };
 
@@ -258,8 +261,10 @@ kr_status bytes_run(const kr_bytes *p, int32_t type, void *out, int64_t ldo, Car
     x.ldo = ldo;
     x.part = c.take((int64_t)bytes_part(x.m, x.n, x.k_bytes));
     if (!out) return KR_OK;
-    hipError_t e = a.fill(st);
-    if (e == hipSuccess) e = b.fill(st);
+    PadArgs pads{};
+    a.add_to(pads);
+    b.add_to(pads);
+    const hipError_t e = launch_pad(pads, st);
     return said(e == hipSuccess ? launch_bytes(x, st) : e);
 }
 

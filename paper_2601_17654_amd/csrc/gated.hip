@@ -248,33 +248,35 @@ hipError_t launch_gated_back(const GatedBackArgs &a, hipStream_t st)
     return a.f.type == KR_F16 ? backward<f16>(a, st) : backward<bf16>(a, st);
 }
 
-// One 16-byte piece of a padded row a thread.
-__global__ __launch_bounds__(256) void pad_kernel(const char *from, int64_t from_ld, int64_t rows,
-                                                  int64_t bytes, char *to, int64_t to_ld)
+// One 16-byte piece of a padded row a thread; blockIdx.y is the matrix.
+__global__ __launch_bounds__(256) void pad_kernel(PadArgs a)
 {
-    const int64_t per = to_ld / 16, all = rows * per;
+    const PadArgs::One m = a.m[blockIdx.y];
+    const int64_t per = m.to_ld / 16, all = m.rows * per;
     for (int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x; id < all;
          id += (int64_t)gridDim.x * 256) {
         const int64_t r = id / per, c = (id - r * per) * 16;
-        const char *p = from + r * from_ld + c;
+        const char *p = m.from + r * m.from_ld + c;
         Pack<char, 16> x;
-        if (c + 16 <= bytes) {
+        if (c + 16 <= m.bytes) {
             x = load16(p);
         } else {
 #pragma unroll
-            for (int e = 0; e < 16; ++e) x.v[e] = c + e < bytes ? p[e] : (char)0;
+            for (int e = 0; e < 16; ++e) x.v[e] = c + e < m.bytes ? p[e] : (char)0;
         }
-        store16(to + r * to_ld + c, x);
+        store16(m.to + r * m.to_ld + c, x);
     }
 }
 
-hipError_t launch_pad(const void *from, int64_t from_ld, int64_t rows, int64_t bytes, void *to,
-                      int64_t to_ld, hipStream_t st)
+hipError_t launch_pad(const PadArgs &a, hipStream_t st)
 {
-    const int64_t blocks = (rows * (to_ld / 16) + 255) / 256;
-    if (blocks > 0)
-        pad_kernel<<<(unsigned)(blocks < 16384 ? blocks : 16384), 256, 0, st>>>(
-            (const char *)from, from_ld, rows, bytes, (char *)to, to_ld);
+    int64_t most = 0;
+    for (int i = 0; i < a.count; ++i) {
+        const int64_t blocks = (a.m[i].rows * (a.m[i].to_ld / 16) + 255) / 256;
+        most = most > blocks ? most : blocks;
+    }
+    if (most == 0) return hipSuccess;
+    pad_kernel<<<dim3((unsigned)(most < 16384 ? most : 16384), a.count), 256, 0, st>>>(a);
     return hipGetLastError();
 }
 

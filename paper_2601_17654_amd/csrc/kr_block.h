@@ -48,7 +48,7 @@ __device__ inline Pack<T, kVec<T>> load_row(const T *row, int c, int width)
     if (c + V <= width) return load16(row + c);
     Pack<T, V> x;
 #pragma unroll
-    for (int e = 0; e < V; ++e) x.v[e] = c + e < width ? row[c + e] : (T)0.0f;
+    for (int e = 0; e < V; ++e) x.v[e] = c + e < width ? row[c + e] : (T)0;
     return x;
 }
 
@@ -75,28 +75,15 @@ __device__ inline void store_row(T *row, int c, int width, const float *f)
     }
 }
 
-__device__ inline float wave_sum(float x)
-{
-#pragma unroll
-    for (int o = 32; o; o >>= 1) x += __shfl_xor(x, o);
-    return x;
-}
-
-__device__ inline uint32_t wave_max(uint32_t x)
-{
-#pragma unroll
-    for (int o = 32; o; o >>= 1) x = max(x, (uint32_t)__shfl_xor((int)x, o));
-    return x;
-}
-
-// Sum (largest) over the TPR threads that share a row, in an order of its own: lanes by
-// halves, then waves in turn.  `part`: TPR / 64 words of LDS, not in use when this is called
-// and free again after the next barrier.
+// Sum (largest) over the TPR threads that share a row, in an order of its own: lanes by halves,
+// then waves in turn.  `part`: TPR / 64 words of LDS where that is above one, not in use when this
+// is called and free again after the next barrier.
 template <int TPR>
 __device__ inline float row_sum(float x, float *part)
 {
-    x = wave_sum(x);
-    if (TPR == 64) return x;
+#pragma unroll
+    for (int o = TPR < 64 ? TPR / 2 : 32; o; o >>= 1) x += __shfl_xor(x, o);
+    if (TPR <= 64) return x;
     if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = x;
     __syncthreads();
     float s = 0.0f;
@@ -108,8 +95,9 @@ __device__ inline float row_sum(float x, float *part)
 template <int TPR>
 __device__ inline uint32_t row_max(uint32_t x, uint32_t *part)
 {
-    x = wave_max(x);
-    if (TPR == 64) return x;
+#pragma unroll
+    for (int o = TPR < 64 ? TPR / 2 : 32; o; o >>= 1) x = max(x, (uint32_t)__shfl_xor((int)x, o));
+    if (TPR <= 64) return x;
     if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = x;
     __syncthreads();
     uint32_t s = 0;

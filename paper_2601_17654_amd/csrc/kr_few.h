@@ -128,6 +128,7 @@ __global__ __launch_bounds__(NW * 64) void few_kernel(FewArgs a, Out out)
     const int token = (int)threadIdx.x / 2, h = (int)threadIdx.x % 2 * 8;
     if (token >= a.m || n0 + h >= a.n) return;  // NW * 32 threads or more: a token each two
     Sum v[PLANES][8] = {};
+#pragma unroll 4
     for (int k = 0; k < NW; ++k)
 #pragma unroll
         for (int p = 0; p < PLANES; ++p)

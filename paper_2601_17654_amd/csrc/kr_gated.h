@@ -5,10 +5,18 @@
 
 namespace kr {
 
-// Rows of `bytes` bytes copied to rows of `to_ld` bytes (a multiple of 16), the rest of each
-// filled with zeros.
-hipError_t launch_pad(const void *from, int64_t from_ld, int64_t rows, int64_t bytes, void *to,
-                      int64_t to_ld, hipStream_t st);
+// Matrices to copy: rows of `bytes` bytes to rows of `to_ld` bytes (a multiple of 16), the rest
+// of each filled with zeros.  All in one launch.
+struct PadArgs {
+    struct One {
+        const char *from;
+        int64_t from_ld, rows, bytes;
+        char *to;
+        int64_t to_ld;
+    } m[3];
+    int count;
+};
+hipError_t launch_pad(const PadArgs &a, hipStream_t st);
 
 // gated.hip.  x [m][k], wg and wu [n][k] as operands that the tiles take, k_bytes of k a row.
 struct GatedArgs {

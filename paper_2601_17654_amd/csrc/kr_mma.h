@@ -292,7 +292,7 @@ __device__ inline void put_tile(E, const MmaArgs &a, const Out &out,
     constexpr int TOGETHER = 4;                            // rows a lane has in hand
     typedef typename Mma<E>::Quad Quad;
     typedef typename Mma<E>::Sum Sum;
-    static_assert(64 * STRIP * 4 <= 2 * (BM + BN) * kStep / (WM * WN), "a wave's share of LDS");
+    static_assert(64 * STRIP * 4 * WM * WN <= 2 * (BM + BN) * kStep, "a wave's share of LDS");
     char *own = lds + wave * 64 * STRIP * 4;
     const int wm = wave / WN, wn = wave % WN;
     const int n = (int)n0 + wn * COLS + lane % LANES * 8, columns = out.columns(a.n);
@@ -499,14 +499,26 @@ __global__ __launch_bounds__(256) void mma_join_kernel(MmaArgs a, Out out)
     const int64_t m = id / per;
     const int n = (int)(id - m * per) * 8;
     Sum v[2][8] = {};
-    for (int s = 0; s < a.splits; ++s)
+    // four splits' loads at a time
+    for (int s = 0; s < a.splits; s += 4) {
+        Pack<Sum, 4> q[4][Out::PLANES][2];
 #pragma unroll
-        for (int p = 0; p < Out::PLANES; ++p) {
-            const Sum *q = (const Sum *)a.part + (((int64_t)s * Out::PLANES + p) * a.m + m) * a.n;
+        for (int u = 0; u < 4; ++u)
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if (n + e < a.n) v[p][e] += q[n + e];
-        }
+            for (int p = 0; p < Out::PLANES; ++p)
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+                    q[u][p][h] = load_row(
+                        (const Sum *)a.part +
+                            (((int64_t)min(s + u, a.splits - 1) * Out::PLANES + p) * a.m + m) * a.n,
+                        n + h * 4, s + u < a.splits ? a.n : 0);
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+#pragma unroll
+            for (int p = 0; p < Out::PLANES; ++p)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[p][e] += q[u][p][e / 4].v[e % 4];
+    }
     out.put(m, n, v[0], v[Out::PLANES - 1], out.mine(n), out.fetch(true, m, n));
 }
 

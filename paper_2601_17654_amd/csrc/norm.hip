@@ -4,7 +4,7 @@
 //   s = x + r,  f = 1 / sqrt(mean(s^2) + eps),  n = s f w
 //
 // Every element is read once and written once: a row stays in the registers of the threads
-// that share it (64, 256 or 1,024 of them, 8 or 16 elements each), so its mean costs no second
+// that share it (16 to 1,024 of them, 8 or 16 elements each), so its mean costs no second
 // pass over memory.  Rows of more than 16,384 elements are read again from memory instead.
 // All arithmetic is in 32 bits; stored values are rounded once.
 #include "kr_block.h"
@@ -63,11 +63,11 @@ template <typename T, int TPR, int FPT, bool HELD>
 __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_kernel(NormArgs a)
 {
     constexpr int V = kVec<T>, NV = FPT / V, RPB = TPR < 256 ? 256 / TPR : 1;
-    __shared__ float part[TPR / 64];
-    __shared__ uint32_t part_top[TPR / 64];
+    __shared__ float part[TPR > 64 ? TPR / 64 : 1];
+    __shared__ uint32_t part_top[TPR > 64 ? TPR / 64 : 1];
     const int t = threadIdx.x % TPR;
     const int64_t row = (int64_t)blockIdx.x * RPB + threadIdx.x / TPR;
-    if (RPB > 1 && row >= a.rows) return;  // whole waves, and such rows take no barrier
+    if (RPB > 1 && row >= a.rows) return;  // whole rows' threads, and such rows take no barrier
     const T *x = (const T *)a.x + row * a.ldx;
     const T *r = a.res ? (const T *)a.res + row * a.ldr : nullptr;
     float s[NV][V];
@@ -187,7 +187,8 @@ template <typename T, int TPR, int FPT>
 __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_back_kernel(NormBackArgs a)
 {
     constexpr int V = kVec<T>, NV = FPT / V, RPB = TPR < 256 ? 256 / TPR : 1;
-    __shared__ float part[2][TPR / 64];
+    constexpr bool AHEAD = FPT == 8;  // the next row's loads: with 16 they cost half the waves
+    __shared__ float part[2][TPR > 64 ? TPR / 64 : 1];
     __shared__ float share[RPB > 1 ? RPB * TPR * FPT : 1];
     const int t = threadIdx.x % TPR, sub = threadIdx.x / TPR;
     float w[NV][V], dw[NV][V];
@@ -197,33 +198,40 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_back_kernel(NormBa
 #pragma unroll
         for (int e = 0; e < V; ++e) dw[j][e] = 0.0f;
     }
-    int turn = 0;
-    for (int64_t row = (int64_t)blockIdx.x * RPB + sub; row < a.rows;
-         row += (int64_t)gridDim.x * RPB, turn ^= 1) {
-        const float f = a.rstd[row];
-        float h[NV][V], g[NV][V];
-        float c = 0.0f;
-        Pack<T, V> hs[NV], gs[NV], ds[NV];
+    Pack<T, V> hs[NV], gs[NV], ds[NV];
+    float f = 0.0f;
+    auto load = [&](int64_t row) {  // of the next row, while one is worked on
+        f = a.rstd[row];
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             hs[j] = load_row((const T *)a.s + row * a.lds, (j * TPR + t) * V, a.width);
             gs[j] = load_row((const T *)a.dout + row * a.ldo, (j * TPR + t) * V, a.width);
-        }
-        if (a.dsum) {
-#pragma unroll
-            for (int j = 0; j < NV; ++j)
+            if (a.dsum)
                 ds[j] = load_row((const T *)a.dsum + row * a.ldd, (j * TPR + t) * V, a.width);
         }
+    };
+    int turn = 0;
+    const int64_t stride = (int64_t)gridDim.x * RPB;
+    int64_t row = (int64_t)blockIdx.x * RPB + sub;
+    if (AHEAD && row < a.rows) load(row);
+    for (; row < a.rows; row += stride, turn ^= 1) {
+        if (!AHEAD) load(row);
+        float h[NV][V], g[NV][V], d[NV][V];
+        const float f0 = f;
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             floats(hs[j], h[j]);
             floats(gs[j], g[j]);
+#pragma unroll
+            for (int e = 0; e < V; ++e) d[j][e] = a.dsum ? (float)ds[j].v[e] : 0.0f;
         }
+        if (AHEAD && row + stride < a.rows) load(row + stride);
+        float c = 0.0f;
 #pragma unroll
         for (int j = 0; j < NV; ++j)
 #pragma unroll
             for (int e = 0; e < V; ++e) {
-                h[j][e] *= f;
+                h[j][e] *= f0;
                 dw[j][e] = fmaf(g[j][e], h[j][e], dw[j][e]);
                 g[j][e] *= w[j][e];
                 c = fmaf(g[j][e], h[j][e], c);
@@ -233,12 +241,8 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_back_kernel(NormBa
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
 #pragma unroll
-            for (int e = 0; e < V; ++e) g[j][e] = (g[j][e] - h[j][e] * c) * f;
-            if (a.dsum) {
-#pragma unroll
-                for (int e = 0; e < V; ++e) g[j][e] += (float)ds[j].v[e];
-            }
-            store_row((T *)a.dx + row * a.ldx, (j * TPR + t) * V, a.width, g[j]);
+            for (int e = 0; e < V; ++e) d[j][e] += (g[j][e] - h[j][e] * c) * f0;
+            store_row((T *)a.dx + row * a.ldx, (j * TPR + t) * V, a.width, d[j]);
         }
     }
     float *slot = a.part + (int64_t)blockIdx.x * a.width;
@@ -319,22 +323,24 @@ __global__ __launch_bounds__(256) void norm_back_long_weight_kernel(NormBackArgs
     a.part[(int64_t)blockIdx.y * a.width + c] = dw;
 }
 
-// dw = sum of the slots: 64 columns a block, 16 waves that take every 16th slot.
+// dw = sum of the slots: 32 columns a block, 32 half waves that take every 32nd slot.
 __global__ __launch_bounds__(1024) void norm_weight_kernel(const float *part, int slots, int width,
                                                            float *dw)
 {
-    __shared__ float sums[16][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t c = (int64_t)blockIdx.x * 64 + lane;
+    __shared__ float sums[32][33];
+    const int lane = threadIdx.x & 31, group = threadIdx.x >> 5;
+    const int64_t c = (int64_t)blockIdx.x * 32 + lane;
     float s = 0.0f;
-    if (c < width)
-        for (int k = wave; k < slots; k += 16) s += part[(int64_t)k * width + c];
-    sums[wave][lane] = s;
+    if (c < width) {
+#pragma unroll 8
+        for (int k = group; k < slots; k += 32) s += part[(int64_t)k * width + c];
+    }
+    sums[group][lane] = s;
     __syncthreads();
-    if (wave == 0 && c < width) {
+    if (group == 0 && c < width) {
         s = 0.0f;
 #pragma unroll
-        for (int k = 0; k < 16; ++k) s += sums[k][lane];
+        for (int k = 0; k < 32; ++k) s += sums[k][lane];
         dw[c] = s;
     }
 }
@@ -345,22 +351,33 @@ struct Shape {
 };
 Shape shape_of(int width)
 {
-    for (int tpr : {64, 256, 1024})
-        for (int fpt : {8, 16})
-            if (width <= tpr * fpt) return {tpr, fpt};
+    for (const Shape s : {Shape{16, 8}, {32, 8}, {64, 8}, {64, 16}, {256, 8}, {256, 16}, {1024, 8},
+                          {1024, 16}})
+        if (width <= s.tpr * s.fpt) return s;
     return {0, 0};
 }
+int rows_per_block(Shape s) { return s.tpr > 0 && s.tpr < 256 ? 256 / s.tpr : 1; }
 
 // Rows of one launch: a grid has fewer than 2^32 threads.
 constexpr int64_t kRowsPerLaunch = 1 << 21;
+
+// The backward pass holds more of a row, and the next one: eight elements a thread, as long as
+// there are threads.
+Shape back_shape_of(int width)
+{
+    const Shape s = shape_of(width);
+    return s.tpr == 256 && s.fpt == 16 ? Shape{512, 8} : s;
+}
 
 template <typename T, bool HELD>
 hipError_t norm_rows(const NormArgs &a, hipStream_t st)
 {
     const Shape s = shape_of(a.width);
-    const int rpb = s.tpr == 64 ? 4 : 1;
+    const int rpb = rows_per_block(s);
     const dim3 grid((unsigned)((a.rows + rpb - 1) / rpb));
-    if (s.tpr == 64 && s.fpt == 8) norm_kernel<T, 64, 8, HELD><<<grid, 256, 0, st>>>(a);
+    if (s.tpr == 16) norm_kernel<T, 16, 8, HELD><<<grid, 256, 0, st>>>(a);
+    else if (s.tpr == 32) norm_kernel<T, 32, 8, HELD><<<grid, 256, 0, st>>>(a);
+    else if (s.tpr == 64 && s.fpt == 8) norm_kernel<T, 64, 8, HELD><<<grid, 256, 0, st>>>(a);
     else if (s.tpr == 64) norm_kernel<T, 64, 16, HELD><<<grid, 256, 0, st>>>(a);
     else if (s.tpr == 256 && s.fpt == 8) norm_kernel<T, 256, 8, HELD><<<grid, 256, 0, st>>>(a);
     else if (s.tpr == 256) norm_kernel<T, 256, 16, HELD><<<grid, 256, 0, st>>>(a);
@@ -406,12 +423,14 @@ hipError_t back_long_rows(NormBackArgs a, hipStream_t st)
 template <typename T>
 hipError_t back_typed(const NormBackArgs &a, int slots, hipStream_t st)
 {
-    const Shape s = shape_of(a.width);
+    const Shape s = back_shape_of(a.width);
     if (a.rows > 0) {
-        if (s.tpr == 64 && s.fpt == 8) norm_back_kernel<T, 64, 8><<<slots, 256, 0, st>>>(a);
+        if (s.tpr == 16) norm_back_kernel<T, 16, 8><<<slots, 256, 0, st>>>(a);
+        else if (s.tpr == 32) norm_back_kernel<T, 32, 8><<<slots, 256, 0, st>>>(a);
+        else if (s.tpr == 64 && s.fpt == 8) norm_back_kernel<T, 64, 8><<<slots, 256, 0, st>>>(a);
         else if (s.tpr == 64) norm_back_kernel<T, 64, 16><<<slots, 256, 0, st>>>(a);
-        else if (s.tpr == 256 && s.fpt == 8) norm_back_kernel<T, 256, 8><<<slots, 256, 0, st>>>(a);
-        else if (s.tpr == 256) norm_back_kernel<T, 256, 16><<<slots, 256, 0, st>>>(a);
+        else if (s.tpr == 256) norm_back_kernel<T, 256, 8><<<slots, 256, 0, st>>>(a);
+        else if (s.tpr == 512) norm_back_kernel<T, 512, 8><<<slots, 512, 0, st>>>(a);
         else if (s.tpr == 1024 && s.fpt == 8)
             norm_back_kernel<T, 1024, 8><<<slots, 1024, 0, st>>>(a);
         else if (s.tpr == 1024) norm_back_kernel<T, 1024, 16><<<slots, 1024, 0, st>>>(a);
@@ -422,7 +441,7 @@ hipError_t back_typed(const NormBackArgs &a, int slots, hipStream_t st)
             norm_back_long_weight_kernel<T><<<grid, 256, 0, st>>>(a);
         }
     }
-    norm_weight_kernel<<<(a.width + 63) / 64, 1024, 0, st>>>(a.part, slots, a.width, a.dw);
+    norm_weight_kernel<<<(a.width + 31) / 32, 1024, 0, st>>>(a.part, slots, a.width, a.dw);
     return hipGetLastError();
 }
 
@@ -438,12 +457,13 @@ hipError_t launch_norm(int dtype, bool held, const NormArgs &a, hipStream_t st)
 int norm_back_slots(int, int64_t rows, int width)
 {
     if (rows <= 0) return 0;
-    const Shape s = shape_of(width);
-    const int rpb = s.tpr == 64 ? 4 : 1;
-    // four blocks of 256 threads a CU, or two of 1,024: enough loads in flight, and the shares
-    // of dw stay a few per cent of the traffic
-    const int most = s.tpr == 0 ? 64 : s.tpr == 1024 ? 512 : 1024;
-    return (int)((rows + rpb - 1) / rpb < most ? (rows + rpb - 1) / rpb : most);
+    const Shape s = back_shape_of(width);
+    const int rpb = rows_per_block(s);
+    // two blocks of 512 threads a CU, or as many threads in others: enough loads in flight, and
+    // the shares of dw stay a few per cent of the traffic
+    const int most = s.tpr == 0 ? 64 : s.tpr == 1024 ? 512 : s.tpr == 512 ? 512 : 1024;
+    const int64_t blocks = (rows + rpb - 1) / rpb;
+    return (int)(blocks < most ? blocks : most);
 }
 
 hipError_t launch_norm_back(int dtype, const NormBackArgs &a, hipStream_t st)

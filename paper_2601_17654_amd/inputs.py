@@ -130,6 +130,15 @@ def make_tables(space: Space, seed: int, comm_bytes: Sequence[float],
     nbytes = _log_uniform(cu[..., 0], comm_bytes[0], comm_bytes[1])
     cpow = 80.0 + 120.0 * cu[..., 1]
 
+    return expand_tables(space, t0, alpha, beta, p0, gamma, nbytes, cpow)
+
+
+def expand_tables(space: Space, t0, alpha, beta, p0, gamma, nbytes, cpow) -> Dict[str, np.ndarray]:
+    """Tables of partitions from each kernel's figures, by the formulas of make_tables: t0,
+    alpha, beta, p0, gamma [partitions][N] of the compute kernels (t0 may be measured), nbytes
+    and cpow [partitions][M] of the communication kernels."""
+    t0, alpha, beta, p0, gamma, nbytes, cpow = (
+        np.asarray(x, dtype=np.float64) for x in (t0, alpha, beta, p0, gamma, nbytes, cpow))
     f = np.asarray(space.freqs_mhz, dtype=np.float64)
     fmax = f.max()
     k = np.asarray(space.sm_counts, dtype=np.float64)
