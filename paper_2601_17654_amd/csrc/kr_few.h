@@ -5,7 +5,7 @@
 //
 // Bound by the weights' bytes, each read once.  A block takes 16 rows of W (of both planes) for
 // all tokens; its waves take k in turn, 128 bytes of every row at a time, straight into the
-// registers of the 16 x 16 matrix instructions: lanes 16 j .. 16 j + 15 hold 16 bytes of the 16
+// registers of the matrix instructions: lanes 16 j .. 16 j + 15 hold 16 bytes of the 16
 // rows each.  (The order of k within a sum is the same for W and X, so any will do: a lane takes
 // 32 neighbouring bytes and gives them to two instructions.)  The waves' sums are added through
 // LDS, in turn.  Rows may start anywhere and be of any length; nothing is copied first.
@@ -16,21 +16,6 @@
 namespace kr {
 
 constexpr int kFewRows = 32;
-
-__device__ inline f32x4 mma_few(bf16, i32x4 a, i32x4 b, f32x4 c)
-{
-    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a),
-                                                   __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
-}
-__device__ inline f32x4 mma_few(f16, i32x4 a, i32x4 b, f32x4 c)
-{
-    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a),
-                                                  __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
-}
-__device__ inline i32x4 mma_few(int8_t, i32x4 a, i32x4 b, i32x4 c)
-{
-    return __builtin_amdgcn_mfma_i32_16x16x64_i8(a, b, c, 0, 0, 0);
-}
 
 struct FewArgs {
     const char *x, *w[2];
@@ -57,7 +42,7 @@ template <typename E, int NW, int MT, typename Out>
 __global__ __launch_bounds__(NW * 64) void few_kernel(FewArgs a, Out out)
 {
     constexpr int PLANES = Out::PLANES, AHEAD = PLANES * MT > 2 ? 2 : 4;
-    typedef typename Mma<E>::Quad Quad;
+    typedef typename Mma<E>::Acc Acc;
     typedef typename Mma<E>::Sum Sum;
     __shared__ __align__(16) Sum sums[NW][PLANES][MT * 16][16];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -71,11 +56,11 @@ __global__ __launch_bounds__(NW * 64) void few_kernel(FewArgs a, Out out)
 #pragma unroll
     for (int t = 0; t < MT; ++t) x[t] = a.x + (int64_t)min(t * 16 + r, a.m - 1) * a.ldx;
 
-    Quad acc[PLANES][MT];
+    Acc acc[PLANES][MT];
 #pragma unroll
     for (int p = 0; p < PLANES; ++p)
 #pragma unroll
-        for (int t = 0; t < MT; ++t) acc[p][t] = Quad{0, 0, 0, 0};
+        for (int t = 0; t < MT; ++t) acc[p][t] = Acc{0, 0, 0, 0};
     auto add = [&](const i32x4 (&fw)[PLANES][2], const i32x4 (&fx)[MT][2]) {
 #pragma unroll
         for (int h = 0; h < 2; ++h)
@@ -83,7 +68,7 @@ __global__ __launch_bounds__(NW * 64) void few_kernel(FewArgs a, Out out)
             for (int p = 0; p < PLANES; ++p)
 #pragma unroll
                 for (int t = 0; t < MT; ++t)
-                    acc[p][t] = mma_few(E(), fw[p][h], fx[t][h], acc[p][t]);
+                    acc[p][t] = mma(E(), fw[p][h], fx[t][h], acc[p][t]);
     };
 
     const int whole = a.bytes / 128;
@@ -123,7 +108,7 @@ __global__ __launch_bounds__(NW * 64) void few_kernel(FewArgs a, Out out)
     for (int p = 0; p < PLANES; ++p)
 #pragma unroll
         for (int t = 0; t < MT; ++t)
-            *(Quad *)&sums[wave][p][t * 16 + r][lane / 16 * 4] = acc[p][t];
+            *(Acc *)&sums[wave][p][t * 16 + r][lane / 16 * 4] = acc[p][t];
     __syncthreads();
     const int token = (int)threadIdx.x / 2, h = (int)threadIdx.x % 2 * 8;
     if (token >= a.m || n0 + h >= a.n) return;  // NW * 32 threads or more: a token each two

@@ -6,9 +6,10 @@
 // contiguous in m ("crossed": row k holds m = 0, 1, ...).  A block computes a BM x BN tile with
 // one wave per (BM / WM) x (BN / WN) part, over k in steps of 128 bytes (64 16-bit values or
 // 128 bytes).  Operand tiles go from memory straight to LDS, 16 bytes a lane, and from there to
-// registers in the layout of the 32 x 32 matrix instructions: 32 rows x 16 bytes of k for each
-// half of a wave.  (They take half the operand registers of the 16 x 16 ones for the same
-// products, and with them less power: under full load the clock is what the power leaves.)
+// registers in the layout of the 16 x 16 matrix instructions: 16 rows x 16 bytes of k for each
+// group of 16 lanes.  (Under full load the clock is what the power leaves, and the 32 x 32 ones,
+// which move twice the sums through the registers for the same products, leave less: out of
+// registers alone, on random values, 1,820 against 1,960 TFLOP/s in bfloat16.)
 //
 // LDS layout.  A direct copy writes 64 lanes' 16 bytes side by side, so the order within a tile
 // is chosen by what each lane fetches:
@@ -16,12 +17,15 @@
 //    consecutive rows, read at one c, then lie in 16 different 16-byte places of the 256 bytes
 //    that the 64 banks hold.
 //  - crossed: one k a row; 32-byte block b (16 values) of row k sits at place b ^ f(k), f(k) =
-//    2 (k % 4) + 8 (k / 8 % 2) (2 (k % 4) where a row has 8 blocks).  The transposing read takes
-//    4 rows x 32 bytes for each group of 16 lanes; two groups read neighbouring blocks of the
-//    same rows, the other two the rows 8 further on: 16 different places (8, twice).
+//    k % 4 + 4 (k / 8 % 4) (k / 8 % 2 where a row has 8 blocks).  The transposing read takes 4
+//    rows x 32 bytes for each group of 16 lanes, the four groups 8 rows apart: 16 different
+//    places (8, twice).
 // Whatever lies outside an operand is read as zero: rows past its end by the buffer's bound, k
 // past the end of a plain row by an offset beyond that bound.
 #pragma once
+
+#include <type_traits>
+#include <utility>
 
 #include "kr_block.h"
 
@@ -37,37 +41,32 @@ constexpr int kStep = 128;               // bytes of k a step
 constexpr uint32_t kNowhere = 1u << 31;  // an offset past every buffer
 constexpr uint32_t kBufferMost = kNowhere - 1;
 
-typedef float f32x16 __attribute__((ext_vector_type(16)));
-typedef int i32x16 __attribute__((ext_vector_type(16)));
-
-// An element type's matrix instruction: 32 x 32 outputs, 32 bytes of k.  The second operand's
-// rows become the lanes (row lane % 32), the first's the registers: register r is its row
-// 8 (r / 4) + 4 (lane / 32) + r % 4.
+// An element type's matrix instruction: 16 x 16 outputs, 64 bytes of k.  The second operand's
+// rows become the lanes (row lane % 16), the first's the registers: register r is its row
+// 4 (lane / 16) + r.
 template <typename E>
 struct Mma {
-    typedef f32x16 Acc;
-    typedef f32x4 Quad;
+    typedef f32x4 Acc;
     typedef float Sum;
 };
 template <>
 struct Mma<int8_t> {
-    typedef i32x16 Acc;
-    typedef i32x4 Quad;
+    typedef i32x4 Acc;
     typedef int Sum;
 };
-__device__ inline f32x16 mma(bf16, i32x4 a, i32x4 b, f32x16 c)
+__device__ inline f32x4 mma(bf16, i32x4 a, i32x4 b, f32x4 c)
 {
-    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a),
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a),
                                                    __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
-__device__ inline f32x16 mma(f16, i32x4 a, i32x4 b, f32x16 c)
+__device__ inline f32x4 mma(f16, i32x4 a, i32x4 b, f32x4 c)
 {
-    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a),
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a),
                                                   __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
 }
-__device__ inline i32x16 mma(int8_t, i32x4 a, i32x4 b, i32x16 c)
+__device__ inline i32x4 mma(int8_t, i32x4 a, i32x4 b, i32x4 c)
 {
-    return __builtin_amdgcn_mfma_i32_32x32x32_i8(a, b, c, 0, 0, 0);
+    return __builtin_amdgcn_mfma_i32_16x16x64_i8(a, b, c, 0, 0, 0);
 }
 
 // One operand as the host describes it: `rows` rows (m, or k where crossed) of `bytes` bytes,
@@ -129,7 +128,7 @@ struct TileLoader {
             const int i = wave * N + j;
             const int r = i * (64 / LANES) + lane / LANES, c = lane % LANES;
             if (CROSSED) {
-                const int f = (r & 3) << 1 | (LANES == 32 ? (r >> 3 & 1) << 3 : 0);
+                const int f = (r & 3) | (r >> 3 & (LANES == 32 ? 3 : 1)) << 2;
                 off[j] = (uint32_t)r * (uint32_t)o.ld + (uint32_t)map((c ^ f << 1) * 8) * 2;
             } else {
                 const int at = c ^ (r >> 1 & 7);
@@ -173,31 +172,29 @@ struct MapPlanes {
     __device__ int operator()(int r) const { return r / STRIP * (STRIP / 2) + r % (STRIP / 2); }
 };
 
-// Reads of a tile in LDS: rows (plain) or columns (crossed) first .. first + 31, quarter h of
-// the step (32 bytes of k).
+// Reads of a tile in LDS: rows (plain) or columns (crossed) first .. first + 15, half h of the
+// step (64 bytes of k).
 template <bool CROSSED, int ROWS>
 struct TileReader {
-    int at[4];  // plain: a lane's byte for each quarter
+    int at[2];  // plain: a lane's byte for either half
     int k0, fl;
 
     __device__ void init(int lane)
     {
+        const int g = lane / 16, i = lane % 16;
         if (CROSSED) {
-            const int g = lane / 16, i = lane % 16;
-            k0 = ((g >> 1) * 8 + i / 4) * ROWS * 2 + (i % 4) * 8;
-            fl = (g & 1) ^ ((i / 4) << 1 | (ROWS == 256 ? (g >> 1) << 3 : 0));
+            k0 = (g * 8 + i / 4) * ROWS * 2 + (i % 4) * 8;
+            fl = i / 4 | (g & (ROWS == 256 ? 3 : 1)) << 2;
         } else {
-            const int r = lane % 32;
 #pragma unroll
-            for (int h = 0; h < 4; ++h)
-                at[h] = r * kStep + (((h * 2 + lane / 32) ^ (r >> 1 & 7)) << 4);
+            for (int h = 0; h < 2; ++h) at[h] = i * kStep + (((h * 4 + g) ^ i >> 1) << 4);
         }
     }
     __device__ i32x4 read(const char *lds, int first, int h) const
     {
         if (!CROSSED) return *(const i32x4 *)(lds + first * kStep + at[h]);
         typedef __attribute__((address_space(3))) s16x4 *Lds;
-        const char *p = lds + k0 + ((first / 16 ^ fl) << 5) + h * 16 * ROWS * 2;
+        const char *p = lds + k0 + ((first / 16 ^ fl) << 5) + h * 32 * ROWS * 2;
         struct {
             s16x4 lo, hi;
         } x;
@@ -283,14 +280,13 @@ __device__ inline void read_done() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_bar
 // a tile's time at 64 steps).  16-byte chunk c of row r lies at place c ^ r % 16.
 template <int BM, int BN, int WM, int WN, typename E, typename Out, typename Acc>
 __device__ inline void put_tile(E, const MmaArgs &a, const Out &out,
-                                const Acc (&acc)[BM / WM / 32][BN / WN / 32], char *lds, int64_t m0,
+                                const Acc (&acc)[BM / WM / 16][BN / WN / 16], char *lds, int64_t m0,
                                 int64_t n0, int wave, int split, int lane)
 {
-    constexpr int TM = BM / WM / 32, TN = BN / WN / 32, PLANES = Out::PLANES;
+    constexpr int TM = BM / WM / 16, TN = BN / WN / 16, PLANES = Out::PLANES;
     constexpr int STRIP = BN / WN, COLS = STRIP / PLANES;  // of a wave's sums, of its output
     constexpr int LANES = COLS / 8;                        // lanes a row
     constexpr int TOGETHER = 4;                            // rows a lane has in hand
-    typedef typename Mma<E>::Quad Quad;
     typedef typename Mma<E>::Sum Sum;
     static_assert(64 * STRIP * 4 * WM * WN <= 2 * (BM + BN) * kStep, "a wave's share of LDS");
     char *own = lds + wave * 64 * STRIP * 4;
@@ -298,19 +294,14 @@ __device__ inline void put_tile(E, const MmaArgs &a, const Out &out,
     const int n = (int)n0 + wn * COLS + lane % LANES * 8, columns = out.columns(a.n);
     const typename Out::Mine mine = out.mine(n);
 #pragma unroll
-    for (int p = 0; p < TM / 2; ++p) {
+    for (int p = 0; p < TM / 4; ++p) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+        for (int i = 0; i < 4; ++i)
 #pragma unroll
-            for (int j = 0; j < TN; ++j)
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const int row = i * 32 + lane % 32, c = j * 8 + q * 2 + lane / 32;
-                    Quad v;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) v[e] = acc[p * 2 + i][j][q * 4 + e];
-                    *(Quad *)(own + row * STRIP * 4 + ((c ^ row % 16) << 4)) = v;
-                }
+            for (int j = 0; j < TN; ++j) {
+                const int row = i * 16 + lane % 16, c = j * 4 + lane / 16;
+                *(Acc *)(own + row * STRIP * 4 + ((c ^ row % 16) << 4)) = acc[p * 4 + i][j];
+            }
 #pragma unroll 1
         for (int it = 0; it < LANES; it += TOGETHER) {
             const int64_t m1 = m0 + wm * (BM / WM) + p * 64 + lane / LANES;
@@ -324,13 +315,13 @@ __device__ inline void put_tile(E, const MmaArgs &a, const Out &out,
             for (int u = 0; u < TOGETHER; ++u) {
                 const int row = (it + u) * (64 / LANES) + lane / LANES;
                 const int64_t m = m1 + (it + u) * (64 / LANES);
-                Quad v[PLANES][2];
+                Acc v[PLANES][2];
 #pragma unroll
                 for (int k = 0; k < PLANES; ++k)
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
                         const int c = k * COLS / 4 + lane % LANES * 2 + h;
-                        v[k][h] = *(const Quad *)(own + row * STRIP * 4 + ((c ^ row % 16) << 4));
+                        v[k][h] = *(const Acc *)(own + row * STRIP * 4 + ((c ^ row % 16) << 4));
                     }
                 if (m >= a.m || n >= columns) continue;
                 const Sum *v0 = (const Sum *)v[0], *v1 = (const Sum *)v[PLANES - 1];
@@ -354,35 +345,43 @@ __device__ inline void put_tile(E, const MmaArgs &a, const Out &out,
 //   put(m, n, v0, v1, mine, fetched)   eight outputs from n on of row m, from the first and second
 //                                      plane
 //
+// f(0), f(1), ... with constants: 128 steps are more than the compiler unrolls of a loop.
+template <int N>
+using Count = std::make_integer_sequence<int, N>;
+template <typename F, int... X>
+__device__ __attribute__((always_inline)) inline void each(std::integer_sequence<int, X...>, F f)
+{
+    (f(std::integral_constant<int, X>()), ...);
+}
+
 // Two steps' tiles are in LDS, and a wave's registers hold one more: the matrix instructions of
-// a step (4 quarters of TM x TN) run on what was read before them, and between them, one or two in
-// front of each, are
-//   the reads of quarters 1 to 3, from the step's beginning;
+// a step (two halves of TM x TN) run on what was read before them, and between them are
+//   the reads of half 1, from the step's beginning;
 //   from instruction T::free on, when every wave has its step in registers (a barrier): the
 //     copies of the step after next, over this one's tile;
 //   from T::next on, when every wave's copies of the next step have arrived (a barrier): the
-//     reads of its quarter 0.
+//     reads of its half 0.
 // The 256 x 256 form has one wave per SIMD: its 128 x 128 sums halve the reads of LDS against
-// 8 waves' 128 x 64.  There a copy follows every second matrix instruction: a CU takes 16 cycles
-// to address one, its four waves start theirs at the same time, and what they wait for each other
-// the matrix cores wait too (one after every instruction: 2 % slower).
+// 8 waves' 128 x 64.  A CU takes 16 cycles, one matrix instruction, to address a copy, and 8 to
+// read 1 KiB of LDS; its four waves start theirs at the same time, and what they wait for each
+// other the matrix cores wait too.  So reads are two instructions apart there and copies four.
 template <int BLOCK>
-struct Timing;  // copies(x): those started before instruction x;  reads: of quarter 0 each
+struct Timing;  // apart: of reads;  copies(x): those started before instruction x
 template <>
-struct Timing<16> {
-    static constexpr int free = 28, next = 52, reads = 1;
-    static constexpr int copies(int x) { return x - free < 32 ? (x - free + 1) / 2 : 16; }
+struct Timing<64> {
+    static constexpr int free = 40, next = 96, apart = 2;
+    static constexpr int copies(int x) { return x - free < 64 ? (x - free + 3) / 4 : 16; }
 };
 template <>
-struct Timing<4> {
-    static constexpr int free = 12, next = 14, reads = 2;
-    static constexpr int copies(int x) { return (x - free) * 2; }
+struct Timing<16> {
+    static constexpr int free = 12, next = 24, apart = 1;
+    static constexpr int copies(int x) { return x - free < 16 ? (x - free + 1) / 2 : 8; }
 };
 
 template <typename E, bool A_CROSSED, bool B_CROSSED, int BM, int BN, int WM, int WN, typename Out>
 __global__ __launch_bounds__(WM *WN * 64) void mma_kernel(MmaArgs a, Out out)
 {
-    constexpr int NW = WM * WN, TM = BM / WM / 32, TN = BN / WN / 32;
+    constexpr int NW = WM * WN, TM = BM / WM / 16, TN = BN / WN / 16;
     constexpr bool TWO = Out::PLANES == 2;
     constexpr int STRIP = BN / WN;
     typedef typename Mma<E>::Acc Acc;
@@ -400,8 +399,9 @@ __global__ __launch_bounds__(WM *WN * 64) void mma_kernel(MmaArgs a, Out out)
     typedef TileLoader<B_CROSSED, BN, NW> LoadB;
     constexpr int COPIES = LoadA::N + LoadB::N, BLOCK = TM * TN, READS = TM + TN;
     typedef Timing<BLOCK> T;
-    static_assert(T::free >= 3 * READS && T::next + READS / T::reads <= 4 * BLOCK &&
-                      T::copies(T::free) == 0 && T::copies(4 * BLOCK) == COPIES,
+    static_assert(T::free >= T::apart * READS && T::next >= BLOCK &&
+                      T::next + T::apart * READS <= 2 * BLOCK && T::copies(T::free) == 0 &&
+                      T::copies(2 * BLOCK) == COPIES,
                   "the timing fits the tile");
     static_assert(!TWO || LoadB::N * 8 == STRIP / 2, "a wave copies rows of one plane only");
     LoadA la;
@@ -415,9 +415,7 @@ __global__ __launch_bounds__(WM *WN * 64) void mma_kernel(MmaArgs a, Out out)
 #pragma unroll
     for (int i = 0; i < TM; ++i)
 #pragma unroll
-        for (int j = 0; j < TN; ++j)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) acc[i][j][e] = 0;
+        for (int j = 0; j < TN; ++j) acc[i][j] = Acc{0, 0, 0, 0};
 
     const int begin = split * a.per_split, end = min(begin + a.per_split, a.steps * a.pairs);
     la.init(a.a[0], m0, wave, lane, MapSame());
@@ -442,12 +440,12 @@ __global__ __launch_bounds__(WM *WN * 64) void mma_kernel(MmaArgs a, Out out)
             lb.copy(j - LoadA::N, rsrc_b, to + BM * kStep, wave);
     };
 
-    i32x4 fa[4][TM], fb[4][TN];
+    i32x4 fa[2][TM], fb[2][TN];  // halves of a step
     auto read = [&](int j, const char *at, int h) {
         if (j < TN)
-            fb[h][j] = rb.read(at + BM * kStep, wn * STRIP + j * 32, h);
+            fb[h][j] = rb.read(at + BM * kStep, wn * STRIP + j * 16, h);
         else
-            fa[h][j - TN] = ra.read(at, wm * (BM / WM) + (j - TN) * 32, h);
+            fa[h][j - TN] = ra.read(at, wm * (BM / WM) + (j - TN) * 16, h);
     };
 
     // Past the last step the copies are of an empty buffer, zeros that nothing uses: every step
@@ -465,23 +463,21 @@ __global__ __launch_bounds__(WM *WN * 64) void mma_kernel(MmaArgs a, Out out)
         const int buf = (s - begin) & 1;
         const char *at = lds[buf], *next = lds[buf ^ 1];
         aim(s + 2);
-#pragma unroll
-        for (int x = 0; x < 4 * BLOCK; ++x) {
-            if (x < 3 * READS) read(x % READS, at, 1 + x / READS);
+        each(Count<2 * BLOCK>(), [&](auto at_x) __attribute__((always_inline)) {
+            constexpr int x = decltype(at_x)::value;
+            if (x % T::apart == 0 && x / T::apart < READS) read(x / T::apart, at, 1);
             if (x == T::free) read_done();
             if (x == T::next) arrived<T::copies(T::next)>();
             if (x >= T::free) {
 #pragma unroll
                 for (int j = T::copies(x); j < T::copies(x + 1); ++j) copy(j, at);
             }
-            if (x >= T::next && x < T::next + READS / T::reads) {
-#pragma unroll
-                for (int j = 0; j < T::reads; ++j) read((x - T::next) * T::reads + j, next, 0);
-            }
-            const int h = x / BLOCK, i = x % BLOCK / TN, j = x % TN;
+            if (x >= T::next && (x - T::next) % T::apart == 0 && (x - T::next) / T::apart < READS)
+                read((x - T::next) / T::apart, next, 0);
+            constexpr int h = x / BLOCK, i = x % BLOCK / TN, j = x % TN;
             acc[i][j] = mma(E(), fb[h][j], fa[h][i], acc[i][j]);
             __builtin_amdgcn_sched_barrier(0);
-        }
+        });
     }
     read_done();
     arrived<0>();  // the tiles' LDS is free, and no copy will write to it
