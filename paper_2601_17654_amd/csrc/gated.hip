@@ -14,20 +14,25 @@ namespace kr {
 
 namespace {
 
-constexpr float kGelu = 1.5957691216057308f;  // 2 sqrt(2 / pi)
+// z = g (c0 + c1 g^2).  The square is held below 1e30: there z is out of the sigmoid's range
+// either way, and 0 times it is 0.
+struct Curve {
+    float c0, c1;
+};
+Curve curve_of(int act)
+{
+    const float c = 1.5957691216057308f;  // 2 sqrt(2 / pi)
+    return act == KR_GELU ? Curve{c, c * 0.044715f} : Curve{1.0f, 0.0f};
+}
 
 struct Act {
     float p, dz;  // sigmoid, dz/dg
 };
-__device__ inline Act activation(float g, int act)
+__device__ inline Act activation(float g, Curve c)
 {
-    float z = g, dz = 1.0f;
-    if (act == KR_GELU) {
-        const float g2 = 0.044715f * g * g;
-        z = kGelu * fmaf(g2, g, g);
-        dz = kGelu * fmaf(3.0f, g2, 1.0f);
-    }
-    return {__builtin_amdgcn_rcpf(1.0f + __expf(-z)), dz};
+    const float g2 = fminf(g * g, 1e30f);
+    const float z = g * fmaf(c.c1, g2, c.c0);
+    return {__builtin_amdgcn_rcpf(1.0f + __expf(-z)), fmaf(3.0f * c.c1, g2, c.c0)};
 }
 
 template <typename T>
@@ -35,7 +40,8 @@ struct PutGated : Plain {
     static constexpr int PLANES = 2;
     T *out;
     int64_t ldo;
-    int n, act;
+    int n;
+    Curve act;
     __device__ __host__ int columns(int c) const { return c; }
     __device__ void put(int64_t m, int c, const float *g, const float *u, Mine, Fetched) const
     {
@@ -52,7 +58,8 @@ struct PutGatedBack {
     T *d;
     const T *dh;
     int64_t ldh;
-    int n, n_pad, act;
+    int n, n_pad;
+    Curve act;
     __device__ __host__ int columns(int) const { return n_pad; }
     typedef Pack<T, 8> Fetched;
     struct Mine {
@@ -129,7 +136,7 @@ MmaArgs two_planes(const GatedArgs &a)
 template <typename T>
 hipError_t forward(const GatedArgs &a, hipStream_t st)
 {
-    const PutGated<T> out{{}, (T *)a.out, a.ldo, (int)a.n, a.act};
+    const PutGated<T> out{{}, (T *)a.out, a.ldo, (int)a.n, curve_of(a.act)};
     const MmaArgs x = two_planes(a);
     return launch_mma<T, false, false>(x, mma_plan(a.m, a.n, 2, x.steps), out, st);
 }
@@ -139,7 +146,7 @@ hipError_t few(const GatedArgs &a, hipStream_t st)
 {
     const FewArgs x{a.x.p, {a.wg.p, a.wu.p}, a.x.ld, {a.wg.ld, a.wu.ld}, (int)a.m, (int)a.n,
                     (int)a.x.bytes};
-    return launch_few<T>(x, PutGated<T>{{}, (T *)a.out, a.ldo, (int)a.n, a.act}, st);
+    return launch_few<T>(x, PutGated<T>{{}, (T *)a.out, a.ldo, (int)a.n, curve_of(a.act)}, st);
 }
 
 // The three products of the backward pass, in turn: their plans share the workspace.
@@ -157,7 +164,7 @@ hipError_t backward(const GatedBackArgs &a, hipStream_t st)
 {
     const int64_t m = a.f.m, n = a.f.n;
     if (m > 0) {
-        const PutGatedBack<T> out{(T *)a.d, (const T *)a.dh, a.ldh, (int)n, (int)a.n_pad, a.f.act};
+        const PutGatedBack<T> out{(T *)a.d, (const T *)a.dh, a.ldh, (int)n, (int)a.n_pad, curve_of(a.f.act)};
         const MmaArgs x = two_planes(a.f);
         if (const hipError_t e = launch_mma<T, false, false>(x, mma_plan(m, a.n_pad, 2, x.steps), out, st);
             e != hipSuccess)
@@ -193,26 +200,33 @@ hipError_t backward(const GatedBackArgs &a, hipStream_t st)
 
 }  // namespace
 
-// Splits: where a product has fewer tiles than the chip has CUs, its sum is cut into runs of at
-// least 8 steps, added up afterwards.
+// The cheaper of the two tile sizes, and of up to 16 splits of the sum, by an estimate in
+// microseconds.  256 x 256: 1.4 a step and 9 for what surrounds them, one tile a CU at a time.
+// 128 x 128: 0.9 and 4, two a CU, so that half a round is one each.  A split adds its partial
+// sums, written and read at 4 TB/s, and a launch.  Measured, bfloat16, two planes (large / small):
+//   4096 x 4096 x 2048   116 / 134 us        4096 x 2176 x 4096   184 / 148 us
+//   1024 x 14336 x 4096  197 / 220 us        2048 x 2048 x 512     23 / 15 us
 MmaPlan mma_plan(int64_t m, int64_t n, int planes, int steps)
 {
-    MmaPlan p{};
-    auto tiles = [&](int64_t bm, int64_t bn) { return ((m + bm - 1) / bm) * ((n + bn - 1) / bn); };
-    p.large = tiles(256, 256 / planes) >= 256;
-    const int bm = p.large ? 256 : 128, bn = bm / planes;
-    p.tiles_m = (int)((m + bm - 1) / bm);
-    p.tiles_n = (int)((n + bn - 1) / bn);
-    const int64_t all = (int64_t)p.tiles_m * p.tiles_n;
-    int64_t s = all >= 256 ? 1 : 512 / all;
-    s = s < steps / 8 ? s : steps / 8;
-    if (s < 1) s = 1;
-    if (s > 64) s = 64;
-    p.per_split = (int)((steps + s - 1) / s);
-    if (p.per_split < 1) p.per_split = 1;
-    p.splits = steps ? (steps + p.per_split - 1) / p.per_split : 1;
-    p.part_bytes = p.splits > 1 ? (int64_t)p.splits * planes * m * n * 4 : 0;
-    return p;
+    MmaPlan best{};
+    double least = 0;
+    for (const bool large : {true, false}) {
+        const int bm = large ? 256 : 128, bn = bm / planes;
+        const int64_t tm = (m + bm - 1) / bm, tn = (n + bn - 1) / bn;
+        for (int s = 1; s <= 16 && (s == 1 || (steps + s - 1) / s >= 4); ++s) {
+            const int per = steps > 0 ? (steps + s - 1) / s : 1;
+            const int splits = steps > 0 ? (steps + per - 1) / per : 1;
+            if (splits != s) continue;
+            const int64_t rounds = (tm * tn * s + 255) / 256;
+            const double part = s > 1 ? 4.0 * s * planes * m * n : 0;
+            const double cost = rounds * (large ? 1.4 * per + 9 : 0.45 * per + 2) +
+                                (s > 1 ? 4 + 2 * part / 4e6 : 0);
+            if (best.tiles_m && cost >= least) continue;
+            least = cost;
+            best = {large, (int)tm, (int)tn, s, per, (int64_t)part};
+        }
+    }
+    return best;
 }
 
 size_t gated_part(int64_t m, int64_t n, int64_t k_bytes)

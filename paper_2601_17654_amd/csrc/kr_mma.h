@@ -69,6 +69,26 @@ __device__ inline i32x4 mma(int8_t, i32x4 a, i32x4 b, i32x4 c)
     return __builtin_amdgcn_mfma_i32_16x16x64_i8(a, b, c, 0, 0, 0);
 }
 
+// The same, c += a b, with the sums kept where they are.  (Left to itself, the compiler gives the
+// result other registers than the sums had, and moves a hundred a step to make room.)  The
+// operands come from LDS, whose arrival the compiler waits for, and an instruction's sums are
+// not touched again before sums_done() but by the next on the same sums, 16 or more later: the
+// wait states that the compiler adds around the builtin are not needed.
+__device__ inline void mma_in_place(bf16, i32x4 a, i32x4 b, f32x4 &c)
+{
+    asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b));
+}
+__device__ inline void mma_in_place(f16, i32x4 a, i32x4 b, f32x4 &c)
+{
+    asm volatile("v_mfma_f32_16x16x32_f16 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b));
+}
+__device__ inline void mma_in_place(int8_t, i32x4 a, i32x4 b, i32x4 &c)
+{
+    asm volatile("v_mfma_i32_16x16x64_i8 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b));
+}
+// Between such instructions and any other use of their sums.
+__device__ inline void sums_done() { asm volatile("s_nop 15\n\ts_nop 15" ::: "memory"); }
+
 // One operand as the host describes it: `rows` rows (m, or k where crossed) of `bytes` bytes,
 // `ld` bytes apart.  p and ld are multiples of 16 bytes, and so is `bytes` (crossed) or it is
 // followed by zeros up to the next multiple (plain, a copy of this library's).
@@ -217,7 +237,7 @@ struct MmaArgs {
 };
 
 // The tile of a block.  Blocks go to the 8 XCDs in turn: each XCD takes a run of consecutive
-// tiles, and a run covers 8 tiles of m before it moves on in n, so that the tiles of an XCD
+// tiles, and a run covers 4 tiles of m before it moves on in n, so that the tiles of an XCD
 // share rows of both operands in its L2.
 __device__ inline void tile_of(const MmaArgs &a, int *tm, int *tn, int *split)
 {
@@ -226,8 +246,8 @@ __device__ inline void tile_of(const MmaArgs &a, int *tm, int *tn, int *split)
     int t = x * q + min(x, r) + (id >> 3);
     *split = t / per;
     t -= *split * per;
-    const int group = 8 * a.tiles_n, g = t / group, first = g * 8;
-    const int size = min(8, a.tiles_m - first);
+    const int group = 4 * a.tiles_n, g = t / group, first = g * 4;
+    const int size = min(4, a.tiles_m - first);
     t -= g * group;
     *tm = first + t % size;
     *tn = t / size;
@@ -459,6 +479,7 @@ __global__ __launch_bounds__(WM *WN * 64) void mma_kernel(MmaArgs a, Out out)
     arrived<COPIES>();
 #pragma unroll
     for (int j = 0; j < TM + TN; ++j) read(j, lds[0], 0);
+    sums_done();
     for (int s = begin; s < end; ++s) {
         const int buf = (s - begin) & 1;
         const char *at = lds[buf], *next = lds[buf ^ 1];
@@ -475,10 +496,11 @@ __global__ __launch_bounds__(WM *WN * 64) void mma_kernel(MmaArgs a, Out out)
             if (x >= T::next && (x - T::next) % T::apart == 0 && (x - T::next) / T::apart < READS)
                 read((x - T::next) / T::apart, next, 0);
             constexpr int h = x / BLOCK, i = x % BLOCK / TN, j = x % TN;
-            acc[i][j] = mma(E(), fb[h][j], fa[h][i], acc[i][j]);
+            mma_in_place(E(), fb[h][j], fa[h][i], acc[i][j]);
             __builtin_amdgcn_sched_barrier(0);
         });
     }
+    sums_done();
     read_done();
     arrived<0>();  // the tiles' LDS is free, and no copy will write to it
     put_tile<BM, BN, WM, WN>(E(), a, out, acc, lds[0], m0, n0, wave, split, lane);
