@@ -435,10 +435,11 @@ hipError_t back_typed(const NormBackArgs &a, int slots, hipStream_t st)
             norm_back_kernel<T, 1024, 8><<<slots, 1024, 0, st>>>(a);
         else if (s.tpr == 1024) norm_back_kernel<T, 1024, 16><<<slots, 1024, 0, st>>>(a);
         else {
-            const hipError_t e = back_long_rows<T>(a, st);
-            if (e != hipSuccess) return e;
+            // dw first: dx may take dout's place
             const dim3 grid((unsigned)((a.width + 255) / 256), slots);
             norm_back_long_weight_kernel<T><<<grid, 256, 0, st>>>(a);
+            const hipError_t e = back_long_rows<T>(a, st);
+            if (e != hipSuccess) return e;
         }
     }
     norm_weight_kernel<<<(a.width + 31) / 32, 1024, 0, st>>>(a.part, slots, a.width, a.dw);

@@ -164,6 +164,26 @@ def test_in_place(kr):
         assert torch.equal(xs, want.out) and torch.equal(rs, want.sum)
 
 
+@pytest.mark.parametrize("over", ["dout", "dsum"])
+@pytest.mark.parametrize("width", [100, 1000, 4096, 9000, 16384, 20000])
+def test_gradient_in_place(kr, width, over):
+    """dx in the place of either gradient that it is made from."""
+    (s, g, d, _), w = make(7, width, torch.bfloat16, width)
+    f = (1 / s.float().square().mean(-1).sqrt()).cuda()
+    s, g, d, w = s.cuda(), g.cuda(), d.cuda(), w.cuda()
+    dx, dw = kr.add_rms_norm_backward(g, s, w, f, d)
+    got = torch.empty_like(dw)
+    wsb = kr._lib.kr_add_rms_norm_backward_workspace(2, 7, width)
+    ws = torch.empty(wsb, dtype=torch.uint8, device="cuda")
+    to = g if over == "dout" else d
+    kr._check("kr_add_rms_norm_backward",
+              kr._lib.kr_add_rms_norm_backward(2, 7, width, kr._ptr(g), width, kr._ptr(s), width,
+                                               kr._ptr(w), kr._ptr(f), kr._ptr(d), width,
+                                               kr._ptr(to), width, kr._ptr(got), kr._ptr(ws), wsb,
+                                               kr._stream()))
+    assert torch.equal(to, dx) and torch.equal(got, dw)
+
+
 @pytest.mark.parametrize("width", [24, 700, 3000, 9000, 20001])
 def test_rows_without_a_usable_value(kr, width):
     """Rows of zeros, of values too small for a scale, with a NaN, with an infinity; their
