@@ -518,7 +518,7 @@ kr_status kr_decode_candidates(const kr_space *space, const int32_t *idx, int64_
  * kr_add_rms_norm -- sum of input and residual, and its root-mean-square norm:
  *   s = x + residual,  rstd = 1 / sqrt(mean(s^2) + eps),  out = s * rstd * weight
  *   type              of x, residual, weight, sum and out
- *   rows, width       rows >= 0, 1 <= width <= 2^30
+ *   rows, width       rows >= 0, 1 <= width <= 2^24 (KR_EUNSUPPORTED above)
  *   residual          NULL: s = x
  *   sum               s, rounded to the type (the norm uses the unrounded s), or NULL
  *   rstd              [rows] or NULL: what the backward pass takes
@@ -565,8 +565,8 @@ size_t kr_add_rms_norm_backward_workspace(int32_t type, int64_t rows, int64_t wi
  *   a [m][k], sa [m]   tokens (kr_add_rms_norm_bytes)
  *   b [n][k], sb [n]   channels: a weight matrix as its rows of inputs
  *   type               of out
- * m >= 0, n >= 1, k >= 1; KR_EUNSUPPORTED for m >= 2^31, n > 2^30 or k > 131071.  Strides are
- * in elements.  The workspace (16-byte aligned) depends on sizes, strides and addresses; 0:
+ * m >= 0, n >= 1, k >= 1; KR_EUNSUPPORTED for m >= 2^31, n > 2^27, k > 131071 or an output of
+ * more than 2^23 tiles of 128 x 64.  Strides are in elements; out overlaps no input.  The workspace (16-byte aligned) depends on sizes, strides and addresses; 0:
  * none needed, or an invalid argument.
  */
 typedef struct kr_bytes {
@@ -587,8 +587,8 @@ size_t kr_byte_matmul_workspace(const kr_bytes *p);
  *   x           [rows][width]
  *   wg, wu      [hidden][width]
  *   out         [rows][hidden]
- * rows >= 0, width >= 1, hidden >= 1; KR_EUNSUPPORTED for rows >= 2^31 or more than 2^20
- * columns.  The workspace (16-byte aligned) depends on sizes, strides and addresses; 0: none
+ * rows >= 0, width >= 1, hidden >= 1; KR_EUNSUPPORTED for rows >= 2^31, more than 2^20 columns
+ * or matrices of more than 2^23 tiles of 128 x 64.  out overlaps no input.  The workspace (16-byte aligned) depends on sizes, strides and addresses; 0: none
  * needed, or an invalid argument.
  */
 #define KR_SILU 0

@@ -782,6 +782,10 @@ def _new(shape, dtype) -> torch.Tensor:
     return torch.empty(shape, dtype=dtype, device="cuda")
 
 
+def _new_like(x: torch.Tensor) -> torch.Tensor:
+    return torch.empty_like(x, memory_format=torch.contiguous_format)
+
+
 def _scratch(nbytes: int):
     """A call's own workspace and its address."""
     if not nbytes:
@@ -822,8 +826,8 @@ def add_rms_norm(x, weight, residual=None, eps: float = 1e-6) -> Normed:
     """s = x + residual and s * rstd * weight, rstd = 1 / sqrt(mean(s^2) + eps) over the last
     dimension (kr_add_rms_norm)."""
     t, dev, xr, n, ldx, width, w, rr, ldr = _norm_inputs(x, weight, residual)
-    out = _new(x.shape, x.dtype)
-    total = x if rr is None else _new(x.shape, x.dtype)
+    out = _new_like(x)
+    total = x if rr is None else _new_like(x)
     rstd = _new(x.shape[:-1], torch.float32)
     _check("kr_add_rms_norm",
            _lib.kr_add_rms_norm(t, n, width, xr.data_ptr(), ldx,
@@ -838,7 +842,7 @@ def add_rms_norm_bytes(x, weight, residual=None, eps: float = 1e-6) -> NormedByt
     (kr_add_rms_norm_bytes)."""
     t, dev, xr, n, ldx, width, w, rr, ldr = _norm_inputs(x, weight, residual)
     q = _new(x.shape, torch.int8)
-    total = x if rr is None else _new(x.shape, x.dtype)
+    total = x if rr is None else _new_like(x)
     scale, rstd = _new(x.shape[:-1], torch.float32), _new(x.shape[:-1], torch.float32)
     _check("kr_add_rms_norm_bytes",
            _lib.kr_add_rms_norm_bytes(t, n, width, xr.data_ptr(), ldx,
@@ -865,7 +869,7 @@ def add_rms_norm_backward(dout, sum, weight, rstd, dsum=None):
     if dsum is not None:
         _like(dsum, dout, "dsum", "dout")
         dr, _, ldd = _rows(dsum, "dsum", dev, width)
-    dx = _new(dout.shape, dout.dtype)
+    dx = _new_like(dout)
     dw = _new(width, torch.float32)
     wsb = _lib.kr_add_rms_norm_backward_workspace(t, n, width)
     ws, at = _scratch(wsb)
@@ -948,8 +952,7 @@ def gated_projection_backward(dh, x, wg, wu, act: str = "silu"):
         raise ValueError("dh must be %s, got %s" % (tuple(x.shape[:-1]) + (g.hidden,),
                                                     tuple(dh.shape)))
     hr, _, ldh = _rows(dh, "dh", dev, g.hidden)
-    dx = _new(x.shape, x.dtype)
-    dwg, dwu = _new(wg.shape, x.dtype), _new(wg.shape, x.dtype)
+    dx, dwg, dwu = _new_like(x), _new_like(wg), _new_like(wu)
     p = ctypes.byref(g)
     wsb = _lib.kr_gated_projection_backward_workspace(p)
     ws, at = _scratch(wsb)

@@ -8,7 +8,7 @@ using namespace kr;
 
 namespace {
 
-constexpr int64_t kWidthMost = 1 << 30;
+constexpr int64_t kWidthMost = 1 << 24;
 
 bool type_ok(int32_t t) { return t == KR_F32 || t == KR_F16 || t == KR_BF16; }
 
@@ -98,6 +98,8 @@ constexpr size_t kAlign = 256;
 constexpr int64_t kLdMost = 1 << 22;    // bytes between rows that the tiles' 32-bit offsets take
 constexpr int64_t kRowMost = 1 << 21;   // bytes of a row: with two rows side by side, that
 constexpr int64_t kRowsMost = 0x7FFFFFFF;
+constexpr int64_t kChannelsMost = 1 << 27;
+constexpr int64_t kTilesMost = 1 << 23;  // a grid has fewer than 2^32 threads, 256 a block
 constexpr int64_t kBytesMost = 131071;  // 2^14 times this is below 2^31: sums cannot overflow
 
 // Bump allocator over the caller's workspace (or a size query when base is null).
@@ -112,6 +114,12 @@ struct Carve {
         return p;
     }
 };
+
+// Whether a grid holds the smaller tiles of rows x columns outputs (two planes: half as wide).
+bool tiles_fit(int64_t rows, int64_t columns)
+{
+    return ((rows + 127) / 128) * ((columns + 63) / 64) <= kTilesMost;
+}
 
 int64_t padded(int64_t bytes) { return (bytes + 15) / 16 * 16; }
 
@@ -149,7 +157,8 @@ bool gated_ok(const kr_gated *g)
 
 bool gated_fits(const kr_gated *g)
 {
-    return g->rows <= kRowsMost && g->width <= kRowMost / 2 && g->hidden <= kRowMost / 2;
+    return g->rows <= kRowsMost && g->width <= kRowMost / 2 && g->hidden <= kRowMost / 2 &&
+           tiles_fit(g->rows, g->hidden > g->width ? g->hidden : g->width);
 }
 
 struct GatedLaid {
@@ -237,7 +246,10 @@ bool bytes_ok(const kr_bytes *p)
            matrix_ok(p->b, p->ldb, p->k, 1) && (p->m == 0 || p->sa) && p->sb;
 }
 
-bool bytes_fits(const kr_bytes *p) { return p->m <= kRowsMost && p->n <= kWidthMost && p->k <= kBytesMost; }
+bool bytes_fits(const kr_bytes *p)
+{
+    return p->m <= kRowsMost && p->n <= kChannelsMost && p->k <= kBytesMost && tiles_fit(p->m, p->n);
+}
 
 kr_status bytes_run(const kr_bytes *p, int32_t type, void *out, int64_t ldo, Carve &c, hipStream_t st)
 {

@@ -151,3 +151,16 @@ def test_binding_products():
         b.gated_projection(x.half(), w.half(), w.half(), act="relu")
     with pytest.raises(ValueError):
         b.gated_projection(x.half(), w.half(), w.half())  # not on the device
+
+
+def test_grids():
+    """Sizes within each limit whose output would take more blocks than a launch has."""
+    big = 1 << 20
+    g = gated(rows=1 << 24, hidden=big, ldx=8)
+    p = ctypes.byref(g)
+    assert L.kr_gated_projection(p, one, big, one, 1 << 50, null) == b.KR_EUNSUPPORTED
+    assert L.kr_gated_projection_backward(p, one, big, one, 8, one, 8, one, 8, one, 1 << 50,
+                                          null) == b.KR_EUNSUPPORTED
+    q = ctypes.byref(b.KrBytes(1 << 24, 1 << 24, 16, 16, 16, 16, 16, 16, 16))
+    assert L.kr_byte_matmul(q, BF16, one, 1 << 24, one, 1 << 50, null) == b.KR_EUNSUPPORTED
+    assert L.kr_byte_matmul_workspace(q) == 0

@@ -157,6 +157,23 @@ def test_strides_and_what_lies_beside(kr, dtype, gap, start):
     assert all(torch.equal(p, q) for p, q in zip(a, b))
 
 
+@pytest.mark.parametrize("rows", [1, 9, 32])
+def test_few_rows_beside_nan(kr, rows):
+    """The same for the form of few rows, which reads the matrices as they lie."""
+    for width, hidden, start, gap in ((200, 152, 8, 8), (131, 75, 3, 2), (64, 33, 1, 0)):
+        x, wg, wu, _ = make(rows, width, hidden, torch.bfloat16, width)
+
+        def inside(t):
+            big = torch.full((t.shape[0] + 2, t.shape[1] + start + gap), float("nan"),
+                             dtype=t.dtype, device="cuda")
+            v = big[1:-1, start:start + t.shape[1]]
+            v.copy_(t)
+            return v
+
+        assert torch.equal(kr.gated_projection(inside(x), inside(wg), inside(wu)),
+                           kr.gated_projection(x, wg, wu))
+
+
 @pytest.mark.parametrize("at", [0, 1])
 def test_weights_of_unlike_strides(kr, at):
     """One weight matrix inside a larger one, aligned and not, the other by itself."""
