@@ -269,7 +269,9 @@ __global__ __launch_bounds__(256) void pad_kernel(PadArgs a)
     const int64_t per = m.to_ld / 16, all = m.rows * per;
     for (int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x; id < all;
          id += (int64_t)gridDim.x * 256) {
-        const int64_t r = id / per, c = (id - r * per) * 16;
+        // a 64-bit division costs more than the copy
+        const int64_t r = id >> 32 ? id / per : (int64_t)((uint32_t)id / (uint32_t)per);
+        const int64_t c = (id - r * per) * 16;
         const char *p = m.from + r * m.from_ld + c;
         Pack<char, 16> x;
         if (c + 16 <= m.bytes) {
