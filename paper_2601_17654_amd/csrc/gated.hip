@@ -272,14 +272,7 @@ __global__ __launch_bounds__(256) void pad_kernel(PadArgs a)
         // a 64-bit division costs more than the copy
         const int64_t r = id >> 32 ? id / per : (int64_t)((uint32_t)id / (uint32_t)per);
         const int64_t c = (id - r * per) * 16;
-        const char *p = m.from + r * m.from_ld + c;
-        Pack<char, 16> x;
-        if (c + 16 <= m.bytes) {
-            x = load16(p);
-        } else {
-#pragma unroll
-            for (int e = 0; e < 16; ++e) x.v[e] = c + e < m.bytes ? p[e] : (char)0;
-        }
+        const Pack<char, 16> x = load_row(m.from + r * m.from_ld, (int)c, (int)m.bytes);
         store16(m.to + r * m.to_ld + c, x);
     }
 }

@@ -39,16 +39,27 @@ __device__ inline void store16(T *p, const Pack<T, kVec<T>> &x)
     *(Loose16 *)p = __builtin_bit_cast(Loose16, x);
 }
 
-// Elements [c, c + kVec) of a row of `width`, 0 past its end.  Loads and conversions are apart
-// so that a thread's loads are all in flight before the first is waited for.
+// Elements [c, c + kVec) of a row of `width`, 0 past its end.  One load for every thread: past the
+// last whole vector it is the row's last one, moved down (elements loaded one by one there made
+// a wave wait for each).  Loads and conversions are apart so that a thread's loads are all in
+// flight before the first is waited for.
 template <typename T>
 __device__ inline Pack<T, kVec<T>> load_row(const T *row, int c, int width)
 {
     constexpr int V = kVec<T>;
-    if (c + V <= width) return load16(row + c);
-    Pack<T, V> x;
+    if (width < V) {
+        Pack<T, V> x;
 #pragma unroll
-    for (int e = 0; e < V; ++e) x.v[e] = c + e < width ? row[c + e] : (T)0;
+        for (int e = 0; e < V; ++e) x.v[e] = c + e < width ? row[c + e] : (T)0;
+        return x;
+    }
+    const int at = min(c, width - V), drop = c - at;
+    Pack<T, V> x = load16(row + at);
+    if (drop) {
+        typedef unsigned __int128 u128;
+        const u128 all = __builtin_bit_cast(u128, x);
+        x = __builtin_bit_cast(Pack<T, V>, drop < V ? all >> (8 * (int)sizeof(T) * drop) : (u128)0);
+    }
     return x;
 }
 
