@@ -82,18 +82,21 @@ __global__ __launch_bounds__(NW * 64) void few_kernel(FewArgs a, Out out)
         for (int u = 0; u < AHEAD; ++u) add(fw[u], fx[u]);
     }
     for (; s * 128 < a.bytes; s += NW) {
-        i32x4 fw[PLANES][2], fx[MT][2];
-        const int c = s * 128 + part;
-#pragma unroll
+#pragma unroll 1
         for (int h = 0; h < 2; ++h) {
+            const int c = s * 128 + part + h * 16;
+            i32x4 fw[PLANES], fx[MT];
 #pragma unroll
             for (int p = 0; p < PLANES; ++p)
-                fw[p][h] = __builtin_bit_cast(i32x4, load_row(w[p], c + h * 16, a.bytes));
+                fw[p] = __builtin_bit_cast(i32x4, load_row(w[p], c, a.bytes));
 #pragma unroll
             for (int t = 0; t < MT; ++t)
-                fx[t][h] = __builtin_bit_cast(i32x4, load_row(x[t], c + h * 16, a.bytes));
+                fx[t] = __builtin_bit_cast(i32x4, load_row(x[t], c, a.bytes));
+#pragma unroll
+            for (int p = 0; p < PLANES; ++p)
+#pragma unroll
+                for (int t = 0; t < MT; ++t) acc[p][t] = mma(E(), fw[p], fx[t], acc[p][t]);
         }
-        add(fw, fx);
     }
 
 #pragma unroll

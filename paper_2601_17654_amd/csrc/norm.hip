@@ -4,11 +4,12 @@
 //   s = x + r,  f = 1 / sqrt(mean(s^2) + eps),  n = s f w
 //
 // Every element is read once and written once: a row stays in the registers of the threads
-// that share it (16 to 1,024 of them, 8 or 16 elements each), so its mean costs no second
+// that share it (16 to 1,024 of them, 8 elements each, 16 above 8,192), so its mean costs no second
 // pass over memory.  Rows of more than 16,384 elements are read again from memory instead.
 // All arithmetic is in 32 bits; stored values are rounded once.
 //
-// Bound by memory.  16384 x 4096 in bfloat16: forward 99 us (5.4 TB/s of its 537 MB), backward
+// Bound by memory.  Eight elements a thread: more waves, each with little to wait for (with 16 the
+// forward pass below takes 99 us).  16384 x 4096 in bfloat16: forward 94 us (5.7 TB/s of its 537 MB), backward
 // 102 us (5.2 TB/s); 8192 x 8192 in float16 to bytes 88 us (5.3 TB/s).
 #include "kr_block.h"
 
@@ -16,6 +17,9 @@ namespace kr {
 
 namespace {
 
+// Threads of a block: rows of up to a wave share one.
+template <int TPR>
+constexpr int kBlock = TPR <= 64 ? 256 : TPR;
 constexpr int kRowMost = 16384;  // elements that 1,024 threads hold, 16 each
 
 // A row's values held in 8 bits.  The largest magnitude stands at 127; one below 2^-100 has no
@@ -63,9 +67,9 @@ __device__ inline float factor_of(float squares, int width, float eps)
 }
 
 template <typename T, int TPR, int FPT, bool HELD>
-__global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_kernel(NormArgs a)
+__global__ __launch_bounds__(kBlock<TPR>) void norm_kernel(NormArgs a)
 {
-    constexpr int V = kVec<T>, NV = FPT / V, RPB = TPR < 256 ? 256 / TPR : 1;
+    constexpr int V = kVec<T>, NV = FPT / V, RPB = kBlock<TPR> / TPR;
     __shared__ float part[TPR > 64 ? TPR / 64 : 1];
     __shared__ uint32_t part_top[TPR > 64 ? TPR / 64 : 1];
     const int t = threadIdx.x % TPR;
@@ -187,10 +191,10 @@ __global__ __launch_bounds__(1024) void norm_long_kernel(NormArgs a)
 // A block takes rows in turn and keeps its share of dw in registers; the blocks' shares are
 // added by norm_weight_kernel in a fixed order.
 template <typename T, int TPR, int FPT>
-__global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_back_kernel(NormBackArgs a)
+__global__ __launch_bounds__(kBlock<TPR>) void norm_back_kernel(NormBackArgs a)
 {
-    constexpr int V = kVec<T>, NV = FPT / V, RPB = TPR < 256 ? 256 / TPR : 1;
-    constexpr bool AHEAD = FPT == 8;  // the next row's loads: with 16 they cost half the waves
+    constexpr int V = kVec<T>, NV = FPT / V, RPB = kBlock<TPR> / TPR;
+    constexpr bool AHEAD = FPT == 8;  // the next row's loads: with 16 there are no registers left
     __shared__ float part[2][TPR > 64 ? TPR / 64 : 1];
     __shared__ float share[RPB > 1 ? RPB * TPR * FPT : 1];
     const int t = threadIdx.x % TPR, sub = threadIdx.x / TPR;
@@ -354,23 +358,15 @@ struct Shape {
 };
 Shape shape_of(int width)
 {
-    for (const Shape s : {Shape{16, 8}, {32, 8}, {64, 8}, {64, 16}, {256, 8}, {384, 8}, {256, 16},
+    for (const Shape s : {Shape{16, 8}, {32, 8}, {64, 8}, {128, 8}, {256, 8}, {384, 8}, {512, 8},
                           {768, 8}, {1024, 8}, {1024, 16}})
         if (width <= s.tpr * s.fpt) return s;
     return {0, 0};
 }
-int rows_per_block(Shape s) { return s.tpr > 0 && s.tpr < 256 ? 256 / s.tpr : 1; }
+int rows_per_block(Shape s) { return s.tpr > 0 && s.tpr <= 64 ? 256 / s.tpr : 1; }
 
 // Rows of one launch: a grid has fewer than 2^32 threads.
 constexpr int64_t kRowsPerLaunch = 1 << 21;
-
-// The backward pass holds more of a row, and the next one: eight elements a thread, as long as
-// there are threads.
-Shape back_shape_of(int width)
-{
-    const Shape s = shape_of(width);
-    return s.tpr == 256 && s.fpt == 16 ? Shape{512, 8} : s;
-}
 
 template <typename T, bool HELD>
 hipError_t norm_rows(const NormArgs &a, hipStream_t st)
@@ -380,12 +376,12 @@ hipError_t norm_rows(const NormArgs &a, hipStream_t st)
     const dim3 grid((unsigned)((a.rows + rpb - 1) / rpb));
     if (s.tpr == 16) norm_kernel<T, 16, 8, HELD><<<grid, 256, 0, st>>>(a);
     else if (s.tpr == 32) norm_kernel<T, 32, 8, HELD><<<grid, 256, 0, st>>>(a);
-    else if (s.tpr == 64 && s.fpt == 8) norm_kernel<T, 64, 8, HELD><<<grid, 256, 0, st>>>(a);
-    else if (s.tpr == 64) norm_kernel<T, 64, 16, HELD><<<grid, 256, 0, st>>>(a);
-    else if (s.tpr == 256 && s.fpt == 8) norm_kernel<T, 256, 8, HELD><<<grid, 256, 0, st>>>(a);
+    else if (s.tpr == 64) norm_kernel<T, 64, 8, HELD><<<grid, 256, 0, st>>>(a);
+    else if (s.tpr == 128) norm_kernel<T, 128, 8, HELD><<<grid, 128, 0, st>>>(a);
+    else if (s.tpr == 256) norm_kernel<T, 256, 8, HELD><<<grid, 256, 0, st>>>(a);
     else if (s.tpr == 384) norm_kernel<T, 384, 8, HELD><<<grid, 384, 0, st>>>(a);
     else if (s.tpr == 768) norm_kernel<T, 768, 8, HELD><<<grid, 768, 0, st>>>(a);
-    else if (s.tpr == 256) norm_kernel<T, 256, 16, HELD><<<grid, 256, 0, st>>>(a);
+    else if (s.tpr == 512) norm_kernel<T, 512, 8, HELD><<<grid, 512, 0, st>>>(a);
     else if (s.tpr == 1024 && s.fpt == 8) norm_kernel<T, 1024, 8, HELD><<<grid, 1024, 0, st>>>(a);
     else if (s.tpr == 1024) norm_kernel<T, 1024, 16, HELD><<<grid, 1024, 0, st>>>(a);
     else norm_long_kernel<T, HELD><<<grid, 1024, 0, st>>>(a);
@@ -428,12 +424,12 @@ hipError_t back_long_rows(NormBackArgs a, hipStream_t st)
 template <typename T>
 hipError_t back_typed(const NormBackArgs &a, int slots, hipStream_t st)
 {
-    const Shape s = back_shape_of(a.width);
+    const Shape s = shape_of(a.width);
     if (a.rows > 0) {
         if (s.tpr == 16) norm_back_kernel<T, 16, 8><<<slots, 256, 0, st>>>(a);
         else if (s.tpr == 32) norm_back_kernel<T, 32, 8><<<slots, 256, 0, st>>>(a);
-        else if (s.tpr == 64 && s.fpt == 8) norm_back_kernel<T, 64, 8><<<slots, 256, 0, st>>>(a);
-        else if (s.tpr == 64) norm_back_kernel<T, 64, 16><<<slots, 256, 0, st>>>(a);
+        else if (s.tpr == 64) norm_back_kernel<T, 64, 8><<<slots, 256, 0, st>>>(a);
+        else if (s.tpr == 128) norm_back_kernel<T, 128, 8><<<slots, 128, 0, st>>>(a);
         else if (s.tpr == 256) norm_back_kernel<T, 256, 8><<<slots, 256, 0, st>>>(a);
         else if (s.tpr == 384) norm_back_kernel<T, 384, 8><<<slots, 384, 0, st>>>(a);
         else if (s.tpr == 512) norm_back_kernel<T, 512, 8><<<slots, 512, 0, st>>>(a);
@@ -465,11 +461,11 @@ hipError_t launch_norm(int dtype, bool held, const NormArgs &a, hipStream_t st)
 int norm_back_slots(int, int64_t rows, int width)
 {
     if (rows <= 0) return 0;
-    const Shape s = back_shape_of(width);
+    const Shape s = shape_of(width);
     const int rpb = rows_per_block(s);
     // 12 to 16 waves a CU: enough loads in flight, and the shares of dw, written once and read
     // once, stay a few per cent of the traffic
-    const int most = s.tpr == 0 ? 64 : s.tpr <= 256 ? 1024 : s.tpr <= 512 ? 512 : 256;
+    const int most = s.tpr == 0 ? 64 : s.tpr == 128 ? 2048 : s.tpr <= 256 ? 1024 : s.tpr <= 512 ? 512 : 256;
     const int64_t blocks = (rows + rpb - 1) / rpb;
     return (int)(blocks < most ? blocks : most);
 }
