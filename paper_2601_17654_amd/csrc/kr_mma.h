@@ -111,6 +111,24 @@ __device__ inline void copy_to_lds(i32x4 rsrc, uint32_t off, const char *lds)
                  "buffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(off), "s"(rsrc)
                  : "memory", "m0");
 }
+// The same in two parts, with a matrix instruction between them and nothing else that uses m0: a
+// wave issues three instructions in a matrix instruction's time, and these are four.
+__device__ inline void copy_ready(uint32_t off, const char *lds)
+{
+    const uint32_t to = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char *)lds;
+    asm volatile("s_mov_b32 m0, %0" ::"s"(to), "v"(off) : "m0");
+}
+__device__ inline void copy_go(uint32_t off, const i32x4 &rsrc)
+{
+    asm volatile("buffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(off), "s"(rsrc) : "memory");
+}
+
+// Scalar work on x is neither moved up past this point nor down.
+template <typename T>
+__device__ __attribute__((always_inline)) inline void here(T &x)
+{
+    asm volatile("" : "+s"(x));
+}
 
 // A tile of ROWS m (or n) x kStep bytes of k, copied by NW waves.  Copy i of the tile fills
 // bytes [1024 i, 1024 i + 1024) of its LDS; wave w makes copies w * N .. w * N + N - 1.
@@ -127,6 +145,8 @@ struct TileLoader {
     const char *base;   // of the tile's first row (column)
     int64_t left;       // bytes of the operand from there
     int64_t step;       // bytes from one k step to the next
+    uint64_t at;        // the step it aims at, and the bytes of the operand from there
+    int64_t rest;
 
     // first: the tile's first m; map: the m, from there, of a row of LDS (runs of 8 rows of LDS,
     // 16 where crossed, are runs of m).
@@ -158,28 +178,50 @@ struct TileLoader {
         }
     }
 
-    // The operand from step t on, `by` bytes from the one that init() took (another of its
-    // shape), as a buffer; an empty one where there is no such step.
-    __device__ i32x4 buffer(int t, int64_t by, bool there) const
+    // The operand from step t on, `by` bytes from the one that init() took (another of its shape).
+    __device__ void aim(int t, int64_t by)
     {
-        const int64_t rest = there ? left - t * step : 0;
-        const uint32_t records = rest <= 0 ? 0u : rest > kBufferMost ? kBufferMost : (uint32_t)rest;
-        const uint64_t at = (uint64_t)(base + by + t * step);
-        return i32x4{(int)at, (int)(at >> 32) & 0xFFFF, (int)records, 0x00020000};
+        at = (uint64_t)(base + by + t * step);
+        rest = left - t * step;
+    }
+    // The step after, or the first of the operand `by` bytes away.
+    __device__ void next_at(bool first, int64_t by)
+    {
+        here(at);
+        at = first ? (uint64_t)(base + by) : at + step;
+        here(at);
+    }
+    __device__ void next_rest(bool first)
+    {
+        here(rest);
+        rest = first ? left : rest - step;
+        here(rest);
+    }
+    // What it aims at as a buffer; an empty one where there is no such step.
+    __device__ i32x4 buffer(bool there) const
+    {
+        int high = (int)(rest >> 32);
+        here(high);
+        const uint32_t low = min((uint32_t)rest, kBufferMost);
+        const uint32_t records = high == 0 ? low : high < 0 ? 0u : kBufferMost;
+        i32x4 x{(int)at, (int)(at >> 32) & 0xFFFF, there ? (int)records : 0, 0x00020000};
+        here(x);
+        return x;
     }
     // Says how many bytes of k there are from the step's start (plain).
-    __device__ void bound(int64_t k_left)
+    __device__ void bound(int k_left)
     {
         if (!CROSSED) {
-            const int most = k_left < kStep ? (int)k_left : kStep;
+            const int most = min(k_left, kStep);
 #pragma unroll
             for (int j = 0; j < 2; ++j) past[j] = chunk[j] < most ? 0 : kNowhere;
         }
     }
-    // Starts the wave's copy j of a step.
-    __device__ void copy(int j, const i32x4 &rsrc, const char *lds, int wave) const
+    // What the wave's copy j of a step fetches, and where to.
+    __device__ uint32_t from(int j) const { return CROSSED ? off[j] : off[j] | past[j & 1]; }
+    __device__ const char *to(int j, const char *lds, int wave) const
     {
-        copy_to_lds(rsrc, CROSSED ? off[j] : off[j] | past[j & 1], lds + (wave * N + j) * 1024);
+        return lds + (wave * N + j) * 1024;
     }
 };
 
@@ -393,23 +435,24 @@ __device__ __attribute__((always_inline)) inline void each(std::integer_sequence
 // The 256 x 256 form has one wave per SIMD: its 128 x 128 sums halve the reads of LDS against
 // 8 waves' 128 x 64.  A CU takes 16 cycles, one matrix instruction, to address a copy, and 8 to
 // read 1 KiB of LDS; its four waves start theirs at the same time, and what they wait for each
-// other the matrix cores wait too.  So reads are two instructions apart there and copies four.
-// 8192 x 8192 x 4096 in bfloat16: 401 us (1,370 TFLOP/s); 8-bit integers, 8192^3: 427 us (2,570
+// other the matrix cores wait too.  So reads are two instructions apart there and copies five.
+// 8192 x 8192 x 4096 in bfloat16: 394 us (1,394 TFLOP/s); 8-bit integers, 8192^3: 408 us (2,700
 // TOP/s).  What bounds it is power: the clock falls from 2.4 to 2.0 GHz on random values (zeros
-// take 350 us).
+// take 335 us).
 // The 128 x 128 form, for outputs that do not fill the chip with large tiles, has two blocks a CU
-// and is bound by its requests to the L2, twice as many bytes for the same products: 0.8 us a step
-// of both (1.05 with steps of 64 bytes, more of them on their way but half a line each).
+// and is bound by LDS, whose reads and whose copies take 512 cycles each a block's step, the
+// matrix cores 512: 0.47 us a step, whether a CU has one block or two (0.5 with steps of 64 bytes,
+// half a line each; the same with four steps' tiles in LDS and one block a CU).
 template <int BLOCK>
 struct Timing;  // apart: of reads;  copies(x): those started before instruction x
 template <>
 struct Timing<64> {
     static constexpr int free = 40, next = 96, apart = 2;
-    static constexpr int copies(int x) { return x - free < 64 ? (x - free + 3) / 4 : 16; }
+    static constexpr int copies(int x) { return x - free < 80 ? (x - free + 4) / 5 : 16; }
 };
 template <>
 struct Timing<16> {
-    static constexpr int free = 12, next = 24, apart = 1;
+    static constexpr int free = 14, next = 24, apart = 1;
     static constexpr int copies(int x) { return x - free < 16 ? (x - free + 1) / 2 : 8; }
 };
 
@@ -459,20 +502,33 @@ __global__ __launch_bounds__(WM *WN * 64) void mma_kernel(MmaArgs a, Out out)
     else
         lb.init(a.b[0], n0, wave, lane, MapSame());
     const int64_t to_second_a = a.a[1].p - a.a[0].p, to_second_b = a.b[1].p - a.b[0].p;
+    // The step that copies are of goes one on in parts, which stand between matrix instructions
+    // (in one piece at a step's head its 55 scalar instructions were 8 % of the step).
+    int step = begin, k_left = 0;
     i32x4 rsrc_a, rsrc_b;
-    auto aim = [&](int s) {  // the copies at step s
-        const bool second = s >= a.steps;
-        const int t = second ? s - a.steps : s;
-        la.bound(a.k_bytes - (int64_t)t * kStep);
-        lb.bound(a.k_bytes - (int64_t)t * kStep);
-        rsrc_a = la.buffer(t, second ? to_second_a : 0, s < end);
-        rsrc_b = lb.buffer(t, second ? to_second_b : 0, s < end);
+    constexpr int PARTS = 8;
+    auto aim = [&](int part) __attribute__((always_inline)) {
+        const bool first = step == a.steps;  // of the second pair
+        if (part == 0) {
+            ++step;
+            here(step);
+        }
+        if (part == 1) la.next_at(first, to_second_a);
+        if (part == 2) la.next_rest(first);
+        if (part == 3) rsrc_a = la.buffer(step < end);
+        if (part == 4) lb.next_at(first, to_second_b);
+        if (part == 5) lb.next_rest(first);
+        if (part == 6) rsrc_b = lb.buffer(step < end);
+        if (part == 7 && !(A_CROSSED && B_CROSSED)) {
+            here(k_left);
+            k_left = first ? (int)a.k_bytes : k_left - kStep;
+            la.bound(k_left);
+            lb.bound(k_left);
+        }
     };
-    auto copy = [&](int j, const char *to) {
-        if (j < LoadA::N)
-            la.copy(j, rsrc_a, to, wave);
-        else
-            lb.copy(j - LoadA::N, rsrc_b, to + BM * kStep, wave);
+    auto from = [&](int j) { return j < LoadA::N ? la.from(j) : lb.from(j - LoadA::N); };
+    auto to = [&](int j, const char *at) {
+        return j < LoadA::N ? la.to(j, at, wave) : lb.to(j - LoadA::N, at + BM * kStep, wave);
     };
 
     i32x4 fa[2][TM], fb[2][TN];  // halves of a step
@@ -485,11 +541,23 @@ __global__ __launch_bounds__(WM *WN * 64) void mma_kernel(MmaArgs a, Out out)
 
     // Past the last step the copies are of an empty buffer, zeros that nothing uses: every step
     // is the same, and the waits too.
+    const bool second = begin >= a.steps;
+    const int t = second ? begin - a.steps : begin;
+    la.aim(t, second ? to_second_a : 0);
+    lb.aim(t, second ? to_second_b : 0);
+    if (!(A_CROSSED && B_CROSSED)) k_left = (int)a.k_bytes - t * kStep;
+    la.bound(k_left);
+    lb.bound(k_left);
+    rsrc_a = la.buffer(begin < end);
+    rsrc_b = lb.buffer(begin < end);
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
-        aim(begin + k);
 #pragma unroll
-        for (int j = 0; j < COPIES; ++j) copy(j, lds[k]);
+        for (int j = 0; j < COPIES; ++j) copy_to_lds(j < LoadA::N ? rsrc_a : rsrc_b, from(j), to(j, lds[k]));
+        if (k == 0) {
+#pragma unroll
+            for (int p = 0; p < PARTS; ++p) aim(p);
+        }
     }
     arrived<COPIES>();
 #pragma unroll
@@ -498,15 +566,20 @@ __global__ __launch_bounds__(WM *WN * 64) void mma_kernel(MmaArgs a, Out out)
     for (int s = begin; s < end; ++s) {
         const int buf = (s - begin) & 1;
         const char *at = lds[buf], *next = lds[buf ^ 1];
-        aim(s + 2);
+        uint32_t off = 0;
         each(Count<2 * BLOCK>(), [&](auto at_x) __attribute__((always_inline)) {
             constexpr int x = decltype(at_x)::value;
             if (x % T::apart == 0 && x / T::apart < READS) read(x / T::apart, at, 1);
             if (x == T::free) read_done();
             if (x == T::next) arrived<T::copies(T::next)>();
-            if (x >= T::free) {
 #pragma unroll
-                for (int j = T::copies(x); j < T::copies(x + 1); ++j) copy(j, at);
+            for (int p = 0; p < PARTS; ++p)
+                if (p * T::free / PARTS == x) aim(p);
+            if (x >= T::free && T::copies(x + 1) > T::copies(x))
+                copy_go(off, T::copies(x) < LoadA::N ? rsrc_a : rsrc_b);
+            if (x + 1 >= T::free && T::copies(x + 2) > T::copies(x + 1)) {
+                off = from(T::copies(x + 1));
+                copy_ready(off, to(T::copies(x + 1), at));
             }
             if (x >= T::next && (x - T::next) % T::apart == 0 && (x - T::next) / T::apart < READS)
                 read((x - T::next) / T::apart, next, 0);

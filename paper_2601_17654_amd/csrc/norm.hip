@@ -9,8 +9,8 @@
 // All arithmetic is in 32 bits; stored values are rounded once.
 //
 // Bound by memory.  Eight elements a thread: more waves, each with little to wait for (with 16 the
-// forward pass below takes 99 us).  16384 x 4096 in bfloat16: forward 94 us (5.7 TB/s of its 537 MB), backward
-// 102 us (5.2 TB/s); 8192 x 8192 in float16 to bytes 88 us (5.3 TB/s).
+// forward pass below takes 99 us).  16384 x 4096 in bfloat16: forward 94 us (5.7 TB/s of its
+// 537 MB), backward 102 us (5.2 TB/s); 8192 x 8192 in float16 to bytes 88 us (5.3 TB/s).
 #include "kr_block.h"
 
 namespace kr {
