@@ -609,9 +609,12 @@ size_t kr_gated_projection_workspace(const kr_gated *g);
  * again).  With dg = dh * u * act'(g) and du = dh * act(g),
  *   dx = dg Wg + du Wu,  dwg = dg^T x,  dwu = du^T x
  * dg and du are rounded to the type between the products (they are the products' operands), in
- * the workspace; in KR_F16 what leaves its range is infinite or 0 there.  dx, dwg and dwu are
- * rounded once and overwritten; without rows the weight gradients are 0.  No output may
- * overlap an input.
+ * the workspace.  In KR_F16 dh is first taken times a power of two that brings its largest
+ * finite magnitude D to [2^-2, 2^7) (1 where it is there), and the sums times its inverse, so
+ * that small gradients keep their bits.  Of dg and du, what is above 2^9 D is infinite and what
+ * is below 2^-21 D loses bits where that magnitude is at the range's upper end; 2^17 D and
+ * 2^-12 D at its lower.  dx, dwg and dwu are rounded once and overwritten; without rows the
+ * weight gradients are 0.  No output may overlap an input.
  */
 kr_status kr_gated_projection_backward(const kr_gated *g, const void *dh, int64_t ldh, void *dx,
                                        int64_t lddx, void *dwg, int64_t lddg, void *dwu,

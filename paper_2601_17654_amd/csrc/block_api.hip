@@ -234,6 +234,8 @@ kr_status gated_back_run(const kr_gated *g, GatedBackArgs &b, Carve &c, hipStrea
     b.width = g->width;
     b.n_pad = (g->hidden + 7) / 8 * 8;
     b.d = c.take(g->rows * 4 * b.n_pad);
+    const int64_t tops = (int64_t)gated_back_tops(g->type);
+    b.tops = tops ? c.take(tops) : nullptr;
     b.f.part = c.take((int64_t)gated_back_part(b.f.m, b.f.n, b.n_pad, b.width, b.f.k_bytes));
     if (!b.dwg) return KR_OK;
     const hipError_t e = l.fill(st);

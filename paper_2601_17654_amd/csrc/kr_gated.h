@@ -40,10 +40,12 @@ struct GatedBackArgs {
     int64_t ldh;
     char *d;                  // [m][2 n_pad]: dg, du, each padded with zeros to n_pad
     int64_t n_pad;
+    char *tops;               // gated_back_tops bytes, or null where that is 0
     void *dx, *dwg, *dwu;
     int64_t lddx, lddg, lddu;
 };
 size_t gated_back_part(int64_t m, int64_t n, int64_t n_pad, int64_t width, int64_t k_bytes);
+size_t gated_back_tops(int type);
 hipError_t launch_gated_back(const GatedBackArgs &a, hipStream_t st);
 
 // bytes.hip

@@ -411,7 +411,8 @@ __device__ inline void put_tile(E, const MmaArgs &a, const Out &out,
 // One product kernel.  Out says what happens to the sums:
 //   PLANES         1, or 2: B's tile is half of b[0], half of b[1] (same rows), two sums
 //   columns(n)     columns to put, n or more
-//   Mine mine(n)   what a lane needs for its columns n .. n + 7 in every row
+//   Mine mine(n)   what a lane needs for its columns n .. n + 7 in every row (called by whole
+//                  waves, but in the form of few rows)
 //   Fetched fetch(there, m, n)   what it reads for them of row m, asked for ahead
 //   put(m, n, v0, v1, mine, fetched)   eight outputs from n on of row m, from the first and second
 //                                      plane
@@ -602,9 +603,10 @@ __global__ __launch_bounds__(256) void mma_join_kernel(MmaArgs a, Out out)
     typedef typename Mma<E>::Sum Sum;
     const int per = (out.columns(a.n) + 7) / 8;
     const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (id >= (int64_t)a.m * per) return;
     const int64_t m = id / per;
     const int n = (int)(id - m * per) * 8;
+    const typename Out::Mine mine = out.mine(n);  // by every lane of the wave
+    if (id >= (int64_t)a.m * per) return;
     Sum v[2][8] = {};
     // four splits' loads at a time
     for (int s = 0; s < a.splits; s += 4) {
@@ -626,7 +628,7 @@ __global__ __launch_bounds__(256) void mma_join_kernel(MmaArgs a, Out out)
 #pragma unroll
                 for (int e = 0; e < 8; ++e) v[p][e] += q[u][p][e / 4].v[e % 4];
     }
-    out.put(m, n, v[0], v[Out::PLANES - 1], out.mine(n), out.fetch(true, m, n));
+    out.put(m, n, v[0], v[Out::PLANES - 1], mine, out.fetch(true, m, n));
 }
 
 // How a product is cut into tiles.
