@@ -720,6 +720,11 @@ def launch_timing_frontier(kind1, kind2, ops, p_static: float, kmax: int, out_ca
 # are rows.  Outputs and workspaces are allocated on the current stream: calls on several
 # streams may overlap.  A single token's call takes about as long here as on the device, so
 # these functions hand over plain integers and ask for each thing once.
+#
+# While torch records a graph and an input requires a gradient, add_rms_norm and gated_projection
+# are nodes of it, whose backward passes are add_rms_norm_backward and
+# gated_projection_backward.  The forms in 8-bit integers have no gradient and refuse such
+# inputs.  The backward functions themselves return plain tensors: they are not differentiated again.
 
 _TYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
@@ -822,9 +827,50 @@ def _norm_inputs(x, weight, residual):
     return t, dev, xr, n, ldx, width, w, rr, ldr
 
 
+def _tracked(*tensors) -> bool:
+    """Whether a graph is recorded that one of these belongs to."""
+    if torch.is_grad_enabled():
+        for t in tensors:
+            if getattr(t, "requires_grad", False):
+                return True
+    return False
+
+
+def _no_gradient(call: str, *tensors) -> None:
+    if _tracked(*tensors):
+        raise ValueError("%s has no gradient: call it under torch.no_grad() or on detached tensors"
+                         % call)
+
+
+class _AddRmsNorm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, residual, eps):
+        r = add_rms_norm(x, weight, residual, eps)
+        ctx.set_materialize_grads(False)
+        ctx.mark_non_differentiable(r.rstd)
+        ctx.save_for_backward(r.sum, weight, r.rstd)
+        # without a residual the sum is x, whose gradient by that path is torch's own matter
+        return (r.out, r.rstd) if residual is None else (r.out, r.rstd, r.sum)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dout, _, dsum=None):
+        total, weight, rstd = ctx.saved_tensors
+        if dout is None:  # only the sum was used
+            dx, dw = dsum, None
+        else:
+            dx, dw = add_rms_norm_backward(dout, total, weight, rstd, dsum)
+            dw = dw.to(weight.dtype).reshape(weight.shape)
+        need = ctx.needs_input_grad
+        return dx if need[0] else None, dw if need[1] else None, dx if need[2] else None, None
+
+
 def add_rms_norm(x, weight, residual=None, eps: float = 1e-6) -> Normed:
     """s = x + residual and s * rstd * weight, rstd = 1 / sqrt(mean(s^2) + eps) over the last
-    dimension (kr_add_rms_norm)."""
+    dimension (kr_add_rms_norm).  out and sum have gradients, rstd has none."""
+    if _tracked(x, weight, residual):
+        out, rstd, *total = _AddRmsNorm.apply(x, weight, residual, eps)
+        return Normed(out, total[0] if total else x, rstd)
     t, dev, xr, n, ldx, width, w, rr, ldr = _norm_inputs(x, weight, residual)
     out = _new_like(x)
     total = x if rr is None else _new_like(x)
@@ -839,7 +885,8 @@ def add_rms_norm(x, weight, residual=None, eps: float = 1e-6) -> Normed:
 
 def add_rms_norm_bytes(x, weight, residual=None, eps: float = 1e-6) -> NormedBytes:
     """add_rms_norm with the norm held in 8-bit integers and a scale for each row: q * scale
-    (kr_add_rms_norm_bytes)."""
+    (kr_add_rms_norm_bytes).  It has no gradient."""
+    _no_gradient("add_rms_norm_bytes", x, weight, residual)
     t, dev, xr, n, ldx, width, w, rr, ldr = _norm_inputs(x, weight, residual)
     q = _new(x.shape, torch.int8)
     total = x if rr is None else _new_like(x)
@@ -884,7 +931,8 @@ def add_rms_norm_backward(dout, sum, weight, rstd, dsum=None):
 
 def byte_matmul(a, sa, b, sb, dtype=torch.bfloat16) -> torch.Tensor:
     """sa * sb * (a b^T) of int8 rows a [..., k] and b [n][k], a float32 scale for each row of
-    either; the result, [..., n], in dtype (kr_byte_matmul)."""
+    either; the result, [..., n], in dtype (kr_byte_matmul).  It has no gradient."""
+    _no_gradient("byte_matmul", sa, sb)
     if dtype not in _TYPES:
         raise TypeError("dtype must be %s, got %s" % (" or ".join(map(str, _TYPES)), dtype))
     _type(a, "a", (torch.int8,))
@@ -929,9 +977,25 @@ def _gated(x, wg, wu, act):
     return g, dev, (xr, gr, ur)
 
 
+class _GatedProjection(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, wg, wu, act):
+        ctx.save_for_backward(x, wg, wu)
+        ctx.act = act
+        return gated_projection(x, wg, wu, act)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dh):
+        grads = gated_projection_backward(dh, *ctx.saved_tensors, act=ctx.act)
+        return (*(g if need else None for g, need in zip(grads, ctx.needs_input_grad)), None)
+
+
 def gated_projection(x, wg, wu, act: str = "silu") -> torch.Tensor:
     """act(x wg^T) * (x wu^T) of x [..., width] and wg, wu [hidden][width], act "silu" or
-    "gelu" (kr_gated_projection)."""
+    "gelu" (kr_gated_projection).  Its gradient reaches all three."""
+    if _tracked(x, wg, wu):
+        return _GatedProjection.apply(x, wg, wu, act)
     g, dev, keep = _gated(x, wg, wu, act)
     out = _new(x.shape[:-1] + (g.hidden,), x.dtype)
     p = ctypes.byref(g)
