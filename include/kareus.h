@@ -566,8 +566,9 @@ size_t kr_add_rms_norm_backward_workspace(int32_t type, int64_t rows, int64_t wi
  *   b [n][k], sb [n]   channels: a weight matrix as its rows of inputs
  *   type               of out
  * m >= 0, n >= 1, k >= 1; KR_EUNSUPPORTED for m >= 2^31, n > 2^27, k > 131071 or an output of
- * more than 2^23 tiles of 128 x 64.  Strides are in elements; out overlaps no input.  The workspace (16-byte aligned) depends on sizes, strides and addresses; 0:
- * none needed, or an invalid argument.
+ * more than 2^23 tiles of 128 x 64.  Strides are in elements; out overlaps no input.  The
+ * workspace (16-byte aligned) depends on sizes, strides and addresses; 0: none needed, or an
+ * invalid argument.
  */
 typedef struct kr_bytes {
     int64_t m, n, k;
@@ -588,8 +589,9 @@ size_t kr_byte_matmul_workspace(const kr_bytes *p);
  *   wg, wu      [hidden][width]
  *   out         [rows][hidden]
  * rows >= 0, width >= 1, hidden >= 1; KR_EUNSUPPORTED for rows >= 2^31, more than 2^20 columns
- * or matrices of more than 2^23 tiles of 128 x 64.  out overlaps no input.  The workspace (16-byte aligned) depends on sizes, strides and addresses; 0: none
- * needed, or an invalid argument.
+ * or matrices of more than 2^23 tiles of 128 x 64 (x and out; backward, dwg and dwu together
+ * too).  out overlaps no input.  The workspace (16-byte aligned) depends on sizes, strides and
+ * addresses; 0: none needed, or an invalid argument.
  */
 #define KR_SILU 0
 #define KR_GELU 1

@@ -161,6 +161,12 @@ bool gated_fits(const kr_gated *g)
            tiles_fit(g->rows, g->hidden > g->width ? g->hidden : g->width);
 }
 
+// The backward pass puts both weights' gradients in one product besides.
+bool gated_back_fits(const kr_gated *g)
+{
+    return gated_fits(g) && tiles_fit(2 * ((g->hidden + 7) / 8 * 8), g->width);
+}
+
 struct GatedLaid {
     Laid x, wg, wu;
     // one_ld: both weights' rows the same distance apart (one sum over both takes them)
@@ -308,7 +314,7 @@ extern "C" kr_status kr_gated_projection(const kr_gated *g, void *out, int64_t l
 
 extern "C" size_t kr_gated_projection_backward_workspace(const kr_gated *g)
 {
-    if (!gated_ok(g) || !gated_fits(g)) return 0;
+    if (!gated_ok(g) || !gated_back_fits(g)) return 0;
     Carve c{nullptr};
     GatedBackArgs b{};
     gated_back_run(g, b, c, nullptr);
@@ -321,7 +327,7 @@ extern "C" kr_status kr_gated_projection_backward(const kr_gated *g, const void 
                                                   size_t ws_bytes, void *stream)
 {
     if (!gated_ok(g)) return KR_EINVAL;
-    if (!gated_fits(g)) return KR_EUNSUPPORTED;
+    if (!gated_back_fits(g)) return KR_EUNSUPPORTED;
     if ((g->rows > 0 && (!matrix_ok(dh, ldh, g->hidden, 2) || !matrix_ok(dx, lddx, g->width, 2))) ||
         !matrix_ok(dwg, lddg, g->width, 2) || !matrix_ok(dwu, lddu, g->width, 2) || (uintptr_t)ws % 16)
         return KR_EINVAL;
