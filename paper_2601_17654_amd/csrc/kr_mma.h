@@ -70,10 +70,11 @@ __device__ inline i32x4 mma(int8_t, i32x4 a, i32x4 b, i32x4 c)
 }
 
 // The same, c += a b, with the sums kept where they are.  (Left to itself, the compiler gives the
-// result other registers than the sums had, and moves a hundred a step to make room.)  The
-// operands come from LDS, whose arrival the compiler waits for, and an instruction's sums are
-// not touched again before sums_done() but by the next on the same sums, 16 or more later: the
-// wait states that the compiler adds around the builtin are not needed.
+// result other registers than the sums had, and moves a hundred a step to make room.)  It adds no
+// wait states around these; what they need is there by the order of things: the operands come from
+// LDS, whose arrival the compiler waits for, not from a vector instruction just before, and an
+// instruction's sums are not touched again before sums_done() but by the next on the same
+// sums, 16 or more later.  tests/test_matrix_instructions.py reads both off the built library.
 __device__ inline void mma_in_place(bf16, i32x4 a, i32x4 b, f32x4 &c)
 {
     asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b));
@@ -86,8 +87,18 @@ __device__ inline void mma_in_place(int8_t, i32x4 a, i32x4 b, i32x4 &c)
 {
     asm volatile("v_mfma_i32_16x16x64_i8 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b));
 }
-// Between such instructions and any other use of their sums.
-__device__ inline void sums_done() { asm volatile("s_nop 15\n\ts_nop 15" ::: "memory"); }
+// Between such instructions and any other use of their sums, which are tied to its middle: no write of
+// them can come to stand after it, and no read before it, with 16 states on either side (11 are needed).
+template <typename Acc, int TM, int TN>
+__device__ __attribute__((always_inline)) inline void sums_done(Acc (&acc)[TM][TN])
+{
+    asm volatile("s_nop 15" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j) asm volatile("" : "+a"(acc[i][j]));
+    asm volatile("s_nop 15" ::: "memory");
+}
 
 // One operand as the host describes it: `rows` rows (m, or k where crossed) of `bytes` bytes,
 // `ld` bytes apart.  p and ld are multiples of 16 bytes, and so is `bytes` (crossed) or it is
@@ -101,26 +112,27 @@ struct Operand {
 // Starts the copy of 16 bytes a lane to LDS, from byte `off` of a buffer; 64 lanes side by side.
 // Written out because the compiler, where it knows of such a copy, waits for all of them before
 // any read of LDS; here the waits are arrived() below.  There is no output register, and the
-// copies' LDS is read only after such a wait.  The idle state stands between m0 and its use.  The
-// buffer's registers come from scalar arithmetic (a vector instruction's result would need five).
-__device__ inline void copy_to_lds(i32x4 rsrc, uint32_t off, const char *lds)
+// copies' LDS is read only after such a wait.  The buffer's registers come from scalar arithmetic
+// (a vector instruction's result would need five states).  In two parts, with a matrix
+// instruction between them: a wave issues three instructions in a matrix instruction's time, and
+// these are four.  m0 is handed on as a value, so that nothing else can come to stand in it.
+__device__ inline uint32_t copy_ready(uint32_t off, const char *lds)
 {
     const uint32_t to = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char *)lds;
-    asm volatile("s_mov_b32 m0, %0\n\t"
-                 "s_nop 0\n\t"
-                 "buffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(off), "s"(rsrc)
-                 : "memory", "m0");
+    uint32_t m0;
+    asm volatile("s_mov_b32 %0, %1" : "={m0}"(m0) : "s"(to), "v"(off));
+    return m0;
 }
-// The same in two parts, with a matrix instruction between them and nothing else that uses m0: a
-// wave issues three instructions in a matrix instruction's time, and these are four.
-__device__ inline void copy_ready(uint32_t off, const char *lds)
+__device__ inline void copy_go(uint32_t off, const i32x4 &rsrc, uint32_t m0)
 {
-    const uint32_t to = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char *)lds;
-    asm volatile("s_mov_b32 m0, %0" ::"s"(to), "v"(off) : "m0");
+    asm volatile("buffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(off), "s"(rsrc), "{m0}"(m0) : "memory");
 }
-__device__ inline void copy_go(uint32_t off, const i32x4 &rsrc)
+// At once, with the idle state that stands between m0 and its use.
+__device__ inline void copy_to_lds(const i32x4 &rsrc, uint32_t off, const char *lds)
 {
-    asm volatile("buffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(off), "s"(rsrc) : "memory");
+    const uint32_t m0 = copy_ready(off, lds);
+    asm volatile("s_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(off), "s"(rsrc), "{m0}"(m0)
+                 : "memory");
 }
 
 // Scalar work on x is neither moved up past this point nor down.
@@ -335,6 +347,15 @@ __device__ inline void arrived()
 // Waits for the wave's reads of LDS, then for the block: what was read may be overwritten.
 __device__ inline void read_done() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
+// Between the writes of a wave's LDS and reads of it by other lanes of the wave: the hardware keeps a
+// wave's own order, this keeps the compiler's (no instruction comes of it).
+__device__ inline void wave_lds()
+{
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 // A block's sums to the output, or to its split's part.  Each wave takes them through its own
 // share of the LDS, 64 rows at a time: out of the matrix layout into rows of 8 neighbouring
 // columns a lane, so that whole lines are written, in a loop that is short in code (unrolled over
@@ -398,6 +419,7 @@ __device__ inline void put_tile(E, const MmaArgs &a, const Out &out,
                 const int row = i * 16 + lane % 16, c = j * 4 + lane / 16;
                 *(Acc *)(own + row * STRIP * 4 + ((c ^ row % 16) << 4)) = acc[p * 4 + i][j];
             }
+        wave_lds();
         if (ASKS) {
 #pragma unroll
             for (int it = 0; it < LANES; ++it) put(p, it, asked[p][it]);
@@ -405,6 +427,7 @@ __device__ inline void put_tile(E, const MmaArgs &a, const Out &out,
 #pragma unroll 4
             for (int it = 0; it < LANES; ++it) put(p, it, typename Out::Fetched());
         }
+        wave_lds();
     }
 }
 
@@ -563,11 +586,11 @@ __global__ __launch_bounds__(WM *WN * 64) void mma_kernel(MmaArgs a, Out out)
     arrived<COPIES>();
 #pragma unroll
     for (int j = 0; j < TM + TN; ++j) read(j, lds[0], 0);
-    sums_done();
+    sums_done(acc);
     for (int s = begin; s < end; ++s) {
         const int buf = (s - begin) & 1;
         const char *at = lds[buf], *next = lds[buf ^ 1];
-        uint32_t off = 0;
+        uint32_t off = 0, m0 = 0;
         each(Count<2 * BLOCK>(), [&](auto at_x) __attribute__((always_inline)) {
             constexpr int x = decltype(at_x)::value;
             if (x % T::apart == 0 && x / T::apart < READS) read(x / T::apart, at, 1);
@@ -577,10 +600,10 @@ __global__ __launch_bounds__(WM *WN * 64) void mma_kernel(MmaArgs a, Out out)
             for (int p = 0; p < PARTS; ++p)
                 if (p * T::free / PARTS == x) aim(p);
             if (x >= T::free && T::copies(x + 1) > T::copies(x))
-                copy_go(off, T::copies(x) < LoadA::N ? rsrc_a : rsrc_b);
+                copy_go(off, T::copies(x) < LoadA::N ? rsrc_a : rsrc_b, m0);
             if (x + 1 >= T::free && T::copies(x + 2) > T::copies(x + 1)) {
                 off = from(T::copies(x + 1));
-                copy_ready(off, to(T::copies(x + 1), at));
+                m0 = copy_ready(off, to(T::copies(x + 1), at));
             }
             if (x >= T::next && (x - T::next) % T::apart == 0 && (x - T::next) / T::apart < READS)
                 read((x - T::next) / T::apart, next, 0);
@@ -590,7 +613,7 @@ __global__ __launch_bounds__(WM *WN * 64) void mma_kernel(MmaArgs a, Out out)
             __builtin_amdgcn_sched_barrier(0);
         });
     }
-    sums_done();
+    sums_done(acc);
     read_done();
     arrived<0>();  // the tiles' LDS is free, and no copy will write to it
     put_tile<BM, BN, WM, WN>(E(), a, out, acc, lds[0], m0, n0, wave, split, lane);
