@@ -292,36 +292,6 @@ hipError_t backward(const GatedBackArgs &a, hipStream_t st)
 
 }  // namespace
 
-// The cheaper of the two tile sizes, and of up to 16 splits of the sum, by an estimate in
-// microseconds.  256 x 256: 1.3 a step and 9 for what surrounds them, one tile a CU at a time.
-// 128 x 128: 0.94 and 4, two a CU, so that half a round is one each.  A split adds its partial
-// sums, written and read at 4 TB/s, and a launch.  Measured, bfloat16, two planes (large / small):
-//   4096 x 4096 x 2048   118 / 135 us        4096 x 2176 x 4096   173 / 141 us
-//   1024 x 14336 x 4096  185 / 213 us        2048 x 2048 x 512     21 / 14 us
-//   700 x 8192 x 8192    163 / 190 us        3000 x 6000 x 1500   144 / 138 us
-MmaPlan mma_plan(int64_t m, int64_t n, int planes, int steps)
-{
-    MmaPlan best{};
-    double least = 0;
-    for (const bool large : {true, false}) {
-        const int bm = large ? 256 : 128, bn = bm / planes;
-        const int64_t tm = (m + bm - 1) / bm, tn = (n + bn - 1) / bn;
-        for (int s = 1; s <= 16 && (s == 1 || (steps + s - 1) / s >= 4); ++s) {
-            const int per = steps > 0 ? (steps + s - 1) / s : 1;
-            const int splits = steps > 0 ? (steps + per - 1) / per : 1;
-            if (splits != s) continue;
-            const int64_t rounds = (tm * tn * s + 255) / 256;
-            const double part = s > 1 ? 4.0 * s * planes * m * n : 0;
-            const double cost = rounds * (large ? 1.3 * per + 9 : 0.47 * per + 2) +
-                                (s > 1 ? 4 + 2 * part / 4e6 : 0);
-            if (best.tiles_m && cost >= least) continue;
-            least = cost;
-            best = {large, (int)tm, (int)tn, s, per, (int64_t)part};
-        }
-    }
-    return best;
-}
-
 size_t gated_part(int64_t m, int64_t n, int64_t k_bytes)
 {
     return (size_t)mma_plan(m, n, 2, steps_of(k_bytes)).part_bytes;

@@ -28,6 +28,7 @@
 #include <utility>
 
 #include "kr_block.h"
+#include "kr_plan.h"
 
 namespace kr {
 
@@ -653,14 +654,6 @@ __global__ __launch_bounds__(256) void mma_join_kernel(MmaArgs a, Out out)
     }
     out.put(m, n, v[0], v[Out::PLANES - 1], mine, out.fetch(true, m, n));
 }
-
-// How a product is cut into tiles.
-struct MmaPlan {
-    bool large;   // 256 x 256 tiles, else 128 x 128
-    int tiles_m, tiles_n, splits, per_split;
-    int64_t part_bytes;
-};
-MmaPlan mma_plan(int64_t m, int64_t n, int planes, int steps);
 
 template <typename E, bool A_CROSSED, bool B_CROSSED, typename Out>
 hipError_t launch_mma(MmaArgs a, const MmaPlan &p, const Out &out, hipStream_t st)
