@@ -779,8 +779,12 @@ def _vector(x: torch.Tensor, n: int, dtype, name: str, dev: int) -> torch.Tensor
 
 
 def _like(x: torch.Tensor, other: torch.Tensor, name: str, of: str) -> None:
-    if not isinstance(x, torch.Tensor) or x.dtype != other.dtype or x.shape != other.shape:
-        raise ValueError("%s must be like %s: %s %s" % (name, of, other.dtype, tuple(other.shape)))
+    if not isinstance(x, torch.Tensor) or x.dtype != other.dtype:
+        raise TypeError("%s must be a tensor of %s like %s, got %s"
+                        % (name, other.dtype, of, getattr(x, "dtype", type(x).__name__)))
+    if x.shape != other.shape:
+        raise ValueError("%s must be like %s: %s, got %s" % (name, of, tuple(other.shape),
+                                                             tuple(x.shape)))
 
 
 def _new(shape, dtype) -> torch.Tensor:
