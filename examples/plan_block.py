@@ -3,8 +3,8 @@
 Runs the compute kernels of a block's feed-forward half -- forward (norm with the residual's
 addition, gated projection), backward (their gradients) and the forward form in 8-bit integers
 (norm held in bytes, byte product) -- times each, expands the times to the planner's tables and
-plans: the time-energy frontier of the step and the schedule of its fastest and its cheapest
-point.
+plans two steps: training (forward and backward) and a forward step in 8 bits.  For either it
+prints the time-energy frontier's size and the schedule of its fastest and its cheapest point.
 
     python examples/plan_block.py [--rows 8192] [--width 4096] [--hidden 14336] [--layers 16]
 
@@ -87,14 +87,15 @@ def run_block(rows, width, hidden, repeats=10):
 
 # The block's partitions: kernels that run beside one collective each.
 PARTITIONS = (("norm", "gated"), ("gated_back", "norm_back"), ("norm_bytes", "bytes"))
+TRAINING, BYTES_FORWARD = PARTITIONS[:2], PARTITIONS[2:]  # those of one step
 
 
-def tables(times, layers, rows, width):
-    """The planner's space and tables of `layers` blocks."""
-    space = I.Space(n_parts=len(PARTITIONS) * layers, n_kernels=2, n_comm=1, n_pos=3,
+def tables(times, layers, rows, width, partitions=PARTITIONS):
+    """The planner's space and tables of `layers` blocks of such partitions."""
+    space = I.Space(n_parts=len(partitions) * layers, n_kernels=2, n_comm=1, n_pos=3,
                     sm_counts=tuple(range(8, 65, 8)), total_sms=UNITS,
                     freqs_mhz=tuple(float(x) for x in np.linspace(1200.0, 2400.0, 25)))
-    t0, per_byte = np.array([[times[k] for k in p] for p in PARTITIONS] * layers).transpose(2, 0, 1)
+    t0, per_byte = np.array([[times[k] for k in p] for p in partitions] * layers).transpose(2, 0, 1)
     share = per_byte / (per_byte + BALANCE)   # of the cost that is operations
     P, N = t0.shape
     ones = np.ones((P, N))
@@ -131,17 +132,20 @@ def main(argv=None):
     times, _ = run_block(a.rows, a.width, a.hidden)
     for name, (s, per_byte) in times.items():
         print("%-11s %9.1f us   %7.1f operations a byte" % (name, s * 1e6, per_byte))
-    space, tabs = tables(times, a.layers, a.rows, a.width)
-    T, E, sched = plan(space, tabs)
-    print("%d frontier points" % len(T))
-    for what, i in (("fastest", int(np.argmin(T))), ("cheapest", int(np.argmin(E)))):
-        print("%-8s %.3f ms  %.3f J" % (what, T[i] * 1e3, E[i]))
-        for p, kernels in enumerate(PARTITIONS):
-            f, pos, sm = sched[i, p]
-            print("   %-24s %4.0f MHz, %2d units to the collective, launched %s"
-                  % (" + ".join(kernels), space.freqs_mhz[f], space.sm_counts[sm],
-                     "after both" if pos == 2 else "with " + kernels[pos]))
-    return T, E, sched
+    plans = []
+    for name, partitions in (("training step", TRAINING), ("forward step in 8 bits", BYTES_FORWARD)):
+        space, tabs = tables(times, a.layers, a.rows, a.width, partitions)
+        T, E, sched = plan(space, tabs)
+        plans.append((T, E, sched))
+        print("%s: %d frontier points" % (name, len(T)))
+        for what, i in (("fastest", int(np.argmin(T))), ("cheapest", int(np.argmin(E)))):
+            print("%-8s %.3f ms  %.3f J" % (what, T[i] * 1e3, E[i]))
+            for p, kernels in enumerate(partitions):
+                f, pos, sm = sched[i, p]
+                print("   %-24s %4.0f MHz, %2d units to the collective, launched %s"
+                      % (" + ".join(kernels), space.freqs_mhz[f], space.sm_counts[sm],
+                         "after both" if pos == 2 else "with " + kernels[pos]))
+    return plans[0]
 
 
 if __name__ == "__main__":
