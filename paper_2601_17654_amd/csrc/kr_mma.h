@@ -20,8 +20,10 @@
 //    k % 4 + 4 (k / 8 % 4) (k / 8 % 2 where a row has 8 blocks).  The transposing read takes 4
 //    rows x 32 bytes for each group of 16 lanes, the four groups 8 rows apart: 16 different
 //    places (8, twice).
-// Whatever lies outside an operand is read as zero: rows past its end by the buffer's bound, k
-// past the end of a plain row by an offset beyond that bound.
+// What a sum takes from outside an operand is zero: rows past its end by the buffer's bound, k
+// past the end of a plain row by an offset beyond that bound.  (Columns past the end of a crossed
+// row are what lies there, the gap between rows or the next one; they end in outputs that are not
+// put.)
 #pragma once
 
 #include <type_traits>
@@ -284,7 +286,7 @@ struct MmaArgs {
     Operand a[2], b[2];  // second pair: the second half of the sum (of the first one's ld), or
                          // B's second plane
     int m, n;            // outputs
-    int64_t k_bytes;     // bytes of k in one pair (plain operands), rows of it where crossed
+    int64_t k_bytes;     // bytes of k in one pair's plain operands; not used where both are crossed
     int steps;           // k steps of one pair
     int pairs;           // 1, or 2: A0 B0 + A1 B1
     int tiles_m, tiles_n, splits, per_split;  // steps of a split
@@ -464,10 +466,13 @@ __device__ __attribute__((always_inline)) inline void each(std::integer_sequence
 // 8192 x 8192 x 4096 in bfloat16: 394 us (1,394 TFLOP/s); 8-bit integers, 8192^3: 408 us (2,700
 // TOP/s).  What bounds it is power: the clock falls from 2.4 to 2.0 GHz on random values (zeros
 // take 335 us).
-// The 128 x 128 form, for outputs that do not fill the chip with large tiles, has two blocks a CU
-// and is bound by LDS, whose reads and whose copies take 512 cycles each a block's step, the
-// matrix cores 512: 0.47 us a step, whether a CU has one block or two (0.5 with steps of 64 bytes,
-// half a line each; the same with four steps' tiles in LDS and one block a CU).
+// The 128 x 128 form, for outputs that do not fill the chip with large tiles, has two blocks a CU.
+// In a long sum a block's step takes 0.47 us, 1,120 cycles, whether a CU has one block or two (0.5
+// with steps of 64 bytes, half a line each; the same with four steps' tiles in LDS and one block a
+// CU): 512 cycles of LDS reads, 512 of what the copies bring there, 512 of the matrix cores.  In
+// short sums that is the smaller part.  1111 x 1030 -> 2731, 387 tiles of 17 steps: 28 us, of which a
+// CU's LDS is busy 8,300 cycles of 67,000 and the matrix cores 20 %; the rest is the first
+// copies' way, the outputs, and CUs with one tile that wait for those with two.
 template <int BLOCK>
 struct Timing;  // apart: of reads;  copies(x): those started before instruction x
 template <>

@@ -5,12 +5,18 @@
 //
 // Every element is read once and written once: a row stays in the registers of the threads
 // that share it (16 to 1,024 of them, 8 elements each, 16 above 8,192), so its mean costs no second
-// pass over memory.  Rows of more than 16,384 elements are read again from memory instead.
+// pass over memory.  (The gradient of rows of 8,193 to 16,384 elements, 16 a thread, needs more than
+// a thread's 128 registers: it keeps 73 of what it carries over the rows in scratch in float32, 2 or
+// 3 in the 16-bit types.)  Rows of more than 16,384 elements are read again from memory instead:
+// x and r twice, three times to bytes, in the gradient s and dout three times.
 // All arithmetic is in 32 bits; stored values are rounded once.
 //
 // Bound by memory.  Eight elements a thread: more waves, each with little to wait for (with 16 the
 // forward pass below takes 99 us).  16384 x 4096 in bfloat16: forward 94 us (5.7 TB/s of its
-// 537 MB), backward 102 us (5.2 TB/s); 8192 x 8192 in float16 to bytes 88 us (5.3 TB/s).
+// 537 MB), backward 102 us (5.2 TB/s); 8192 x 8192 in float16 to bytes 91 us (5.1 TB/s).  Wide
+// rows, forward and backward, of the bytes that they cannot do without: 4096 x 16384 in bfloat16 100
+// and 113 us (5.4, 4.8 TB/s), in float32 193 and 271 us (5.6, 4.0 TB/s); 2048 x 28672 in
+// bfloat16 114 and 182 us (4.1, 2.6 TB/s), in float32 226 and 306 us (4.2, 3.1 TB/s).
 #include "kr_block.h"
 
 namespace kr {
