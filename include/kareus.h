@@ -558,6 +558,75 @@ kr_status kr_add_rms_norm_backward(int32_t type, int64_t rows, int64_t width, co
 size_t kr_add_rms_norm_backward_workspace(int32_t type, int64_t rows, int64_t width);
 
 /*
+ * Dropout.  Value (row i, column c) is kept where its 16 random bits are round(65536 p) or more, and
+ * taken times 65536 / (65536 - round(65536 p)); the others become 0, whatever they were.  Its bits are
+ * number c % 8 (word c % 8 / 2, low half first) of Philox4x32-10 at the counter
+ * (c / 8, i, offset's low word, its high word) under the key (seed's low word, its high word): a mask
+ * is a function of p, seed, offset and the rows' places, is stored nowhere, and is the same in the
+ * backward pass.  Calls that are to differ take another offset or seed.
+ *   p         0 .. 1 (1: nothing is kept)
+ *   seed_at   device, or NULL: one word that is read when the kernels run, in place of seed (so that
+ *             the replays of a captured call can differ); it has to hold the same word when the
+ *             backward pass runs
+ * 2^32 rows at most (KR_EUNSUPPORTED above).
+ */
+typedef struct kr_drop {
+    double p;
+    uint64_t seed, offset;
+    const uint64_t *seed_at;
+} kr_drop;
+
+/*
+ * kr_dropout -- out = D(x) + residual; the sum is taken in 32 bits and rounded once.  The gradient
+ * of x is D of out's.
+ *   residual   NULL: none
+ *   out        may be x or residual itself (same ld)
+ * 1 <= width <= 2^30.  No workspace.
+ */
+kr_status kr_dropout(int32_t type, int64_t rows, int64_t width, const void *x, int64_t ldx,
+                     const void *residual, int64_t ldr, const kr_drop *drop, void *out, int64_t ldo,
+                     void *stream);
+
+/*
+ * kr_add_layer_norm -- sum of residual and branch, and its layer norm:
+ *   s = D(x) + residual,  mean = mean(s),  rstd = 1 / sqrt(mean((s - mean)^2) + eps),
+ *   out = (s - mean) * rstd * weight + bias
+ *   type              of x, residual, weight, bias, sum and out
+ *   rows, width       rows >= 0, 1 <= width <= 2^24 (KR_EUNSUPPORTED above)
+ *   residual, bias    NULL: 0
+ *   drop              NULL: D(x) = x
+ *   sum               s, rounded to the type (the norm uses the unrounded s), or NULL
+ *   mean, rstd        [rows] or NULL: what the backward pass takes
+ * sum and out may be x or residual themselves (same rows and ld), not each other.
+ * KR_EINVAL for a negative, infinite or NaN eps.  No workspace.
+ */
+kr_status kr_add_layer_norm(int32_t type, int64_t rows, int64_t width, const void *x, int64_t ldx,
+                            const void *residual, int64_t ldr, const void *weight, const void *bias,
+                            float eps, const kr_drop *drop, void *sum, int64_t lds, void *out,
+                            int64_t ldo, float *mean, float *rstd, void *stream);
+
+/*
+ * kr_add_layer_norm_backward -- gradients of kr_add_layer_norm, given the sum s, mean and rstd that
+ * it returned.  With h = (s - mean) * rstd and g = dout * weight,
+ *   dresidual = rstd * (g - mean(g) - h * mean(g * h)) + dsum,  dx = D(dresidual)
+ *   dweight = sum over rows of dout * h,  dbias = sum over rows of dout
+ *   dsum       gradient that reaches s by the residual's path, or NULL: 0
+ *   drop       as it was forward
+ *   dresidual  may be dout or dsum itself
+ *   dx         NULL where nothing is dropped (drop NULL or p below 2^-17): dresidual is x's gradient
+ *              too.  D is taken of the unrounded dresidual.
+ *   dweight    float [width]; 0 where there are no rows
+ *   dbias      float [width], likewise, or NULL
+ */
+kr_status kr_add_layer_norm_backward(int32_t type, int64_t rows, int64_t width, const void *dout,
+                                     int64_t ldo, const void *sum, int64_t lds, const void *weight,
+                                     const float *mean, const float *rstd, const void *dsum,
+                                     int64_t ldd, const kr_drop *drop, void *dresidual, int64_t ldr,
+                                     void *dx, int64_t ldx, float *dweight, float *dbias, void *ws,
+                                     size_t ws_bytes, void *stream);
+size_t kr_add_layer_norm_backward_workspace(int32_t type, int64_t rows, int64_t width);
+
+/*
  * kr_byte_matmul -- product of 8-bit integers with a scale for each token and channel:
  *   out[i][j] = sa[i] * sb[j] * sum over k of a[i][k] * b[j][k]
  * The sum is exact (32-bit integers); the scales are applied in 32 bits, (sum * sa) * sb, and

@@ -48,6 +48,12 @@ class KrGated(ctypes.Structure):
                 ("x", _vp), ("wg", _vp), ("wu", _vp), ("ldx", _i64), ("ldg", _i64), ("ldu", _i64)]
 
 
+class KrDrop(ctypes.Structure):
+    _fields_ = [("p", _f64), ("seed", ctypes.c_uint64), ("offset", ctypes.c_uint64),
+                ("seed_at", _vp)]
+
+
+_DP = ctypes.POINTER(KrDrop)
 _BP, _GP = ctypes.POINTER(KrBytes), ctypes.POINTER(KrGated)
 _SIGS = {
     "kr_evaluate_partition": (_i32, [_SP, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp]),
@@ -92,6 +98,13 @@ _SIGS = {
     "kr_add_rms_norm_backward": (_i32, [_i32, _i64, _i64, _vp, _i64, _vp, _i64, _vp, _vp, _vp,
                                         _i64, _vp, _i64, _vp, _vp, _sz, _vp]),
     "kr_add_rms_norm_backward_workspace": (_sz, [_i32, _i64, _i64]),
+    "kr_dropout": (_i32, [_i32, _i64, _i64, _vp, _i64, _vp, _i64, _DP, _vp, _i64, _vp]),
+    "kr_add_layer_norm": (_i32, [_i32, _i64, _i64, _vp, _i64, _vp, _i64, _vp, _vp, _f32, _DP, _vp,
+                                 _i64, _vp, _i64, _vp, _vp, _vp]),
+    "kr_add_layer_norm_backward": (_i32, [_i32, _i64, _i64, _vp, _i64, _vp, _i64, _vp, _vp, _vp,
+                                          _vp, _i64, _DP, _vp, _i64, _vp, _i64, _vp, _vp, _vp, _sz,
+                                          _vp]),
+    "kr_add_layer_norm_backward_workspace": (_sz, [_i32, _i64, _i64]),
     "kr_byte_matmul": (_i32, [_BP, _i32, _vp, _i64, _vp, _sz, _vp]),
     "kr_byte_matmul_workspace": (_sz, [_BP]),
     "kr_gated_projection": (_i32, [_GP, _vp, _i64, _vp, _sz, _vp]),
@@ -931,6 +944,164 @@ def add_rms_norm_backward(dout, sum, weight, rstd, dsum=None):
                                          dx.data_ptr(), width, dw.data_ptr(), at, wsb,
                                          _raw_stream(dev)))
     return dx, dw
+
+
+def _drop(p, seed, offset, dev):
+    """kr_drop, and what it keeps alive.  seed: a number, or a 64-bit integer tensor of one element
+    that is read when the kernels run."""
+    if not 0.0 <= p <= 1.0:
+        raise ValueError("p must be in [0, 1], got %r" % (p,))
+    if not 0 <= offset < 1 << 64:
+        raise ValueError("offset must be in [0, 2^64), got %r" % (offset,))
+    if isinstance(seed, torch.Tensor):
+        if seed.dtype not in (torch.int64, torch.uint64):
+            raise TypeError("seed must be a number or a tensor of 64-bit integers, got %s" % seed.dtype)
+        if seed.get_device() != dev or seed.numel() != 1:
+            raise ValueError("seed must have one element on the current device, got %s on %s"
+                             % (tuple(seed.shape), seed.device))
+        return KrDrop(p, 0, offset, seed.data_ptr())
+    if not 0 <= seed < 1 << 64:
+        raise ValueError("seed must be in [0, 2^64), got %r" % (seed,))
+    return KrDrop(p, seed, offset, None)
+
+
+class _Dropout(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, residual, p, seed, offset):
+        tensor = isinstance(seed, torch.Tensor)
+        ctx.save_for_backward(*((seed,) if tensor else ()))
+        ctx.drop = p, seed if not tensor else None, offset
+        return dropout(x, p, seed, offset, residual)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dout):
+        p, seed, offset = ctx.drop
+        need = ctx.needs_input_grad
+        dx = dropout(dout, p, *ctx.saved_tensors or (seed,), offset) if need[0] else None
+        return dx, dout if need[1] else None, None, None, None
+
+
+def dropout(x, p: float, seed, offset: int = 0, residual=None) -> torch.Tensor:
+    """D(x), or D(x) + residual: each value of x is kept with probability 1 - p, and divided by it, by
+    random numbers that depend on seed, offset and its row and column alone (kr_dropout).  seed is a
+    number, or a 64-bit integer tensor of one element on the device, which is read when the kernel
+    runs: a captured call draws anew where that changed, and the backward pass needs it unchanged.
+    Its gradient reaches x and residual."""
+    if _tracked(x, residual):
+        return _Dropout.apply(x, residual, p, seed, offset)
+    t = _type(x, "x")
+    dev = _here(x, "x")
+    xr, n, ldx = _rows(x, "x", dev)
+    width = xr.shape[1]
+    rr, ldr = None, 0
+    if residual is not None:
+        _like(residual, x, "residual", "x")
+        rr, _, ldr = _rows(residual, "residual", dev, width)
+    d = _drop(p, seed, offset, dev)
+    out = _new_like(x)
+    _check("kr_dropout",
+           _lib.kr_dropout(t, n, width, xr.data_ptr(), ldx, None if rr is None else rr.data_ptr(),
+                           ldr, d, out.data_ptr(), width, _raw_stream(dev)))
+    return out
+
+
+@dataclasses.dataclass
+class LayerNormed:
+    out: torch.Tensor              # the norm, like x
+    sum: torch.Tensor              # D(x) + residual, like x (x itself where that is all)
+    mean: torch.Tensor             # float32, one for each row
+    rstd: torch.Tensor
+
+
+class _AddLayerNorm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, bias, residual, eps, p, seed, offset):
+        r = add_layer_norm(x, weight, bias, residual, eps, p, seed, offset)
+        ctx.set_materialize_grads(False)
+        ctx.mark_non_differentiable(r.mean, r.rstd)
+        tensor = isinstance(seed, torch.Tensor)
+        ctx.save_for_backward(r.sum, weight, r.mean, r.rstd, *((seed,) if tensor else ()))
+        ctx.drop = p, None if tensor else seed, offset
+        ctx.bias = None if bias is None else bias.shape
+        # where the sum is x, its gradient by that path is torch's own matter
+        return (r.out, r.mean, r.rstd, *(() if residual is None and not p else (r.sum,)))
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dout, _, __, dsum=None):
+        total, weight, mean, rstd, *held = ctx.saved_tensors
+        p, seed, offset = ctx.drop
+        seed = held[0] if held else seed
+        need = ctx.needs_input_grad
+        if dout is None:  # only the sum was used
+            dx, dres, dw, db = dsum, dsum, None, None
+            if p and need[0]:
+                dx = dropout(dsum, p, seed, offset)
+        else:
+            dx, dres, dw, db = add_layer_norm_backward(dout, total, weight, mean, rstd, dsum, p,
+                                                       seed, offset)
+            dw = dw.to(weight.dtype).reshape(weight.shape) if need[1] else None
+            db = db.to(weight.dtype).reshape(ctx.bias) if need[2] else None
+        return (dx if need[0] else None, dw, db, dres if need[3] else None, None, None, None, None)
+
+
+def add_layer_norm(x, weight, bias=None, residual=None, eps: float = 1e-5, p: float = 0.0,
+                   seed=0, offset: int = 0) -> LayerNormed:
+    """s = D(x) + residual and its layer norm over the last dimension, (s - mean) * rstd * weight +
+    bias (kr_add_layer_norm); D is dropout(x, p, seed, offset), of the same mask.  out and sum have
+    gradients, mean and rstd have none."""
+    if _tracked(x, weight, bias, residual):
+        out, mean, rstd, *total = _AddLayerNorm.apply(x, weight, bias, residual, eps, p, seed, offset)
+        return LayerNormed(out, total[0] if total else x, mean, rstd)
+    t, dev, xr, n, ldx, width, w, rr, ldr = _norm_inputs(x, weight, residual)
+    b = None if bias is None else _vector(bias, width, x.dtype, "bias", dev)
+    d = _drop(p, seed, offset, dev) if p else None
+    out = _new_like(x)
+    total = x if rr is None and d is None else _new_like(x)
+    mean, rstd = _new(x.shape[:-1], torch.float32), _new(x.shape[:-1], torch.float32)
+    _check("kr_add_layer_norm",
+           _lib.kr_add_layer_norm(t, n, width, xr.data_ptr(), ldx,
+                                  None if rr is None else rr.data_ptr(), ldr, w.data_ptr(),
+                                  None if b is None else b.data_ptr(), eps, d,
+                                  None if total is x else total.data_ptr(), width, out.data_ptr(),
+                                  width, mean.data_ptr(), rstd.data_ptr(), _raw_stream(dev)))
+    return LayerNormed(out, total, mean, rstd)
+
+
+def add_layer_norm_backward(dout, sum, weight, mean, rstd, dsum=None, p: float = 0.0, seed=0,
+                            offset: int = 0):
+    """(dx, dresidual, dweight, dbias) of add_layer_norm from its sum, mean and rstd; dsum is the
+    gradient that reaches the sum by the residual's path.  dx is dresidual itself where p is 0;
+    dweight and dbias are float32 (kr_add_layer_norm_backward)."""
+    t = _type(dout, "dout")
+    _like(sum, dout, "sum", "dout")
+    dev = _here(dout, "dout")
+    gr, n, ldo = _rows(dout, "dout", dev)
+    width = gr.shape[1]
+    sr, _, lds = _rows(sum, "sum", dev, width)
+    w = _vector(weight, width, dout.dtype, "weight", dev)
+    m = _vector(mean, n, torch.float32, "mean", dev)
+    f = _vector(rstd, n, torch.float32, "rstd", dev)
+    dr, ldd = None, 0
+    if dsum is not None:
+        _like(dsum, dout, "dsum", "dout")
+        dr, _, ldd = _rows(dsum, "dsum", dev, width)
+    d = _drop(p, seed, offset, dev) if p else None
+    dres = _new_like(dout)
+    dx = dres if d is None else _new_like(dout)
+    dw, db = _new(width, torch.float32), _new(width, torch.float32)
+    wsb = _lib.kr_add_layer_norm_backward_workspace(t, n, width)
+    ws, at = _scratch(wsb)
+    _check("kr_add_layer_norm_backward",
+           _lib.kr_add_layer_norm_backward(t, n, width, gr.data_ptr(), ldo, sr.data_ptr(), lds,
+                                           w.data_ptr(), m.data_ptr(), f.data_ptr(),
+                                           None if dr is None else dr.data_ptr(), ldd, d,
+                                           dres.data_ptr(), width,
+                                           None if d is None else dx.data_ptr(), width,
+                                           dw.data_ptr(), db.data_ptr(), at, wsb,
+                                           _raw_stream(dev)))
+    return dx, dres, dw, db
 
 
 def byte_matmul(a, sa, b, sb, dtype=torch.bfloat16) -> torch.Tensor:

@@ -2,6 +2,7 @@
 // order.  Declarations and contracts: include/kareus.h.
 #include <cmath>
 
+#include "kr_drop.h"
 #include "kr_gated.h"
 
 using namespace kr;
@@ -88,6 +89,85 @@ extern "C" kr_status kr_add_rms_norm_backward(int32_t type, int64_t rows, int64_
     const NormBackArgs a{rows, (int)width, sum, weight, dout, dsum, lds, ldo, ldd, rstd,
                          dx, ldx, dweight, (float *)ws};
     return said(launch_norm_back(type, a, (hipStream_t)stream));
+}
+
+// ---- dropout and layer norm -----------------------------------------------------------------
+
+namespace {
+
+constexpr int64_t kDropWidthMost = 1 << 30;
+constexpr int64_t kDropRowsMost = (int64_t)1 << 32;  // a row's number is one word of the counter
+
+bool drop_ok(const kr_drop *d)
+{
+    return !d || (d->p >= 0.0 && d->p <= 1.0 && (uintptr_t)d->seed_at % 8 == 0);
+}
+
+}  // namespace
+
+extern "C" kr_status kr_dropout(int32_t type, int64_t rows, int64_t width, const void *x, int64_t ldx,
+                                const void *residual, int64_t ldr, const kr_drop *drop, void *out,
+                                int64_t ldo, void *stream)
+{
+    if (!type_ok(type) || rows < 0 || width < 1 || !drop || !drop_ok(drop)) return KR_EINVAL;
+    if (width > kDropWidthMost || rows > kDropRowsMost) return KR_EUNSUPPORTED;
+    if (rows == 0) return KR_OK;
+    const size_t es = size_of(type);
+    if (!matrix_ok(x, ldx, width, es) || (residual && !matrix_ok(residual, ldr, width, es)) ||
+        !matrix_ok(out, ldo, width, es))
+        return KR_EINVAL;
+    const DropoutArgs a{rows, width, x, residual, out, ldx, ldr, ldo, 0, drop_of(drop)};
+    return said(launch_dropout(type, a, (hipStream_t)stream));
+}
+
+extern "C" kr_status kr_add_layer_norm(int32_t type, int64_t rows, int64_t width, const void *x,
+                                       int64_t ldx, const void *residual, int64_t ldr,
+                                       const void *weight, const void *bias, float eps,
+                                       const kr_drop *drop, void *sum, int64_t lds, void *out,
+                                       int64_t ldo, float *mean, float *rstd, void *stream)
+{
+    if (!type_ok(type) || rows < 0 || width < 1 || !(eps >= 0.0f) || std::isinf(eps) || !drop_ok(drop))
+        return KR_EINVAL;
+    if (width > kWidthMost || (drop && rows > kDropRowsMost)) return KR_EUNSUPPORTED;
+    if (rows == 0) return KR_OK;
+    const size_t es = size_of(type);
+    if (!matrix_ok(x, ldx, width, es) || (residual && !matrix_ok(residual, ldr, width, es)) ||
+        !weight || (uintptr_t)weight % es || (uintptr_t)bias % es ||
+        (sum && !matrix_ok(sum, lds, width, es)) || !matrix_ok(out, ldo, width, es))
+        return KR_EINVAL;
+    const LayerNormArgs a{rows, (int)width, x, residual, weight, bias, ldx, ldr, eps,
+                          sum, out, lds, ldo, mean, rstd, 0, drop_of(drop)};
+    return said(launch_layer_norm(type, a, (hipStream_t)stream));
+}
+
+extern "C" size_t kr_add_layer_norm_backward_workspace(int32_t type, int64_t rows, int64_t width)
+{
+    if (!type_ok(type) || rows < 0 || width < 1 || width > kWidthMost) return 0;
+    return (size_t)layer_norm_back_slots(rows, (int)width) * 2 * (size_t)width * sizeof(float);
+}
+
+extern "C" kr_status kr_add_layer_norm_backward(
+    int32_t type, int64_t rows, int64_t width, const void *dout, int64_t ldo, const void *sum,
+    int64_t lds, const void *weight, const float *mean, const float *rstd, const void *dsum,
+    int64_t ldd, const kr_drop *drop, void *dresidual, int64_t ldr, void *dx, int64_t ldx,
+    float *dweight, float *dbias, void *ws, size_t ws_bytes, void *stream)
+{
+    if (!type_ok(type) || rows < 0 || width < 1 || !dweight || !drop_ok(drop)) return KR_EINVAL;
+    if (width > kWidthMost || (drop && rows > kDropRowsMost)) return KR_EUNSUPPORTED;
+    const size_t es = size_of(type);
+    const Drop d = drop_of(drop);
+    if (rows > 0 &&
+        (!matrix_ok(dout, ldo, width, es) || !matrix_ok(sum, lds, width, es) || !weight ||
+         (uintptr_t)weight % es || !mean || !rstd || (dsum && !matrix_ok(dsum, ldd, width, es)) ||
+         !matrix_ok(dresidual, ldr, width, es) || (d.cut && !dx) ||
+         (dx && (dx == dresidual || !matrix_ok(dx, ldx, width, es)))))
+        return KR_EINVAL;
+    const size_t need = kr_add_layer_norm_backward_workspace(type, rows, width);
+    if (ws_bytes < need || (need && !ws)) return KR_ECAPACITY;
+    if ((uintptr_t)ws % sizeof(float)) return KR_EINVAL;
+    const LayerNormBackArgs a{rows, (int)width, sum, weight, dout, dsum, lds, ldo, ldd, mean, rstd,
+                              dresidual, dx, ldr, ldx, dweight, dbias, (float *)ws, 0, d};
+    return said(launch_layer_norm_back(type, a, (hipStream_t)stream));
 }
 
 // ---- projections --------------------------------------------------------------------------

@@ -1,0 +1,51 @@
+// How rows are shared out to threads by kernels that keep a row in registers.
+#pragma once
+
+#include <initializer_list>
+#include <type_traits>
+
+#include "kr_block.h"
+
+namespace kr {
+
+// Threads of a block: rows of up to a wave share one.
+template <int TPR>
+constexpr int kBlock = TPR <= 64 ? 256 : TPR;
+
+// Threads a row and elements a thread for a width, the fewest that hold it.
+struct Shape {
+    int tpr, fpt;
+};
+inline Shape shape_of(int width)
+{
+    for (const Shape s : {Shape{16, 8}, {32, 8}, {64, 8}, {128, 8}, {256, 8}, {384, 8}, {512, 8},
+                          {768, 8}, {1024, 8}, {1024, 16}})
+        if (width <= s.tpr * s.fpt) return s;
+    return {0, 0};
+}
+inline int rows_per_block(Shape s) { return s.tpr > 0 && s.tpr <= 64 ? 256 / s.tpr : 1; }
+
+// f(threads a row, elements a thread) with the shape as constants; false where no shape holds the row.
+template <typename F>
+inline bool with_shape(Shape s, F f)
+{
+#define KR_SHAPE(T, E) \
+    if (s.tpr == T && s.fpt == E) return f(std::integral_constant<int, T>(), std::integral_constant<int, E>()), true
+    KR_SHAPE(16, 8);
+    KR_SHAPE(32, 8);
+    KR_SHAPE(64, 8);
+    KR_SHAPE(128, 8);
+    KR_SHAPE(256, 8);
+    KR_SHAPE(384, 8);
+    KR_SHAPE(512, 8);
+    KR_SHAPE(768, 8);
+    KR_SHAPE(1024, 8);
+    KR_SHAPE(1024, 16);
+#undef KR_SHAPE
+    return false;
+}
+
+// Rows of one launch: a grid has fewer than 2^32 threads.
+constexpr int64_t kRowsPerLaunch = 1 << 21;
+
+}  // namespace kr

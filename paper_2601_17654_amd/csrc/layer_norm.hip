@@ -1,0 +1,463 @@
+// Layer norm with the residual's addition and dropout of the branch, forward and backward.
+//
+//   s = r + D(x),  m = mean(s),  f = 1 / sqrt(mean((s - m)^2) + eps),  n = (s - m) f w + b
+//
+// A row stays in the registers of the threads that share it, so that each element is read once and
+// written once, and the variance is that of the differences from the mean: no sum of squares
+// from which a square is taken.  Rows of more than 16,384 elements are read again from memory
+// instead: three times forward, twice backward and once more for the sums over rows.
+// All arithmetic is in 32 bits; stored values are rounded once.
+#include "kr_drop.h"
+#include "kr_rows.h"
+
+namespace kr {
+
+namespace {
+
+template <typename T, int TPR, int FPT, bool DROP>
+__global__ __launch_bounds__(kBlock<TPR>) void layer_norm_kernel(LayerNormArgs a)
+{
+    constexpr int V = kVec<T>, NV = FPT / V, RPB = kBlock<TPR> / TPR;
+    __shared__ float part[2][TPR > 64 ? TPR / 64 : 1];
+    const int t = threadIdx.x % TPR;
+    const int64_t row = (int64_t)blockIdx.x * RPB + threadIdx.x / TPR;
+    if (RPB > 1 && row >= a.rows) return;  // whole rows' threads, and such rows take no barrier
+    const T *x = (const T *)a.x + row * a.ldx;
+    const T *r = a.res ? (const T *)a.res + row * a.ldr : nullptr;
+    float s[NV][V];
+    Pack<T, V> xs[NV], rs[NV], ws[NV], bs[NV];
+#pragma unroll
+    for (int j = 0; j < NV; ++j) xs[j] = load_row(x, (j * TPR + t) * V, a.width);
+    if (r) {
+#pragma unroll
+        for (int j = 0; j < NV; ++j) rs[j] = load_row(r, (j * TPR + t) * V, a.width);
+    }
+#pragma unroll
+    for (int j = 0; j < NV; ++j) ws[j] = load_row((const T *)a.w, (j * TPR + t) * V, a.width);
+    if (a.b) {
+#pragma unroll
+        for (int j = 0; j < NV; ++j) bs[j] = load_row((const T *)a.b, (j * TPR + t) * V, a.width);
+    }
+#pragma unroll
+    for (int j = 0; j < NV; ++j) floats(xs[j], s[j]);
+    if (DROP) {
+        const uint64_t seed = drop_seed(a.drop);
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+            drop_out<V>(a.drop, seed, (j * TPR + t) * V, (uint32_t)(a.row0 + row), s[j]);
+    }
+    if (r) {
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+#pragma unroll
+            for (int e = 0; e < V; ++e) s[j][e] += (float)rs[j].v[e];
+    }
+    if (a.sum) {
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+            store_row((T *)a.sum + row * a.lds, (j * TPR + t) * V, a.width, s[j]);
+    }
+    float total = 0.0f, squares = 0.0f;  // past the row's end there are zeros
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+#pragma unroll
+        for (int e = 0; e < V; ++e) total += s[j][e];
+    const float m = row_sum<TPR>(total, part[0]) / (float)a.width;
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            s[j][e] = (j * TPR + t) * V + e < a.width ? s[j][e] - m : 0.0f;
+            squares = fmaf(s[j][e], s[j][e], squares);
+        }
+    const float f = 1.0f / sqrtf(row_sum<TPR>(squares, part[1]) / (float)a.width + a.eps);
+    if (t == 0) {
+        if (a.mean) a.mean[row] = m;
+        if (a.rstd) a.rstd[row] = f;
+    }
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            s[j][e] = s[j][e] * f * (float)ws[j].v[e];
+            if (a.b) s[j][e] += (float)bs[j].v[e];
+        }
+        store_row((T *)a.out + row * a.ldo, (j * TPR + t) * V, a.width, s[j]);
+    }
+}
+
+// Rows of any length.  Each thread writes an element after its last read of it.
+template <typename T, bool DROP>
+__global__ __launch_bounds__(1024) void layer_norm_long_kernel(LayerNormArgs a)
+{
+    constexpr int V = kVec<T>, STEP = 1024 * V;
+    __shared__ float part[2][16];
+    const int t = threadIdx.x;
+    const int64_t row = blockIdx.x;
+    const T *x = (const T *)a.x + row * a.ldx;
+    const T *r = a.res ? (const T *)a.res + row * a.ldr : nullptr;
+    const uint64_t seed = DROP ? drop_seed(a.drop) : 0;
+    auto load = [&](int64_t c, float *s) {
+        floats(load_row(x, (int)c, a.width), s);
+        if (DROP) drop_out<V>(a.drop, seed, (int)c, (uint32_t)(a.row0 + row), s);
+        if (r) {
+            const Pack<T, V> b = load_row(r, (int)c, a.width);
+#pragma unroll
+            for (int e = 0; e < V; ++e) s[e] += (float)b.v[e];
+        }
+    };
+    float total = 0.0f, squares = 0.0f, s[V];
+    for (int64_t c = t * V; c < a.width; c += STEP) {
+        load(c, s);
+#pragma unroll
+        for (int e = 0; e < V; ++e) total += s[e];
+    }
+    const float m = row_sum<1024>(total, part[0]) / (float)a.width;
+    for (int64_t c = t * V; c < a.width; c += STEP) {
+        load(c, s);
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            const float d = c + e < a.width ? s[e] - m : 0.0f;
+            squares = fmaf(d, d, squares);
+        }
+    }
+    const float f = 1.0f / sqrtf(row_sum<1024>(squares, part[1]) / (float)a.width + a.eps);
+    if (t == 0) {
+        if (a.mean) a.mean[row] = m;
+        if (a.rstd) a.rstd[row] = f;
+    }
+    for (int64_t c = t * V; c < a.width; c += STEP) {
+        load(c, s);
+        float n[V], b[V];
+        const Pack<T, V> w = load_row((const T *)a.w, (int)c, a.width);
+        if (a.b) {
+            floats(load_row((const T *)a.b, (int)c, a.width), b);
+        } else {
+#pragma unroll
+            for (int e = 0; e < V; ++e) b[e] = 0.0f;
+        }
+#pragma unroll
+        for (int e = 0; e < V; ++e) n[e] = (s[e] - m) * f * (float)w.v[e] + b[e];
+        if (a.sum) store_row((T *)a.sum + row * a.lds, (int)c, a.width, s);
+        store_row((T *)a.out + row * a.ldo, (int)c, a.width, n);
+    }
+}
+
+// Two sums over the TPR threads that share a row, as row_sum adds one.
+template <int TPR>
+__device__ inline float2 row_sums(float2 x, float2 *part)
+{
+#pragma unroll
+    for (int o = TPR < 64 ? TPR / 2 : 32; o; o >>= 1) {
+        x.x += __shfl_xor(x.x, o);
+        x.y += __shfl_xor(x.y, o);
+    }
+    if (TPR <= 64) return x;
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = x;
+    __syncthreads();
+    float2 s = make_float2(0.0f, 0.0f);
+#pragma unroll
+    for (int i = 0; i < TPR / 64; ++i) {
+        s.x += part[i].x;
+        s.y += part[i].y;
+    }
+    return s;
+}
+
+// Gradients, with h = (s - m) f, g = dn w:  ds = f (g - mean(g) - h mean(g h)) + dsum,
+// dx = D(ds),  dw = sum dn h,  db = sum dn.
+// A block takes rows in turn and keeps its shares of dw and db in registers; the blocks' shares
+// are added by layer_norm_weight_kernel in a fixed order.
+template <typename T, int TPR, int FPT, bool DROP>
+__global__ __launch_bounds__(kBlock<TPR>) void layer_norm_back_kernel(LayerNormBackArgs a)
+{
+    constexpr int V = kVec<T>, NV = FPT / V, RPB = kBlock<TPR> / TPR;
+    constexpr bool AHEAD = FPT == 8;  // the next row's loads: with 16 there are no registers left
+    __shared__ float2 part[2][TPR > 64 ? TPR / 64 : 1];
+    __shared__ float share[RPB > 1 ? RPB * TPR * FPT : 1];
+    const int t = threadIdx.x % TPR, sub = threadIdx.x / TPR;
+    const uint64_t seed = DROP ? drop_seed(a.drop) : 0;
+    float dw[NV][V], db[NV][V];
+    Pack<T, V> ws[NV];
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        ws[j] = load_row((const T *)a.w, (j * TPR + t) * V, a.width);
+#pragma unroll
+        for (int e = 0; e < V; ++e) dw[j][e] = db[j][e] = 0.0f;
+    }
+    Pack<T, V> hs[NV], gs[NV], ds[NV];
+    float m = 0.0f, f = 0.0f;
+    auto load = [&](int64_t row) {  // of the next row, while one is worked on
+        m = a.mean[row];
+        f = a.rstd[row];
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            hs[j] = load_row((const T *)a.s + row * a.lds, (j * TPR + t) * V, a.width);
+            gs[j] = load_row((const T *)a.dout + row * a.ldo, (j * TPR + t) * V, a.width);
+            if (a.dsum)
+                ds[j] = load_row((const T *)a.dsum + row * a.ldd, (j * TPR + t) * V, a.width);
+        }
+    };
+    int turn = 0;
+    const int64_t stride = (int64_t)gridDim.x * RPB;
+    int64_t row = (int64_t)blockIdx.x * RPB + sub;
+    if (AHEAD && row < a.rows) load(row);
+    for (; row < a.rows; row += stride, turn ^= 1) {
+        if (!AHEAD) load(row);
+        float h[NV][V], g[NV][V], d[NV][V];
+        const float m0 = m, f0 = f;
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            floats(hs[j], h[j]);
+            floats(gs[j], g[j]);
+#pragma unroll
+            for (int e = 0; e < V; ++e) d[j][e] = a.dsum ? (float)ds[j].v[e] : 0.0f;
+        }
+        if (AHEAD && row + stride < a.rows) load(row + stride);
+        float2 c = make_float2(0.0f, 0.0f);  // past the row's end g is 0
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                h[j][e] = (h[j][e] - m0) * f0;
+                dw[j][e] = fmaf(g[j][e], h[j][e], dw[j][e]);
+                db[j][e] += g[j][e];
+                g[j][e] *= (float)ws[j].v[e];
+                c.x += g[j][e];
+                c.y = fmaf(g[j][e], (j * TPR + t) * V + e < a.width ? h[j][e] : 0.0f, c.y);
+            }
+        // two sets of words in turn: one barrier a row keeps a set until all have read it
+        c = row_sums<TPR>(c, part[turn]);
+        c.x /= (float)a.width;
+        c.y /= (float)a.width;
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+#pragma unroll
+            for (int e = 0; e < V; ++e) d[j][e] += (g[j][e] - c.x - h[j][e] * c.y) * f0;
+            store_row((T *)a.dres + row * a.ldr, (j * TPR + t) * V, a.width, d[j]);
+            if (DROP) {
+                drop_out<V>(a.drop, seed, (j * TPR + t) * V, (uint32_t)(a.row0 + row), d[j]);
+                store_row((T *)a.dx + row * a.ldx, (j * TPR + t) * V, a.width, d[j]);
+            }
+        }
+    }
+    float *slot = a.part + (int64_t)blockIdx.x * 2 * a.width;
+    if (RPB > 1) {  // the block's rows side by side: their shares in turn
+#pragma unroll
+        for (int what = 0; what < 2; ++what) {
+#pragma unroll
+            for (int j = 0; j < NV; ++j)
+#pragma unroll
+                for (int e = 0; e < V; ++e)
+                    share[sub * TPR * FPT + (j * TPR + t) * V + e] = what ? db[j][e] : dw[j][e];
+            __syncthreads();
+            for (int c = threadIdx.x; c < a.width; c += 256) {
+                float x = 0.0f;
+#pragma unroll
+                for (int k = 0; k < RPB; ++k) x += share[k * TPR * FPT + c];
+                slot[(int64_t)what * a.width + c] = x;
+            }
+            __syncthreads();
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+#pragma unroll
+            for (int e = 0; e < V; e += kVec<float>) {
+                store_row(slot, (j * TPR + t) * V + e, a.width, dw[j] + e);
+                store_row(slot + a.width, (j * TPR + t) * V + e, a.width, db[j] + e);
+            }
+        (void)share;
+    }
+}
+
+// Rows of any length: one block a row, read twice.
+template <typename T, bool DROP>
+__global__ __launch_bounds__(1024) void layer_norm_back_long_kernel(LayerNormBackArgs a)
+{
+    constexpr int V = kVec<T>, STEP = 1024 * V;
+    __shared__ float2 part[16];
+    const int t = threadIdx.x;
+    const int64_t row = blockIdx.x;
+    const uint64_t seed = DROP ? drop_seed(a.drop) : 0;
+    const float m = a.mean[row], f = a.rstd[row];
+    const T *sr = (const T *)a.s + row * a.lds, *gr = (const T *)a.dout + row * a.ldo;
+    float2 c = make_float2(0.0f, 0.0f);
+    float h[V], g[V], w[V];
+    auto load = [&](int64_t k) {
+        floats(load_row(sr, (int)k, a.width), h);
+        floats(load_row(gr, (int)k, a.width), g);
+        floats(load_row((const T *)a.w, (int)k, a.width), w);
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            h[e] = k + e < a.width ? (h[e] - m) * f : 0.0f;
+            g[e] *= w[e];
+        }
+    };
+    for (int64_t k = t * V; k < a.width; k += STEP) {
+        load(k);
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            c.x += g[e];
+            c.y = fmaf(g[e], h[e], c.y);
+        }
+    }
+    c = row_sums<1024>(c, part);
+    c.x /= (float)a.width;
+    c.y /= (float)a.width;
+    for (int64_t k = t * V; k < a.width; k += STEP) {
+        float d[V];
+        load(k);
+        if (a.dsum) {
+            floats(load_row((const T *)a.dsum + row * a.ldd, (int)k, a.width), d);
+        } else {
+#pragma unroll
+            for (int e = 0; e < V; ++e) d[e] = 0.0f;
+        }
+#pragma unroll
+        for (int e = 0; e < V; ++e) d[e] += (g[e] - c.x - h[e] * c.y) * f;
+        store_row((T *)a.dres + row * a.ldr, (int)k, a.width, d);
+        if (DROP) {
+            drop_out<V>(a.drop, seed, (int)k, (uint32_t)(a.row0 + row), d);
+            store_row((T *)a.dx + row * a.ldx, (int)k, a.width, d);
+        }
+    }
+}
+
+// Their dw and db: 256 columns and every gridDim.y-th row a block.
+template <typename T>
+__global__ __launch_bounds__(256) void layer_norm_back_long_weight_kernel(LayerNormBackArgs a)
+{
+    const int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (c >= a.width) return;
+    float dw = 0.0f, db = 0.0f;
+    for (int64_t row = blockIdx.y; row < a.rows; row += gridDim.y) {
+        const float g = (float)((const T *)a.dout)[row * a.ldo + c];
+        dw = fmaf(g, ((float)((const T *)a.s)[row * a.lds + c] - a.mean[row]) * a.rstd[row], dw);
+        db += g;
+    }
+    float *slot = a.part + (int64_t)blockIdx.y * 2 * a.width;
+    slot[c] = dw;
+    slot[a.width + c] = db;
+}
+
+// dw and db = sums of the slots: 32 columns a block, 32 half waves that take every 32nd slot.
+__global__ __launch_bounds__(1024) void layer_norm_weight_kernel(const float *part, int slots,
+                                                                 int64_t width, float *dw, float *db)
+{
+    __shared__ float sums[32][33];
+    const int lane = threadIdx.x & 31, group = threadIdx.x >> 5;
+    const int64_t c = (int64_t)blockIdx.x * 32 + lane, both = 2 * width;
+    float s = 0.0f;
+    if (c < both) {
+#pragma unroll 8
+        for (int k = group; k < slots; k += 32) s += part[k * both + c];
+    }
+    sums[group][lane] = s;
+    __syncthreads();
+    if (group == 0 && c < both) {
+        s = 0.0f;
+#pragma unroll
+        for (int k = 0; k < 32; ++k) s += sums[k][lane];
+        if (c < width) dw[c] = s;
+        else if (db) db[c - width] = s;
+    }
+}
+
+template <typename T, bool DROP>
+hipError_t typed(LayerNormArgs a, hipStream_t st)
+{
+    const Shape s = shape_of(a.width);
+    const int rpb = rows_per_block(s);
+    const int64_t rows = a.rows;
+    for (int64_t done = 0; done < rows; done += kRowsPerLaunch) {
+        a.rows = rows - done < kRowsPerLaunch ? rows - done : kRowsPerLaunch;
+        const unsigned grid = (unsigned)((a.rows + rpb - 1) / rpb);
+        if (!with_shape(s, [&](auto tpr, auto fpt) {
+                constexpr int TPR = decltype(tpr)::value, FPT = decltype(fpt)::value;
+                layer_norm_kernel<T, TPR, FPT, DROP><<<grid, kBlock<TPR>, 0, st>>>(a);
+            }))
+            layer_norm_long_kernel<T, DROP><<<grid, 1024, 0, st>>>(a);
+        if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+        a.x = (const T *)a.x + a.rows * a.ldx;
+        if (a.res) a.res = (const T *)a.res + a.rows * a.ldr;
+        if (a.sum) a.sum = (T *)a.sum + a.rows * a.lds;
+        a.out = (T *)a.out + a.rows * a.ldo;
+        if (a.mean) a.mean += a.rows;
+        if (a.rstd) a.rstd += a.rows;
+        a.row0 += a.rows;
+    }
+    return hipSuccess;
+}
+
+template <typename T, bool DROP>
+hipError_t back_long(LayerNormBackArgs a, int slots, hipStream_t st)
+{
+    // dw and db first: an output may take dout's place
+    const dim3 grid((unsigned)((a.width + 255) / 256), slots);
+    layer_norm_back_long_weight_kernel<T><<<grid, 256, 0, st>>>(a);
+    const int64_t rows = a.rows;
+    for (int64_t done = 0; done < rows; done += kRowsPerLaunch) {
+        a.rows = rows - done < kRowsPerLaunch ? rows - done : kRowsPerLaunch;
+        layer_norm_back_long_kernel<T, DROP><<<(unsigned)a.rows, 1024, 0, st>>>(a);
+        a.s = (const T *)a.s + a.rows * a.lds;
+        a.dout = (const T *)a.dout + a.rows * a.ldo;
+        if (a.dsum) a.dsum = (const T *)a.dsum + a.rows * a.ldd;
+        a.dres = (T *)a.dres + a.rows * a.ldr;
+        if (DROP) a.dx = (T *)a.dx + a.rows * a.ldx;
+        a.mean += a.rows;
+        a.rstd += a.rows;
+        a.row0 += a.rows;
+    }
+    return hipGetLastError();
+}
+
+template <typename T, bool DROP>
+hipError_t back_typed(const LayerNormBackArgs &a, hipStream_t st)
+{
+    const int slots = layer_norm_back_slots(a.rows, a.width);
+    if (a.rows > 0) {
+        hipError_t e = hipSuccess;
+        if (!with_shape(shape_of(a.width), [&](auto tpr, auto fpt) {
+                constexpr int TPR = decltype(tpr)::value, FPT = decltype(fpt)::value;
+                layer_norm_back_kernel<T, TPR, FPT, DROP><<<slots, kBlock<TPR>, 0, st>>>(a);
+                e = hipGetLastError();
+            }))
+            e = back_long<T, DROP>(a, slots, st);
+        if (e != hipSuccess) return e;
+    }
+    const int64_t columns = a.db ? 2 * (int64_t)a.width : a.width;
+    layer_norm_weight_kernel<<<(unsigned)((columns + 31) / 32), 1024, 0, st>>>(a.part, slots, a.width,
+                                                                              a.dw, a.db);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_layer_norm(int dtype, const LayerNormArgs &a, hipStream_t st)
+{
+    const bool drop = a.drop.cut != 0;
+    if (dtype == KR_F32) return drop ? typed<float, true>(a, st) : typed<float, false>(a, st);
+    if (dtype == KR_F16) return drop ? typed<f16, true>(a, st) : typed<f16, false>(a, st);
+    return drop ? typed<bf16, true>(a, st) : typed<bf16, false>(a, st);
+}
+
+int layer_norm_back_slots(int64_t rows, int width)
+{
+    if (rows <= 0) return 0;
+    const Shape s = shape_of(width);
+    const int rpb = rows_per_block(s);
+    const int most = s.tpr == 0 ? 64 : s.tpr == 128 ? 2048 : s.tpr <= 256 ? 1024 : s.tpr <= 512 ? 512 : 256;
+    const int64_t blocks = (rows + rpb - 1) / rpb;
+    return (int)(blocks < most ? blocks : most);
+}
+
+hipError_t launch_layer_norm_back(int dtype, const LayerNormBackArgs &a, hipStream_t st)
+{
+    const bool drop = a.dx != nullptr;
+    if (dtype == KR_F32) return drop ? back_typed<float, true>(a, st) : back_typed<float, false>(a, st);
+    if (dtype == KR_F16) return drop ? back_typed<f16, true>(a, st) : back_typed<f16, false>(a, st);
+    return drop ? back_typed<bf16, true>(a, st) : back_typed<bf16, false>(a, st);
+}
+
+}  // namespace kr

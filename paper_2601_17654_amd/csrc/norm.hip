@@ -17,16 +17,11 @@
 // rows, forward and backward, of the bytes that they cannot do without: 4096 x 16384 in bfloat16 100
 // and 113 us (5.4, 4.8 TB/s), in float32 193 and 271 us (5.6, 4.0 TB/s); 2048 x 28672 in
 // bfloat16 114 and 182 us (4.1, 2.6 TB/s), in float32 226 and 306 us (4.2, 3.1 TB/s).
-#include "kr_block.h"
+#include "kr_rows.h"
 
 namespace kr {
 
 namespace {
-
-// Threads of a block: rows of up to a wave share one.
-template <int TPR>
-constexpr int kBlock = TPR <= 64 ? 256 : TPR;
-constexpr int kRowMost = 16384;  // elements that 1,024 threads hold, 16 each
 
 // A row's values held in 8 bits.  The largest magnitude stands at 127; one below 2^-100 has no
 // use and would overflow the factor, so such a row is held as zeros.  Magnitudes are compared
@@ -357,22 +352,6 @@ __global__ __launch_bounds__(1024) void norm_weight_kernel(const float *part, in
         dw[c] = s;
     }
 }
-
-// Threads a row and elements a thread for a width, the fewest that hold it.
-struct Shape {
-    int tpr, fpt;
-};
-Shape shape_of(int width)
-{
-    for (const Shape s : {Shape{16, 8}, {32, 8}, {64, 8}, {128, 8}, {256, 8}, {384, 8}, {512, 8},
-                          {768, 8}, {1024, 8}, {1024, 16}})
-        if (width <= s.tpr * s.fpt) return s;
-    return {0, 0};
-}
-int rows_per_block(Shape s) { return s.tpr > 0 && s.tpr <= 64 ? 256 / s.tpr : 1; }
-
-// Rows of one launch: a grid has fewer than 2^32 threads.
-constexpr int64_t kRowsPerLaunch = 1 << 21;
 
 template <typename T, bool HELD>
 hipError_t norm_rows(const NormArgs &a, hipStream_t st)
