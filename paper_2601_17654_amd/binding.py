@@ -11,7 +11,7 @@ from __future__ import annotations
 import ctypes
 import dataclasses
 import os
-from typing import Optional
+from typing import NamedTuple, Optional
 
 import numpy as np
 import torch
@@ -53,6 +53,15 @@ class KrDrop(ctypes.Structure):
                 ("seed_at", _vp)]
 
 
+class KrScaled(ctypes.Structure):
+    _fields_ = [("q", _vp), ("ld", _i64), ("room", _i64), ("scale", _vp), ("lds", _i64)]
+
+
+class KrScaledProduct(ctypes.Structure):
+    _fields_ = [("m", _i64), ("n", _i64), ("k", _i64), ("a", KrScaled), ("b", KrScaled)]
+
+
+_HP, _PP = ctypes.POINTER(KrScaled), ctypes.POINTER(KrScaledProduct)
 _DP = ctypes.POINTER(KrDrop)
 _BP, _GP = ctypes.POINTER(KrBytes), ctypes.POINTER(KrGated)
 _SIGS = {
@@ -112,6 +121,10 @@ _SIGS = {
     "kr_gated_projection_backward": (_i32, [_GP, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _vp,
                                             _sz, _vp]),
     "kr_gated_projection_backward_workspace": (_sz, [_GP]),
+    "kr_scaled_hold": (_i32, [_i32, _i64, _i64, _vp, _i64, _i32, _HP, _HP, _vp]),
+    "kr_scaled_values": (_i32, [_i32, _i64, _i64, _HP, _vp, _i64, _vp]),
+    "kr_scaled_matmul": (_i32, [_PP, _i32, _vp, _i64, _vp, _sz, _vp]),
+    "kr_scaled_matmul_workspace": (_sz, [_PP]),
     "kr_status_string": (ctypes.c_char_p, [_i32]),
     "kr_set_phase_events": (_i32, [_i32, _vp, _vp]),
 }
@@ -739,6 +752,8 @@ def launch_timing_frontier(kind1, kind2, ops, p_static: float, kmax: int, out_ca
 # gated_projection_backward.  The forms in 8-bit integers have no gradient and refuse such
 # inputs.  The backward functions themselves return plain tensors: they are not differentiated again.
 
+# (scaled_hold, scaled_values and scaled_matmul have none either; scaled_linear has.)
+
 _TYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
     lambda dev: torch.cuda.current_stream(dev).cuda_stream)
@@ -1200,3 +1215,181 @@ def gated_projection_backward(dh, x, wg, wu, act: str = "silu"):
                                              dwg.data_ptr(), g.width, dwu.data_ptr(), g.width, at,
                                              wsb, _raw_stream(dev)))
     return dx, dwg, dwu
+
+
+# ---- products of values held in 8-bit floating point ----
+
+_SCALED = 128  # values that share a scale
+
+
+@dataclasses.dataclass
+class Scaled:
+    """Values held in 8-bit floating point with a power of two for each 128 along a row (kr_scaled):
+    q * 2^(byte - 127)."""
+    q: torch.Tensor                # float8_e4m3fn, [..., width]
+    scale: torch.Tensor            # uint8 [blocks of a row][rows up to 128], in the kernels' order
+    room: int = 0                  # columns of a row that may be read, zeros past width; 0: width
+
+
+class ScaledForms(NamedTuple):
+    plain: Optional[Scaled]        # of x
+    crossed: Optional[Scaled]      # of its transpose, [width][rows]
+
+
+def _up(x: int, to: int) -> int:
+    return -(-x // to) * to
+
+
+def _new_scaled(shape, rows: int, width: int):
+    """An empty Scaled, rows of a multiple of 16 bytes, and its kr_scaled."""
+    room, lds = _up(width, 16), _up(rows, _SCALED)
+    q = _new(shape[:-1] + (room,), torch.float8_e4m3fn)
+    scale = _new((_up(width, _SCALED) // _SCALED, lds), torch.uint8)
+    return (Scaled(q if room == width else q[..., :width], scale, room),
+            KrScaled(q.data_ptr(), room, room, scale.data_ptr(), lds))
+
+
+def _held(h: Scaled, name: str, dev: int):
+    """kr_scaled of h, its rows and width, and what has to live."""
+    if not isinstance(h, Scaled):
+        raise TypeError("%s must be Scaled, got %s" % (name, type(h).__name__))
+    _type(h.q, name + ".q", (torch.float8_e4m3fn,))
+    _type(h.scale, name + ".scale", (torch.uint8,))
+    q, n, ld = _rows(h.q, name + ".q", dev)
+    width = q.shape[1]
+    # a copy, and a single row, have no room past their width but the multiple that is theirs
+    room = h.room if q.data_ptr() == h.q.data_ptr() else width
+    room = max(room, width)
+    ld = max(ld, room) if n <= 1 else ld
+    if room > width and n > 0:
+        there = q.untyped_storage().nbytes() - q.storage_offset()
+        if room > ld or (n - 1) * ld + room > there:
+            raise ValueError("%s has no room of %d columns in its rows" % (name, room))
+    s = h.scale
+    if s.get_device() != dev:
+        raise ValueError("%s.scale must be on the current device, got %s" % (name, s.device))
+    blocks = _up(width, _SCALED) // _SCALED
+    if s.dim() != 2 or s.shape[0] != blocks or s.shape[1] < _up(n, _SCALED):
+        raise ValueError("%s.scale must be [%d][%d], got %s"
+                         % (name, blocks, _up(n, _SCALED), tuple(s.shape)))
+    if n and (s.stride(1) != 1 or s.stride(0) % 4 or s.stride(0) < s.shape[1] or s.data_ptr() % 4):
+        s = s.contiguous()
+    if n and s.stride(0) % 4:
+        raise ValueError("%s.scale must have rows of a multiple of 4 bytes" % name)
+    return KrScaled(q.data_ptr(), ld, room, s.data_ptr(), s.stride(0)), n, width, (q, s)
+
+
+def scaled_hold(x, square: bool = False, plain: bool = True, crossed: bool = False) -> ScaledForms:
+    """x [..., width] held in 8-bit floating point, a power of two for each 128 along a row: as it
+    is (plain), and its transpose [width][rows] (crossed).  square: 128 x 128 values share one, so
+    that both forms hold the same values (kr_scaled_hold).  It has no gradient."""
+    _no_gradient("scaled_hold", x)
+    t = _type(x, "x")
+    dev = _here(x, "x")
+    if not plain and not crossed:
+        raise ValueError("one of plain and crossed has to be asked for")
+    xr, n, ldx = _rows(x, "x", dev)
+    width = xr.shape[1]
+    p, pk = _new_scaled(x.shape, n, width) if plain else (None, None)
+    c, ck = _new_scaled((width, n), width, n) if crossed else (None, None)
+    _check("kr_scaled_hold",
+           _lib.kr_scaled_hold(t, n, width, xr.data_ptr(), ldx, int(square), pk, ck,
+                               _raw_stream(dev)))
+    return ScaledForms(p, c)
+
+
+def scaled_values(h: Scaled, dtype=torch.float32) -> torch.Tensor:
+    """The values that h holds, in dtype (kr_scaled_values)."""
+    if dtype not in _TYPES:
+        raise TypeError("dtype must be %s, got %s" % (" or ".join(map(str, _TYPES)), dtype))
+    _type(getattr(h, "q", h), "h.q", (torch.float8_e4m3fn,))
+    dev = _here(h.q, "h.q")
+    k, n, width, keep = _held(h, "h", dev)
+    out = _new(h.q.shape, dtype)
+    _check("kr_scaled_values",
+           _lib.kr_scaled_values(_TYPES[dtype], n, width, k, out.data_ptr(), width,
+                                 _raw_stream(dev)))
+    return out
+
+
+def scaled_matmul(a: Scaled, b: Scaled, dtype=torch.bfloat16) -> torch.Tensor:
+    """a b^T of the values that a [..., k] and b [n][k] hold; the result, [..., n], in dtype
+    (kr_scaled_matmul).  It has no gradient."""
+    if dtype not in _TYPES:
+        raise TypeError("dtype must be %s, got %s" % (" or ".join(map(str, _TYPES)), dtype))
+    _type(getattr(a, "q", a), "a.q", (torch.float8_e4m3fn,))
+    dev = _here(a.q, "a.q")
+    ak, m, k, keep_a = _held(a, "a", dev)
+    bk, n, kb, keep_b = _held(b, "b", dev)
+    if b.q.dim() != 2 or n < 1 or kb != k:
+        raise ValueError("b.q must be [n][%d], got %s" % (k, tuple(b.q.shape)))
+    out = _new(a.q.shape[:-1] + (n,), dtype)
+    p = KrScaledProduct(m, n, k, ak, bk)
+    wsb = _lib.kr_scaled_matmul_workspace(p)
+    ws, at = _scratch(wsb)
+    _check("kr_scaled_matmul",
+           _lib.kr_scaled_matmul(p, _TYPES[dtype], out.data_ptr(), n, at, wsb, _raw_stream(dev)))
+    return out
+
+
+class _ScaledLinear(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, w):
+        ctx.save_for_backward(x, w)
+        return scaled_linear(x, w)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dout):
+        return scaled_linear_backward(dout, *ctx.saved_tensors, need=ctx.needs_input_grad)
+
+
+def _linear_weight(x, w):
+    if not isinstance(w, torch.Tensor) or w.dtype != x.dtype:
+        raise TypeError("w must be Scaled or a tensor of %s like x" % x.dtype)
+    if w.dim() != 2 or w.shape[0] < 1 or w.shape[1] != x.shape[-1]:
+        raise ValueError("w must be [hidden][%d], got %s" % (x.shape[-1], tuple(w.shape)))
+
+
+def scaled_linear(x, w) -> torch.Tensor:
+    """x w^T of x [..., width] and w [hidden][width], both held in 8-bit floating point first: x by
+    rows, w by squares; the result in x's type.  w may be Scaled (a weight that is held once, by
+    scaled_hold(w, square=True).plain); then there is no gradient.  Else the gradient reaches both,
+    holding taken as if it left values as they are."""
+    if isinstance(w, Scaled):
+        _no_gradient("scaled_linear with a weight that is held", x)
+    elif _tracked(x, w):
+        return _ScaledLinear.apply(x, w)
+    _type(x, "x")
+    if not isinstance(w, Scaled):
+        _linear_weight(x, w)
+        w = scaled_hold(w.detach(), square=True).plain
+    return scaled_matmul(scaled_hold(x.detach()).plain, w, x.dtype)
+
+
+def scaled_linear_backward(dout, x, w, need=(True, True)):
+    """(dx, dw) of scaled_linear from its inputs and the gradient dout of its output.  Each of the two
+    products takes operands held along what it sums over: dx = dout w, dout held by rows and w by
+    squares, as forward; dw = dout^T x, both held by columns, 128 rows a block.  None where `need`
+    is false."""
+    _type(x, "x")
+    _linear_weight(x, w)
+    if not isinstance(dout, torch.Tensor) or dout.dtype != x.dtype:
+        raise TypeError("dout must be a tensor of %s" % x.dtype)
+    if dout.shape != x.shape[:-1] + (w.shape[0],):
+        raise ValueError("dout must be %s, got %s" % (tuple(x.shape[:-1]) + (w.shape[0],),
+                                                      tuple(dout.shape)))
+    if x.numel() == 0:
+        return torch.empty_like(x) if need[0] else None, torch.zeros_like(w) if need[1] else None
+    x, w, dout = x.detach(), w.detach(), dout.detach()
+    if not need[0] and not need[1]:
+        return None, None
+    d = scaled_hold(dout, plain=bool(need[0]), crossed=bool(need[1]))
+    dx = dw = None
+    if need[0]:
+        wt = scaled_hold(w, square=True, plain=False, crossed=True).crossed
+        dx = scaled_matmul(d.plain, wt, x.dtype)
+    if need[1]:
+        xt = scaled_hold(x, plain=False, crossed=True).crossed
+        dw = scaled_matmul(d.crossed, xt, x.dtype)
+    return dx, dw

@@ -4,6 +4,7 @@
 
 #include "kr_drop.h"
 #include "kr_gated.h"
+#include "kr_scaled.h"
 
 using namespace kr;
 
@@ -443,4 +444,97 @@ extern "C" kr_status kr_byte_matmul(const kr_bytes *p, int32_t type, void *out, 
     if (!ws_ok(ws, ws_bytes, kr_byte_matmul_workspace(p))) return KR_ECAPACITY;
     Carve c{(char *)ws};
     return bytes_run(p, type, out, ldo, c, (hipStream_t)stream);
+}
+
+// ---- products of values held in 8-bit floating point ----------------------------------------
+
+namespace {
+
+constexpr int64_t kHeldMost = 1 << 30;  // rows and columns of a held matrix
+
+int64_t up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
+
+// A held matrix of rows x width as an argument.
+bool held_ok(const kr_scaled *h, int64_t rows, int64_t width)
+{
+    return h && (rows == 0 || (h->q && h->ld >= h->room && h->room >= width && h->scale &&
+                               (uintptr_t)h->scale % 4 == 0 && h->lds % 4 == 0 &&
+                               h->lds >= up(rows, kScaled)));
+}
+
+HeldMatrix held(const kr_scaled *h)
+{
+    return {(char *)h->q, h->ld, h->room, (uint8_t *)h->scale, h->lds};
+}
+
+bool scaled_ok(const kr_scaled_product *p)
+{
+    return p && p->m >= 0 && p->n >= 1 && p->k >= 1 && held_ok(&p->a, p->m, p->k) &&
+           held_ok(&p->b, p->n, p->k);
+}
+
+bool scaled_fits(const kr_scaled_product *p)
+{
+    return p->m <= kRowsMost && p->n <= kChannelsMost && p->k <= kRowMost && tiles_fit(p->m, p->n);
+}
+
+kr_status scaled_run(const kr_scaled_product *p, int32_t type, void *out, int64_t ldo, Carve &c,
+                     hipStream_t st)
+{
+    if (!out) return KR_OK;
+    const ScaledArgs a{type, p->m, p->n, p->k, held(&p->a), held(&p->b), out, ldo, nullptr};
+    return said(launch_scaled_few(a, st));
+}
+
+}  // namespace
+
+extern "C" kr_status kr_scaled_hold(int32_t type, int64_t rows, int64_t width, const void *x,
+                                    int64_t ldx, int32_t square, const kr_scaled *plain,
+                                    const kr_scaled *crossed, void *stream)
+{
+    if (!type_ok(type) || rows < 0 || width < 1 || (square != 0 && square != 1) || (!plain && !crossed))
+        return KR_EINVAL;
+    if (rows > kHeldMost || width > kHeldMost ||
+        up(rows, kScaled) / kScaled * (up(width, kScaled) / kScaled) > kTilesMost)
+        return KR_EUNSUPPORTED;
+    if (rows == 0) return KR_OK;
+    if (!matrix_ok(x, ldx, width, size_of(type)) ||
+        (plain && (!held_ok(plain, rows, width) || plain->room > up(width, kScaled))) ||
+        (crossed && (!held_ok(crossed, width, rows) || crossed->room > up(rows, kScaled))))
+        return KR_EINVAL;
+    HoldArgs a{rows, width, x, ldx, {}, {}, up(width, kScaled) / kScaled};
+    if (plain) a.plain = held(plain);
+    if (crossed) a.crossed = held(crossed);
+    return said(launch_hold(type, square != 0, a, (hipStream_t)stream));
+}
+
+extern "C" kr_status kr_scaled_values(int32_t type, int64_t rows, int64_t width, const kr_scaled *h,
+                                      void *out, int64_t ldo, void *stream)
+{
+    if (!type_ok(type) || rows < 0 || width < 1 || !held_ok(h, rows, width)) return KR_EINVAL;
+    if (rows > kHeldMost || width > kHeldMost) return KR_EUNSUPPORTED;
+    if (rows == 0) return KR_OK;
+    if (!matrix_ok(out, ldo, width, size_of(type))) return KR_EINVAL;
+    const HeldValuesArgs a{rows, width, held(h), out, ldo};
+    return said(launch_held_values(type, a, (hipStream_t)stream));
+}
+
+extern "C" size_t kr_scaled_matmul_workspace(const kr_scaled_product *p)
+{
+    if (!scaled_ok(p) || !scaled_fits(p) || p->m == 0) return 0;
+    Carve c{nullptr};
+    scaled_run(p, KR_F32, nullptr, 0, c, nullptr);
+    return c.used;
+}
+
+extern "C" kr_status kr_scaled_matmul(const kr_scaled_product *p, int32_t type, void *out, int64_t ldo,
+                                      void *ws, size_t ws_bytes, void *stream)
+{
+    if (!scaled_ok(p) || !type_ok(type)) return KR_EINVAL;
+    if (!scaled_fits(p)) return KR_EUNSUPPORTED;
+    if (p->m == 0) return KR_OK;
+    if (!matrix_ok(out, ldo, p->n, size_of(type)) || (uintptr_t)ws % 16) return KR_EINVAL;
+    if (!ws_ok(ws, ws_bytes, kr_scaled_matmul_workspace(p))) return KR_ECAPACITY;
+    Carve c{(char *)ws};
+    return scaled_run(p, type, out, ldo, c, (hipStream_t)stream);
 }
