@@ -1,6 +1,8 @@
 // C ABI of the transformer-block operators: argument checks, workspace layout and launch
 // order.  Declarations and contracts: include/kareus.h.
+#include <algorithm>
 #include <cmath>
+#include <utility>
 
 #include "kr_drop.h"
 #include "kr_gated.h"
@@ -481,9 +483,24 @@ bool scaled_fits(const kr_scaled_product *p)
 kr_status scaled_run(const kr_scaled_product *p, int32_t type, void *out, int64_t ldo, Carve &c,
                      hipStream_t st)
 {
+    ScaledArgs x{type, p->m, p->n, p->k, held(&p->a), held(&p->b), out, ldo, nullptr};
+    if (p->m <= kFewRows) return out ? said(launch_scaled_few(x, st)) : KR_OK;
+    // rows to a multiple of 16 bytes: theirs, where they have that room
+    const int64_t wide = padded(p->k);
+    const Laid a(p->a.q, p->a.ld, p->m, p->a.room >= wide ? wide : p->k, c);
+    const Laid b(p->b.q, p->b.ld, p->n, p->b.room >= wide ? wide : p->k, c);
+    x.part = c.take((int64_t)scaled_part(type, p->m, p->n, p->k));
     if (!out) return KR_OK;
-    const ScaledArgs a{type, p->m, p->n, p->k, held(&p->a), held(&p->b), out, ldo, nullptr};
-    return said(launch_scaled_few(a, st));
+    PadArgs pads{};
+    a.add_to(pads);
+    b.add_to(pads);
+    if (const hipError_t e = launch_pad(pads, st); e != hipSuccess) return said(e);
+    for (const auto &to : {std::make_pair(&x.a, &a), std::make_pair(&x.b, &b)}) {
+        to.first->q = (char *)to.second->op.p;
+        to.first->ld = to.second->op.ld;
+        to.first->bytes = to.second->op.bytes;
+    }
+    return said(launch_scaled(x, st));
 }
 
 }  // namespace
@@ -522,9 +539,13 @@ extern "C" kr_status kr_scaled_values(int32_t type, int64_t rows, int64_t width,
 extern "C" size_t kr_scaled_matmul_workspace(const kr_scaled_product *p)
 {
     if (!scaled_ok(p) || !scaled_fits(p) || p->m == 0) return 0;
-    Carve c{nullptr};
-    scaled_run(p, KR_F32, nullptr, 0, c, nullptr);
-    return c.used;
+    size_t most = 0;
+    for (const int32_t type : {KR_F32, KR_BF16}) {
+        Carve c{nullptr};
+        scaled_run(p, type, nullptr, 0, c, nullptr);
+        most = std::max(most, c.used);
+    }
+    return most;
 }
 
 extern "C" kr_status kr_scaled_matmul(const kr_scaled_product *p, int32_t type, void *out, int64_t ldo,

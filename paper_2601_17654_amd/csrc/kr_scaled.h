@@ -88,6 +88,11 @@ struct ScaledArgs {
     int64_t ldo;
     void *part;
 };
+// Bytes of ScaledArgs::part.
+size_t scaled_part(int out_type, int64_t m, int64_t n, int64_t k);
+// a, b: 16-byte aligned, rows of a multiple of 16 bytes, zeros past k.
+hipError_t launch_scaled(const ScaledArgs &a, hipStream_t st);
+// Up to 32 rows, any alignment, k bytes of each row; no part.
 hipError_t launch_scaled_few(const ScaledArgs &a, hipStream_t st);
 
 }  // namespace kr

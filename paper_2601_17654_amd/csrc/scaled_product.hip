@@ -129,24 +129,400 @@ __global__ __launch_bounds__(NW * 64) void scaled_few_kernel(ScaledArgs a)
     store8((T *)a.out + token * a.ldo, (int)n0 + h, (int)a.n, v);
 }
 
-template <typename T>
-hipError_t few(const ScaledArgs &all, hipStream_t st)
+// ---- tiles ---------------------------------------------------------------------------------
+
+struct E4m3 {};  // of Mma: 32-bit sums
+
+struct TileArgs {
+    MmaArgs p;
+    const uint8_t *scale[2];  // of a, of b
+    int64_t lds[2];           // bytes from one block's to the next
+    int64_t rows[2];          // of a block that may be read
+};
+
+// A block's copies to LDS: the operands' tiles as in mma_kernel, 16 bytes a lane, and the step's scale
+// bytes, 4 a lane: the first wave those of a's tile, the second of b's, each to 256 bytes of its own (the
+// others copy an empty buffer, so that every wave counts the same copies).
+template <int BM, int BN>
+struct Copies {
+    typedef TileLoader<false, BM, 4> LoadA;
+    typedef TileLoader<false, BN, 4> LoadB;
+    static constexpr int N = LoadA::N + LoadB::N + 1;  // of a wave and step, the scales last
+    struct Lds {
+        char tile[2][(BM + BN) * kStep];
+        uint8_t scale[2][4][256];
+    };
+    LoadA la;
+    LoadB lb;
+    i32x4 ra, rb, rs;
+    uint64_t at;       // of the step's scales
+    int64_t ld;
+    int records, k_left, step, end, wave;
+    uint32_t lane4;
+
+    __device__ void init(const TileArgs &a, int64_t m0, int64_t n0, int begin, int end_, int wave_,
+                         int lane)
+    {
+        wave = wave_;
+        step = begin;
+        end = end_;
+        la.init(a.p.a[0], m0, wave, lane, MapSame());
+        lb.init(a.p.b[0], n0, wave, lane, MapSame());
+        la.aim(begin, 0);
+        lb.aim(begin, 0);
+        const bool odd = wave & 1;
+        const int64_t first = odd ? n0 : m0, left = (odd ? a.rows[1] : a.rows[0]) - first;
+        ld = odd ? a.lds[1] : a.lds[0];
+        at = (uint64_t)((odd ? a.scale[1] : a.scale[0]) + begin * ld + first);
+        records = wave < 2 ? (int)(left < 256 ? left : 256) : 0;
+        lane4 = lane * 4;
+        k_left = (int)a.p.k_bytes - begin * kStep;
+        la.bound(k_left);
+        lb.bound(k_left);
+        ra = la.buffer(begin < end);
+        rb = lb.buffer(begin < end);
+        scales();
+    }
+    __device__ void scales()
+    {
+        i32x4 x{(int)at, (int)(at >> 32) & 0xFFFF, step < end ? records : 0, 0x00020000};
+        here(x);
+        rs = x;
+    }
+    // Goes one step on, in eight parts that stand between matrix instructions.
+    static constexpr int PARTS = 8;
+    __device__ __attribute__((always_inline)) void part(int p)
+    {
+        if (p == 0) {
+            ++step;
+            here(step);
+        }
+        if (p == 1) la.next_at(false, 0);
+        if (p == 2) la.next_rest(false);
+        if (p == 3) ra = la.buffer(step < end);
+        if (p == 4) {
+            lb.next_at(false, 0);
+            lb.next_rest(false);
+        }
+        if (p == 5) rb = lb.buffer(step < end);
+        if (p == 6) {
+            here(k_left);
+            k_left -= kStep;
+            la.bound(k_left);
+            lb.bound(k_left);
+        }
+        if (p == 7) {
+            here(at);
+            at += ld;
+            scales();
+        }
+    }
+    __device__ uint32_t from(int j) const
+    {
+        return j < LoadA::N ? la.from(j) : j < N - 1 ? lb.from(j - LoadA::N) : lane4;
+    }
+    __device__ const char *to(int j, Lds &lds, int buf) const
+    {
+        if (j == N - 1) return (const char *)lds.scale[buf][wave];
+        return j < LoadA::N ? la.to(j, lds.tile[buf], wave)
+                            : lb.to(j - LoadA::N, lds.tile[buf] + BM * kStep, wave);
+    }
+    __device__ __attribute__((always_inline)) void go(int j, uint32_t off, uint32_t m0) const
+    {
+        if (j == N - 1)
+            asm volatile("buffer_load_dword %0, %1, 0 offen lds" ::"v"(off), "s"(rs), "{m0}"(m0) : "memory");
+        else
+            copy_go(off, j < LoadA::N ? ra : rb, m0);
+    }
+    __device__ __attribute__((always_inline)) void all(Lds &lds, int buf) const
+    {
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            const uint32_t m0 = copy_ready(from(j), to(j, lds, buf));
+            asm volatile("s_nop 0");
+            go(j, from(j), m0);
+        }
+    }
+};
+
+// Scale bytes of a wave's 128 rows (tile t of 16 at byte t) or 64 (the half of 128 that is its).
+template <int ROWS>
+__device__ inline i32x2 read_scales(const uint8_t *scale, int part, int lane)
 {
-    const unsigned blocks = (unsigned)((all.n + 15) / 16);
-    ScaledArgs a = all;
-    for (int64_t m0 = 0; m0 < all.m; m0 += 32) {
-        a.m = all.m - m0 < 32 ? all.m - m0 : 32;
-        a.a.q = all.a.q + m0 * all.a.ld;
-        // 32 rows on: two 16-row tiles
-        a.a.scale = all.a.scale + m0 / kScaled * kScaled + m0 % kScaled / 16;
-        a.out = (T *)all.out + m0 * all.ldo;
-        if (a.m <= 16) scaled_few_kernel<4, 1, T><<<blocks, 256, 0, st>>>(a);
-        else scaled_few_kernel<4, 2, T><<<blocks, 256, 0, st>>>(a);
+    if (ROWS == 128) return *(const i32x2 *)(scale + part * 128 + lane % 16 * 8);
+    return i32x2{*(const int *)(scale + lane % 16 * 8 + part * 4), 0};
+}
+
+// c += a b with the scales in bytes SA of sa and SB of sb, in place as mma_in_place().
+template <int SA, int SB>
+__device__ inline void scaled_in_place(const i32x8 &a, const i32x8 &b, f32x4 &c, int sa, int sb)
+{
+    asm volatile("v_mfma_scale_f32_16x16x128_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel:[%5,%6,0] op_sel_hi:[%7,%8,0]"
+                 : "+a"(c)
+                 : "v"(a), "v"(b), "v"(sa), "v"(sb), "n"(SA & 1), "n"(SB & 1), "n"(SA >> 1), "n"(SB >> 1));
+}
+
+// When a step's work stands among its matrix instructions: reads one tile of 16 rows (two reads of
+// LDS) each `apart` of them; from `free` on every wave has its step in registers, and the copies of the
+// step after next go over it, those started before instruction x being copies(x); from `next` on the next
+// step's tiles have arrived.
+template <int BLOCK>
+struct When;
+template <>
+struct When<64> {
+    static constexpr int apart = 2, free = 20, next = 40;
+    static constexpr int copies(int x)
+    {
+        return x <= free ? 0 : ((x - free) * 2 + 4) / 5 < 17 ? ((x - free) * 2 + 4) / 5 : 17;
+    }
+};
+template <>
+struct When<16> {
+    static constexpr int apart = 1, free = 6, next = 10;
+    static constexpr int copies(int x) { return x <= free ? 0 : x - free < 9 ? x - free : 9; }
+};
+
+// Two steps' tiles are in LDS, and the registers hold one step, no more: its sums take half of them
+// already.  A step's products are four quarters, halves of a's rows by halves of b's, and the order of b's
+// halves turns with each step (P), so that a half is overwritten by the next step's as soon as its last
+// quarter is done, and is wanted again a quarter later at the soonest:
+//   P = 0: a0 b0, a0 b1, a1 b1, a1 b0     P = 1: a0 b1, a0 b0, a1 b0, a1 b1
+// In a step's first quarter come the reads of its second b half and of a1, from `next` on those of the next
+// step's a0 and of its first b half.
+template <int BM, int BN, typename Out>
+__global__ __launch_bounds__(256) void scaled_tile_kernel(TileArgs a, Out out)
+{
+    constexpr int WM = 2, WN = 2, RM = BM / WM, RN = BN / WN, TM = RM / 16, TN = RN / 16;
+    constexpr int BLOCK = TM * TN, QUARTER = BLOCK / 4, HM = TM / 2, HN = TN / 2;
+    typedef When<BLOCK> W;
+    typedef Copies<BM, BN> C;
+    static_assert(HM == HN && W::free >= 2 * HM * W::apart && W::next >= 2 * QUARTER &&
+                      W::next + HM * W::apart >= 3 * QUARTER && W::next + 2 * HM * W::apart <= BLOCK &&
+                      2 * HM * W::apart <= QUARTER * 2 && HM * W::apart <= QUARTER &&
+                      W::copies(BLOCK) == C::N,
+                  "the reads and copies fit the step");
+    __shared__ __align__(1024) typename C::Lds lds;
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int wm = wave / WN, wn = wave % WN;
+    int tm, tn, split;
+    tile_of(a.p, &tm, &tn, &split);
+    const int64_t m0 = (int64_t)tm * BM, n0 = (int64_t)tn * BN;
+    const int begin = split * a.p.per_split, end = min(begin + a.p.per_split, a.p.steps);
+
+    C c;
+    c.init(a, m0, n0, begin, end, wave, lane);
+    TileReader<false, BM> reader;
+    reader.init(lane);
+    f32x4 acc[TM][TN];
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j) acc[i][j] = f32x4{0, 0, 0, 0};
+    i32x8 fa[TM], fb[TN];
+    i32x2 sa[2], sb[2];
+    auto tile = [&](const char *at, int first) __attribute__((always_inline)) {
+        return __builtin_shufflevector(reader.read(at, first, 0), reader.read(at, first, 1), 0, 1, 2, 3, 4,
+                                       5, 6, 7);
+    };
+    auto read_a = [&](int buf, int i) __attribute__((always_inline)) {
+        fa[i] = tile(lds.tile[buf], wm * RM + i * 16);
+    };
+    auto read_b = [&](int buf, int j) __attribute__((always_inline)) {
+        fb[j] = tile(lds.tile[buf] + BM * kStep, wn * RN + j * 16);
+    };
+    auto read_s = [&](int buf, int p) __attribute__((always_inline)) {
+        sa[p] = read_scales<RM>(lds.scale[buf][0], wm, lane);
+        sb[p] = read_scales<RN>(lds.scale[buf][1], wn, lane);
+    };
+
+    c.all(lds, 0);
+#pragma unroll
+    for (int p = 0; p < C::PARTS; ++p) c.part(p);
+    c.all(lds, 1);
+    arrived<C::N>();
+    read_s(0, 0);
+#pragma unroll
+    for (int i = 0; i < HM; ++i) {
+        read_a(0, i);
+        read_b(0, i);
+    }
+    sums_done(acc);
+    auto body = [&](auto parity) __attribute__((always_inline)) {
+        constexpr int P = decltype(parity)::value;
+        uint32_t off = 0, m0 = 0;
+        each(Count<BLOCK>(), [&](auto at_x) __attribute__((always_inline)) {
+            constexpr int x = decltype(at_x)::value, A = W::apart;
+            if (x % A == 0 && x / A < HM) read_b(P, (1 - P) * HN + x / A);
+            if (x % A == 0 && x / A >= HM && x / A < 2 * HM) read_a(P, x / A);
+            if (x == W::free) read_done();
+            if (x == W::next) arrived<W::copies(W::next)>();
+#pragma unroll
+            for (int p = 0; p < C::PARTS; ++p)
+                if (p * W::free / C::PARTS == x) c.part(p);
+            if (W::copies(x + 1) > W::copies(x)) c.go(W::copies(x), off, m0);
+            if (x + 1 < BLOCK && W::copies(x + 2) > W::copies(x + 1)) {
+                off = c.from(W::copies(x + 1));
+                m0 = copy_ready(off, c.to(W::copies(x + 1), lds, P));
+            }
+            if (x >= W::next && (x - W::next) % A == 0) {
+                constexpr int r = (x - W::next) / A;
+                if (r == 0) read_s(1 - P, 1 - P);
+                if (r < HM) read_a(1 - P, r);
+                if (r >= HM && r < 2 * HM) read_b(1 - P, (1 - P) * HN + r - HM);
+            }
+            constexpr int q = x / QUARTER, y = x % QUARTER, ih = q / 2;
+            constexpr int jh = q == 0 || q == 3 ? P : 1 - P;
+            constexpr int jj = y / HM, ii = jj % 2 ? HM - 1 - y % HM : y % HM;  // to and fro
+            constexpr int i = ih * HM + ii, j = jh * HN + jj;
+            scaled_in_place<j % 4, i % 4>(fb[j], fa[i], acc[i][j], sb[P][j / 4], sa[P][i / 4]);
+            __builtin_amdgcn_sched_barrier(0);
+        });
+    };
+    int s = begin;
+    for (; s + 1 < end; s += 2) {
+        body(std::integral_constant<int, 0>());
+        body(std::integral_constant<int, 1>());
+    }
+    if (s < end) body(std::integral_constant<int, 0>());
+    sums_done(acc);
+    read_done();
+    arrived<0>();  // the tiles' LDS is free, and no copy will write to it
+    put_tile<BM, BN, WM, WN>(E4m3(), a.p, out, acc, lds.tile[0], m0, n0, wave, split, lane);
+}
+
+// The same for outputs of 32 bits: a step's values go to bfloat16 on their way to the instructions.  The
+// compiler places these, and two blocks a CU fill each other's waits.
+template <typename Out>
+__global__ __launch_bounds__(256) void scaled_wide_kernel(TileArgs a, Out out)
+{
+    constexpr int BM = 128, BN = 128, WN = 2, TM = 4, TN = 4;
+    typedef Copies<BM, BN> C;
+    __shared__ __align__(1024) typename C::Lds lds;
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int wm = wave / WN, wn = wave % WN;
+    int tm, tn, split;
+    tile_of(a.p, &tm, &tn, &split);
+    const int64_t m0 = (int64_t)tm * BM, n0 = (int64_t)tn * BN;
+    const int begin = split * a.p.per_split, end = min(begin + a.p.per_split, a.p.steps);
+    C c;
+    c.init(a, m0, n0, begin, end, wave, lane);
+    TileReader<false, BM> reader;
+    reader.init(lane);
+    f32x4 acc[TM][TN];
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j) acc[i][j] = f32x4{0, 0, 0, 0};
+    auto tile = [&](const char *at, int first) __attribute__((always_inline)) {
+        return __builtin_shufflevector(reader.read(at, first, 0), reader.read(at, first, 1), 0, 1, 2, 3, 4,
+                                       5, 6, 7);
+    };
+    c.all(lds, 0);
+#pragma unroll
+    for (int p = 0; p < C::PARTS; ++p) c.part(p);
+    c.all(lds, 1);
+    for (int s = begin; s < end; ++s) {
+        const int buf = (s - begin) & 1;
+        arrived<C::N>();
+        const int sa = read_scales<64>(lds.scale[buf][0], wm, lane)[0];
+        const int sb = read_scales<64>(lds.scale[buf][1], wn, lane)[0];
+        i32x8 qa[TM], qb[TN];
+#pragma unroll
+        for (int i = 0; i < TM; ++i) qa[i] = tile(lds.tile[buf], wm * 64 + i * 16);
+#pragma unroll
+        for (int j = 0; j < TN; ++j) qb[j] = tile(lds.tile[buf] + BM * kStep, wn * 64 + j * 16);
+        read_done();
+#pragma unroll
+        for (int p = 0; p < C::PARTS; ++p) c.part(p);
+        c.all(lds, buf);
+        auto byte = [](int x, int t) { return x >> (8 * t) & 255; };
+        const Values<true> va[TM] = {{qa[0], byte(sa, 0)}, {qa[1], byte(sa, 1)}, {qa[2], byte(sa, 2)},
+                                     {qa[3], byte(sa, 3)}};
+#pragma unroll
+        for (int j = 0; j < TN; ++j) {
+            const Values<true> vb(qb[j], byte(sb, j));
+#pragma unroll
+            for (int i = 0; i < TM; ++i) acc[i][j] = mma_values(vb, va[i], acc[i][j]);
+        }
+    }
+    read_done();
+    arrived<0>();  // the tiles' LDS is free, and no copy will write to it
+    put_tile<BM, BN, 2, WN>(E4m3(), a.p, out, acc, lds.tile[0], m0, n0, wave, split, lane);
+}
+
+MmaPlan plan_of(int out_type, int64_t m, int64_t n, int steps)
+{
+    MmaPlan p = mma_plan(m, n, 1, steps);
+    if (out_type == KR_F32 && p.large) {  // small tiles only
+        p.large = false;
+        p.tiles_m = (int)((m + 127) / 128);
+        p.tiles_n = (int)((n + 127) / 128);
+    }
+    return p;
+}
+
+template <typename T>
+hipError_t tiles(const ScaledArgs &a, hipStream_t st)
+{
+    TileArgs x{};
+    x.p.a[0] = Operand{a.a.q, a.a.ld, a.m, a.a.bytes};
+    x.p.b[0] = Operand{a.b.q, a.b.ld, a.n, a.b.bytes};
+    x.p.m = (int)a.m;
+    x.p.n = (int)a.n;
+    x.p.k_bytes = a.a.bytes;
+    x.p.steps = (int)((a.k + kScaled - 1) / kScaled);
+    x.p.pairs = 1;
+    const MmaPlan p = plan_of(a.out_type, a.m, a.n, x.p.steps);
+    x.p.tiles_m = p.tiles_m;
+    x.p.tiles_n = p.tiles_n;
+    x.p.splits = p.splits;
+    x.p.per_split = p.per_split;
+    x.p.part = (float *)a.part;
+    for (int i = 0; i < 2; ++i) {
+        const HeldMatrix &h = i ? a.b : a.a;
+        x.scale[i] = h.scale;
+        x.lds[i] = h.lds;
+        x.rows[i] = ((i ? a.n : a.m) + kScaled - 1) / kScaled * kScaled;
+    }
+    const PutAs<T> out{(T *)a.out, a.ldo, (int)a.n};
+    const unsigned blocks = (unsigned)(p.tiles_m * p.tiles_n * p.splits);
+    if constexpr (sizeof(T) == 4)
+        scaled_wide_kernel<<<blocks, 256, 0, st>>>(x, out);
+    else if (p.large)
+        scaled_tile_kernel<256, 256><<<blocks, 256, 0, st>>>(x, out);
+    else
+        scaled_tile_kernel<128, 128><<<blocks, 256, 0, st>>>(x, out);
+    if (p.splits > 1) {
+        const int64_t threads = a.m * ((a.n + 7) / 8);
+        mma_join_kernel<E4m3><<<(unsigned)((threads + 255) / 256), 256, 0, st>>>(x.p, out);
     }
     return hipGetLastError();
 }
 
+template <typename T>
+hipError_t few(const ScaledArgs &a, hipStream_t st)
+{
+    const unsigned blocks = (unsigned)((a.n + 15) / 16);
+    if (a.m <= 16) scaled_few_kernel<4, 1, T><<<blocks, 256, 0, st>>>(a);
+    else scaled_few_kernel<4, 2, T><<<blocks, 256, 0, st>>>(a);
+    return hipGetLastError();
+}
+
 }  // namespace
+
+size_t scaled_part(int out_type, int64_t m, int64_t n, int64_t k)
+{
+    return (size_t)plan_of(out_type, m, n, (int)((k + kScaled - 1) / kScaled)).part_bytes;
+}
+
+hipError_t launch_scaled(const ScaledArgs &a, hipStream_t st)
+{
+    if (a.out_type == KR_F32) return tiles<float>(a, st);
+    if (a.out_type == KR_F16) return tiles<f16>(a, st);
+    return tiles<bf16>(a, st);
+}
 
 hipError_t launch_scaled_few(const ScaledArgs &a, hipStream_t st)
 {
