@@ -45,6 +45,33 @@ inline bool with_shape(Shape s, F f)
     return false;
 }
 
+// load_row and store_row for rows of a whole number of vectors (WHOLE), which need no shifts and no
+// element by element end: the layer norm's gradient below takes 30 registers less with them.
+template <bool WHOLE, typename T>
+__device__ inline Pack<T, kVec<T>> load_part(const T *row, int c, int width)
+{
+    if (!WHOLE) return load_row(row, c, width);
+    Pack<T, kVec<T>> x = load16(row + min(c, width - kVec<T>));
+    if (c >= width) {
+#pragma unroll
+        for (int e = 0; e < kVec<T>; ++e) x.v[e] = (T)0;
+    }
+    return x;
+}
+
+template <bool WHOLE, typename T>
+__device__ inline void store_part(T *row, int c, int width, const float *f)
+{
+    if (!WHOLE) {
+        store_row(row, c, width, f);
+    } else if (c < width) {
+        Pack<T, kVec<T>> x;
+#pragma unroll
+        for (int e = 0; e < kVec<T>; ++e) x.v[e] = (T)f[e];
+        store16(row + c, x);
+    }
+}
+
 // Rows of one launch: a grid has fewer than 2^32 threads.
 constexpr int64_t kRowsPerLaunch = 1 << 21;
 

@@ -14,11 +14,53 @@ namespace kr {
 
 namespace {
 
-template <typename T, int TPR, int FPT, bool DROP>
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+
+// x of the lane that is N before in its 16, in a ring.
+template <int N>
+__device__ inline float ring(float x)
+{
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x120 + N, 0xF, 0xF, true));
+}
+
+// Sum over groups of 16 lanes, in every one of them; the pairs are the same seen from either, so
+// that all have the same bits.
+__device__ inline float sum16(float x)
+{
+    x += ring<8>(x);
+    x += ring<4>(x);
+    x += ring<2>(x);
+    return x + ring<1>(x);
+}
+
+// Sums over the TPR threads that share a row, in an order of its own: 16 lanes, those of a wave, then
+// the waves' by 16 lanes again (read one by one, 16 waves' pairs of sums take 32 registers at once).
+// `part`: as row_sum's.
+template <int TPR, int N>
+__device__ inline void row_sums(float (&x)[N], float (*part)[N])
+{
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+        x[n] = sum16(x[n]);
+        if (TPR > 16) x[n] += __shfl_xor(x[n], 16);
+        if (TPR > 32) x[n] += __shfl_xor(x[n], 32);
+    }
+    if (TPR <= 64) return;
+    const int lane = threadIdx.x & 63;
+    if (lane == 0) {
+#pragma unroll
+        for (int n = 0; n < N; ++n) part[threadIdx.x >> 6][n] = x[n];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int n = 0; n < N; ++n) x[n] = sum16(lane % 16 < TPR / 64 ? part[lane % 16][n] : 0.0f);
+}
+
+template <typename T, int TPR, int FPT, bool DROP, bool WHOLE>
 __global__ __launch_bounds__(kBlock<TPR>) void layer_norm_kernel(LayerNormArgs a)
 {
     constexpr int V = kVec<T>, NV = FPT / V, RPB = kBlock<TPR> / TPR;
-    __shared__ float part[2][TPR > 64 ? TPR / 64 : 1];
+    __shared__ float part[2][TPR > 64 ? TPR / 64 : 1][1];
     const int t = threadIdx.x % TPR;
     const int64_t row = (int64_t)blockIdx.x * RPB + threadIdx.x / TPR;
     if (RPB > 1 && row >= a.rows) return;  // whole rows' threads, and such rows take no barrier
@@ -27,16 +69,16 @@ __global__ __launch_bounds__(kBlock<TPR>) void layer_norm_kernel(LayerNormArgs a
     float s[NV][V];
     Pack<T, V> xs[NV], rs[NV], ws[NV], bs[NV];
 #pragma unroll
-    for (int j = 0; j < NV; ++j) xs[j] = load_row(x, (j * TPR + t) * V, a.width);
+    for (int j = 0; j < NV; ++j) xs[j] = load_part<WHOLE>(x, (j * TPR + t) * V, a.width);
     if (r) {
 #pragma unroll
-        for (int j = 0; j < NV; ++j) rs[j] = load_row(r, (j * TPR + t) * V, a.width);
+        for (int j = 0; j < NV; ++j) rs[j] = load_part<WHOLE>(r, (j * TPR + t) * V, a.width);
     }
 #pragma unroll
-    for (int j = 0; j < NV; ++j) ws[j] = load_row((const T *)a.w, (j * TPR + t) * V, a.width);
+    for (int j = 0; j < NV; ++j) ws[j] = load_part<WHOLE>((const T *)a.w, (j * TPR + t) * V, a.width);
     if (a.b) {
 #pragma unroll
-        for (int j = 0; j < NV; ++j) bs[j] = load_row((const T *)a.b, (j * TPR + t) * V, a.width);
+        for (int j = 0; j < NV; ++j) bs[j] = load_part<WHOLE>((const T *)a.b, (j * TPR + t) * V, a.width);
     }
 #pragma unroll
     for (int j = 0; j < NV; ++j) floats(xs[j], s[j]);
@@ -55,22 +97,24 @@ __global__ __launch_bounds__(kBlock<TPR>) void layer_norm_kernel(LayerNormArgs a
     if (a.sum) {
 #pragma unroll
         for (int j = 0; j < NV; ++j)
-            store_row((T *)a.sum + row * a.lds, (j * TPR + t) * V, a.width, s[j]);
+            store_part<WHOLE>((T *)a.sum + row * a.lds, (j * TPR + t) * V, a.width, s[j]);
     }
-    float total = 0.0f, squares = 0.0f;  // past the row's end there are zeros
+    float total[1] = {}, squares[1] = {};  // past the row's end there are zeros
 #pragma unroll
     for (int j = 0; j < NV; ++j)
 #pragma unroll
-        for (int e = 0; e < V; ++e) total += s[j][e];
-    const float m = row_sum<TPR>(total, part[0]) / (float)a.width;
+        for (int e = 0; e < V; ++e) total[0] += s[j][e];
+    row_sums<TPR>(total, part[0]);
+    const float m = total[0] / (float)a.width;
 #pragma unroll
     for (int j = 0; j < NV; ++j)
 #pragma unroll
         for (int e = 0; e < V; ++e) {
-            s[j][e] = (j * TPR + t) * V + e < a.width ? s[j][e] - m : 0.0f;
-            squares = fmaf(s[j][e], s[j][e], squares);
+            s[j][e] = (j * TPR + t) * V + (WHOLE ? 0 : e) < a.width ? s[j][e] - m : 0.0f;
+            squares[0] = fmaf(s[j][e], s[j][e], squares[0]);
         }
-    const float f = 1.0f / sqrtf(row_sum<TPR>(squares, part[1]) / (float)a.width + a.eps);
+    row_sums<TPR>(squares, part[1]);
+    const float f = 1.0f / sqrtf(squares[0] / (float)a.width + a.eps);
     if (t == 0) {
         if (a.mean) a.mean[row] = m;
         if (a.rstd) a.rstd[row] = f;
@@ -82,7 +126,7 @@ __global__ __launch_bounds__(kBlock<TPR>) void layer_norm_kernel(LayerNormArgs a
             s[j][e] = s[j][e] * f * (float)ws[j].v[e];
             if (a.b) s[j][e] += (float)bs[j].v[e];
         }
-        store_row((T *)a.out + row * a.ldo, (j * TPR + t) * V, a.width, s[j]);
+        store_part<WHOLE>((T *)a.out + row * a.ldo, (j * TPR + t) * V, a.width, s[j]);
     }
 }
 
@@ -143,37 +187,28 @@ __global__ __launch_bounds__(1024) void layer_norm_long_kernel(LayerNormArgs a)
     }
 }
 
-// Two sums over the TPR threads that share a row, as row_sum adds one.
-template <int TPR>
-__device__ inline float2 row_sums(float2 x, float2 *part)
+// The compiler knows nothing of x from here on.
+template <typename T>
+__device__ inline void anew(Pack<T, kVec<T>> &x)
 {
-#pragma unroll
-    for (int o = TPR < 64 ? TPR / 2 : 32; o; o >>= 1) {
-        x.x += __shfl_xor(x.x, o);
-        x.y += __shfl_xor(x.y, o);
-    }
-    if (TPR <= 64) return x;
-    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = x;
-    __syncthreads();
-    float2 s = make_float2(0.0f, 0.0f);
-#pragma unroll
-    for (int i = 0; i < TPR / 64; ++i) {
-        s.x += part[i].x;
-        s.y += part[i].y;
-    }
-    return s;
+    i32x4 v = __builtin_bit_cast(i32x4, x);
+    asm("" : "+v"(v));
+    x = __builtin_bit_cast(Pack<T, kVec<T>>, v);
 }
 
 // Gradients, with h = (s - m) f, g = dn w:  ds = f (g - mean(g) - h mean(g h)) + dsum,
 // dx = D(ds),  dw = sum dn h,  db = sum dn.
 // A block takes rows in turn and keeps its shares of dw and db in registers; the blocks' shares
 // are added by layer_norm_weight_kernel in a fixed order.
-template <typename T, int TPR, int FPT, bool DROP>
-__global__ __launch_bounds__(kBlock<TPR>) void layer_norm_back_kernel(LayerNormBackArgs a)
+template <typename T, int TPR, int FPT, bool DROP, bool WHOLE>
+__global__ __launch_bounds__(kBlock<TPR>) __attribute__((amdgpu_waves_per_eu(4))) void
+layer_norm_back_kernel(LayerNormBackArgs a)
 {
     constexpr int V = kVec<T>, NV = FPT / V, RPB = kBlock<TPR> / TPR;
-    constexpr bool AHEAD = FPT == 8;  // the next row's loads: with 16 there are no registers left
-    __shared__ float2 part[2][TPR > 64 ? TPR / 64 : 1];
+    // the next row's loads: with 16, or with dropout between odd rows in 32 bits, there are no
+    // registers left
+    constexpr bool AHEAD = FPT == 8 && (WHOLE || !DROP || sizeof(T) == 2);
+    __shared__ float part[2][TPR > 64 ? TPR / 64 : 1][2];
     __shared__ float share[RPB > 1 ? RPB * TPR * FPT : 1];
     const int t = threadIdx.x % TPR, sub = threadIdx.x / TPR;
     const uint64_t seed = DROP ? drop_seed(a.drop) : 0;
@@ -181,7 +216,7 @@ __global__ __launch_bounds__(kBlock<TPR>) void layer_norm_back_kernel(LayerNormB
     Pack<T, V> ws[NV];
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-        ws[j] = load_row((const T *)a.w, (j * TPR + t) * V, a.width);
+        ws[j] = load_part<WHOLE>((const T *)a.w, (j * TPR + t) * V, a.width);
 #pragma unroll
         for (int e = 0; e < V; ++e) dw[j][e] = db[j][e] = 0.0f;
     }
@@ -192,10 +227,10 @@ __global__ __launch_bounds__(kBlock<TPR>) void layer_norm_back_kernel(LayerNormB
         f = a.rstd[row];
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
-            hs[j] = load_row((const T *)a.s + row * a.lds, (j * TPR + t) * V, a.width);
-            gs[j] = load_row((const T *)a.dout + row * a.ldo, (j * TPR + t) * V, a.width);
+            hs[j] = load_part<WHOLE>((const T *)a.s + row * a.lds, (j * TPR + t) * V, a.width);
+            gs[j] = load_part<WHOLE>((const T *)a.dout + row * a.ldo, (j * TPR + t) * V, a.width);
             if (a.dsum)
-                ds[j] = load_row((const T *)a.dsum + row * a.ldd, (j * TPR + t) * V, a.width);
+                ds[j] = load_part<WHOLE>((const T *)a.dsum + row * a.ldd, (j * TPR + t) * V, a.width);
         }
     };
     int turn = 0;
@@ -204,41 +239,50 @@ __global__ __launch_bounds__(kBlock<TPR>) void layer_norm_back_kernel(LayerNormB
     if (AHEAD && row < a.rows) load(row);
     for (; row < a.rows; row += stride, turn ^= 1) {
         if (!AHEAD) load(row);
-        float h[NV][V], g[NV][V], d[NV][V];
+        Pack<T, V> hn[NV], gn[NV], dn[NV];
         const float m0 = m, f0 = f;
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
-            floats(hs[j], h[j]);
-            floats(gs[j], g[j]);
-#pragma unroll
-            for (int e = 0; e < V; ++e) d[j][e] = a.dsum ? (float)ds[j].v[e] : 0.0f;
+            hn[j] = hs[j];
+            gn[j] = gs[j];
+            dn[j] = ds[j];
         }
         if (AHEAD && row + stride < a.rows) load(row + stride);
-        float2 c = make_float2(0.0f, 0.0f);  // past the row's end g is 0
-#pragma unroll
-        for (int j = 0; j < NV; ++j)
-#pragma unroll
-            for (int e = 0; e < V; ++e) {
-                h[j][e] = (h[j][e] - m0) * f0;
-                dw[j][e] = fmaf(g[j][e], h[j][e], dw[j][e]);
-                db[j][e] += g[j][e];
-                g[j][e] *= (float)ws[j].v[e];
-                c.x += g[j][e];
-                c.y = fmaf(g[j][e], (j * TPR + t) * V + e < a.width ? h[j][e] : 0.0f, c.y);
-            }
-        // two sets of words in turn: one barrier a row keeps a set until all have read it
-        c = row_sums<TPR>(c, part[turn]);
-        c.x /= (float)a.width;
-        c.y /= (float)a.width;
+        float c[2] = {};  // past the row's end g is 0
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
 #pragma unroll
-            for (int e = 0; e < V; ++e) d[j][e] += (g[j][e] - c.x - h[j][e] * c.y) * f0;
-            store_row((T *)a.dres + row * a.ldr, (j * TPR + t) * V, a.width, d[j]);
-            if (DROP) {
-                drop_out<V>(a.drop, seed, (j * TPR + t) * V, (uint32_t)(a.row0 + row), d[j]);
-                store_row((T *)a.dx + row * a.ldx, (j * TPR + t) * V, a.width, d[j]);
+            for (int e = 0; e < V; ++e) {
+                const float h = ((float)hn[j].v[e] - m0) * f0, g = (float)gn[j].v[e];
+                dw[j][e] = fmaf(g, h, dw[j][e]);
+                db[j][e] += g;
+                const float gw = g * (float)ws[j].v[e];
+                c[0] += gw;
+                c[1] = fmaf(gw, (j * TPR + t) * V + (WHOLE ? 0 : e) < a.width ? h : 0.0f, c[1]);
             }
+            if (FPT == 16) __builtin_amdgcn_sched_barrier(0);  // a vector at a time: registers
+        }
+        // two sets of words in turn: one barrier a row keeps a set until all have read it
+        row_sums<TPR>(c, part[turn]);
+        c[0] /= (float)a.width;
+        c[1] /= (float)a.width;
+        // what was loaded is converted again: kept in 32 bits it would take twice the registers
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            anew(hn[j]);
+            anew(gn[j]);
+            float d[V];
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                const float h = ((float)hn[j].v[e] - m0) * f0, g = (float)gn[j].v[e] * (float)ws[j].v[e];
+                d[e] = (a.dsum ? (float)dn[j].v[e] : 0.0f) + (g - c[0] - h * c[1]) * f0;
+            }
+            store_part<WHOLE>((T *)a.dres + row * a.ldr, (j * TPR + t) * V, a.width, d);
+            if (DROP) {
+                drop_out<V>(a.drop, seed, (j * TPR + t) * V, (uint32_t)(a.row0 + row), d);
+                store_part<WHOLE>((T *)a.dx + row * a.ldx, (j * TPR + t) * V, a.width, d);
+            }
+            if (FPT == 16) __builtin_amdgcn_sched_barrier(0);
         }
     }
     float *slot = a.part + (int64_t)blockIdx.x * 2 * a.width;
@@ -276,14 +320,13 @@ template <typename T, bool DROP>
 __global__ __launch_bounds__(1024) void layer_norm_back_long_kernel(LayerNormBackArgs a)
 {
     constexpr int V = kVec<T>, STEP = 1024 * V;
-    __shared__ float2 part[16];
+    __shared__ float part[16][2];
     const int t = threadIdx.x;
     const int64_t row = blockIdx.x;
     const uint64_t seed = DROP ? drop_seed(a.drop) : 0;
     const float m = a.mean[row], f = a.rstd[row];
     const T *sr = (const T *)a.s + row * a.lds, *gr = (const T *)a.dout + row * a.ldo;
-    float2 c = make_float2(0.0f, 0.0f);
-    float h[V], g[V], w[V];
+    float c[2] = {}, h[V], g[V], w[V];
     auto load = [&](int64_t k) {
         floats(load_row(sr, (int)k, a.width), h);
         floats(load_row(gr, (int)k, a.width), g);
@@ -298,13 +341,13 @@ __global__ __launch_bounds__(1024) void layer_norm_back_long_kernel(LayerNormBac
         load(k);
 #pragma unroll
         for (int e = 0; e < V; ++e) {
-            c.x += g[e];
-            c.y = fmaf(g[e], h[e], c.y);
+            c[0] += g[e];
+            c[1] = fmaf(g[e], h[e], c[1]);
         }
     }
-    c = row_sums<1024>(c, part);
-    c.x /= (float)a.width;
-    c.y /= (float)a.width;
+    row_sums<1024>(c, part);
+    c[0] /= (float)a.width;
+    c[1] /= (float)a.width;
     for (int64_t k = t * V; k < a.width; k += STEP) {
         float d[V];
         load(k);
@@ -315,7 +358,7 @@ __global__ __launch_bounds__(1024) void layer_norm_back_long_kernel(LayerNormBac
             for (int e = 0; e < V; ++e) d[e] = 0.0f;
         }
 #pragma unroll
-        for (int e = 0; e < V; ++e) d[e] += (g[e] - c.x - h[e] * c.y) * f;
+        for (int e = 0; e < V; ++e) d[e] += (g[e] - c[0] - h[e] * c[1]) * f;
         store_row((T *)a.dres + row * a.ldr, (int)k, a.width, d);
         if (DROP) {
             drop_out<V>(a.drop, seed, (int)k, (uint32_t)(a.row0 + row), d);
@@ -375,7 +418,10 @@ hipError_t typed(LayerNormArgs a, hipStream_t st)
         const unsigned grid = (unsigned)((a.rows + rpb - 1) / rpb);
         if (!with_shape(s, [&](auto tpr, auto fpt) {
                 constexpr int TPR = decltype(tpr)::value, FPT = decltype(fpt)::value;
-                layer_norm_kernel<T, TPR, FPT, DROP><<<grid, kBlock<TPR>, 0, st>>>(a);
+                if (a.width % kVec<T> == 0)
+                    layer_norm_kernel<T, TPR, FPT, DROP, true><<<grid, kBlock<TPR>, 0, st>>>(a);
+                else
+                    layer_norm_kernel<T, TPR, FPT, DROP, false><<<grid, kBlock<TPR>, 0, st>>>(a);
             }))
             layer_norm_long_kernel<T, DROP><<<grid, 1024, 0, st>>>(a);
         if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
@@ -420,7 +466,10 @@ hipError_t back_typed(const LayerNormBackArgs &a, hipStream_t st)
         hipError_t e = hipSuccess;
         if (!with_shape(shape_of(a.width), [&](auto tpr, auto fpt) {
                 constexpr int TPR = decltype(tpr)::value, FPT = decltype(fpt)::value;
-                layer_norm_back_kernel<T, TPR, FPT, DROP><<<slots, kBlock<TPR>, 0, st>>>(a);
+                if (a.width % kVec<T> == 0)
+                    layer_norm_back_kernel<T, TPR, FPT, DROP, true><<<slots, kBlock<TPR>, 0, st>>>(a);
+                else
+                    layer_norm_back_kernel<T, TPR, FPT, DROP, false><<<slots, kBlock<TPR>, 0, st>>>(a);
                 e = hipGetLastError();
             }))
             e = back_long<T, DROP>(a, slots, st);
