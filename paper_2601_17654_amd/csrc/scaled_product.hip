@@ -102,19 +102,46 @@ __global__ __launch_bounds__(NW * 64) void scaled_few_kernel(ScaledArgs a)
     f32x4 acc[MT];
 #pragma unroll
     for (int t = 0; t < MT; ++t) acc[t] = f32x4{0, 0, 0, 0};
-    auto load = [&](const char *row, int c) {
-        struct {
-            Pack<char, 16> v[2];
-        } f{{load_row(row, c, (int)a.k), load_row(row, c + 16, (int)a.k)}};
-        return __builtin_bit_cast(i32x8, f);
+    // the steps that are whole, some at a time: all of their loads are in flight at once
+    constexpr int AHEAD = MT > 1 ? 2 : 4;
+    const int whole = (int)(a.k / kScaled), steps = (int)((a.k + kScaled - 1) / kScaled);
+    struct Raw {
+        Pack<char, 16> v[2];
     };
-    const int steps = (int)((a.k + kScaled - 1) / kScaled);
-    for (int s = wave; s < steps; s += NW) {
+    int s = wave;
+    for (; s + (AHEAD - 1) * NW < whole; s += AHEAD * NW) {
+        Raw fw[AHEAD], fx[AHEAD][MT];
+        int sw[AHEAD], sx[AHEAD][MT];
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+            const int64_t b = s + u * NW;
+            const int c = (int)b * kScaled + part;
+            fw[u] = Raw{{load16(w + c), load16(w + c + 16)}};
+            sw[u] = ws[b * a.b.lds];
+#pragma unroll
+            for (int t = 0; t < MT; ++t) {
+                fx[u][t] = Raw{{load16(x[t] + c), load16(x[t] + c + 16)}};
+                sx[u][t] = xs[t][b * a.a.lds];
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+            const V vw(__builtin_bit_cast(i32x8, fw[u]), sw[u]);
+#pragma unroll
+            for (int t = 0; t < MT; ++t)
+                acc[t] = mma_values(vw, V(__builtin_bit_cast(i32x8, fx[u][t]), sx[u][t]), acc[t]);
+        }
+    }
+    auto load = [&](const char *row, int c) {
+        return __builtin_bit_cast(i32x8, Raw{{load_row(row, c, (int)a.k), load_row(row, c + 16, (int)a.k)}});
+    };
+#pragma unroll 1
+    for (; s < steps; s += NW) {
         const int c = s * kScaled + part;
-        const V fw(load(w, c), ws[s * a.b.lds]);
+        const V vw(load(w, c), ws[s * a.b.lds]);
 #pragma unroll
         for (int t = 0; t < MT; ++t)
-            acc[t] = mma_values(fw, V(load(x[t], c), xs[t][s * a.a.lds]), acc[t]);
+            acc[t] = mma_values(vw, V(load(x[t], c), xs[t][s * a.a.lds]), acc[t]);
     }
 #pragma unroll
     for (int t = 0; t < MT; ++t) *(f32x4 *)&sums[wave][t * 16 + r][lane / 16 * 4] = acc[t];
@@ -505,8 +532,15 @@ template <typename T>
 hipError_t few(const ScaledArgs &a, hipStream_t st)
 {
     const unsigned blocks = (unsigned)((a.n + 15) / 16);
-    if (a.m <= 16) scaled_few_kernel<4, 1, T><<<blocks, 256, 0, st>>>(a);
-    else scaled_few_kernel<4, 2, T><<<blocks, 256, 0, st>>>(a);
+    // four waves a block where there are blocks for every CU twice over, else sixteen
+    const bool many = blocks >= 512;
+    if (a.m <= 16) {
+        if (many) scaled_few_kernel<4, 1, T><<<blocks, 256, 0, st>>>(a);
+        else scaled_few_kernel<16, 1, T><<<blocks, 1024, 0, st>>>(a);
+    } else {
+        if (many) scaled_few_kernel<4, 2, T><<<blocks, 256, 0, st>>>(a);
+        else scaled_few_kernel<16, 2, T><<<blocks, 1024, 0, st>>>(a);
+    }
     return hipGetLastError();
 }
 
