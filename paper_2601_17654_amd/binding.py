@@ -1074,7 +1074,8 @@ def add_layer_norm(x, weight, bias=None, residual=None, eps: float = 1e-5, p: fl
     d = _drop(p, seed, offset, dev) if p else None
     out = _new_like(x)
     total = x if rr is None and d is None else _new_like(x)
-    mean, rstd = _new(x.shape[:-1], torch.float32), _new(x.shape[:-1], torch.float32)
+    mean = x.new_empty(x.shape[:-1], dtype=torch.float32)
+    rstd = torch.empty_like(mean)
     _check("kr_add_layer_norm",
            _lib.kr_add_layer_norm(t, n, width, xr.data_ptr(), ldx,
                                   None if rr is None else rr.data_ptr(), ldr, w.data_ptr(),
@@ -1243,40 +1244,51 @@ def _up(x: int, to: int) -> int:
 def _new_scaled(shape, rows: int, width: int):
     """An empty Scaled, rows of a multiple of 16 bytes, and its kr_scaled."""
     room, lds = _up(width, 16), _up(rows, _SCALED)
-    q = _new(shape[:-1] + (room,), torch.float8_e4m3fn)
+    q = _new(shape[:-1] + (room,), _E4M3)
     scale = _new((_up(width, _SCALED) // _SCALED, lds), torch.uint8)
     return (Scaled(q if room == width else q[..., :width], scale, room),
             KrScaled(q.data_ptr(), room, room, scale.data_ptr(), lds))
+
+
+_E4M3 = torch.float8_e4m3fn
 
 
 def _held(h: Scaled, name: str, dev: int):
     """kr_scaled of h, its rows and width, and what has to live."""
     if not isinstance(h, Scaled):
         raise TypeError("%s must be Scaled, got %s" % (name, type(h).__name__))
-    _type(h.q, name + ".q", (torch.float8_e4m3fn,))
-    _type(h.scale, name + ".scale", (torch.uint8,))
-    q, n, ld = _rows(h.q, name + ".q", dev)
+    q, s, room = h.q, h.scale, h.room
+    if not isinstance(q, torch.Tensor) or q.dtype is not _E4M3:
+        _type(q, name + ".q", (_E4M3,))
+    if not isinstance(s, torch.Tensor) or s.dtype is not torch.uint8:
+        _type(s, name + ".scale", (torch.uint8,))
+    was = q
+    q, n, ld = _rows(q, name, dev)
     width = q.shape[1]
-    # a copy, and a single row, have no room past their width but the multiple that is theirs
-    room = h.room if q.data_ptr() == h.q.data_ptr() else width
-    room = max(room, width)
-    ld = max(ld, room) if n <= 1 else ld
-    if room > width and n > 0:
-        there = q.untyped_storage().nbytes() - q.storage_offset()
-        if room > ld or (n - 1) * ld + room > there:
+    # a copy has no room past its width but the multiple that is its own
+    if room <= width or (q is not was and q.data_ptr() != was.data_ptr()):
+        room = width
+    elif n > 0:
+        if n == 1:
+            ld = room
+        if room > ld or (n - 1) * ld + room > q.untyped_storage().nbytes() - q.storage_offset():
             raise ValueError("%s has no room of %d columns in its rows" % (name, room))
-    s = h.scale
     if s.get_device() != dev:
         raise ValueError("%s.scale must be on the current device, got %s" % (name, s.device))
-    blocks = _up(width, _SCALED) // _SCALED
-    if s.dim() != 2 or s.shape[0] != blocks or s.shape[1] < _up(n, _SCALED):
+    blocks = (width + 127) // _SCALED
+    shape = s.shape
+    if len(shape) != 2 or shape[0] != blocks or shape[1] < (n + 127) // _SCALED * _SCALED:
         raise ValueError("%s.scale must be [%d][%d], got %s"
-                         % (name, blocks, _up(n, _SCALED), tuple(s.shape)))
-    if n and (s.stride(1) != 1 or s.stride(0) % 4 or s.stride(0) < s.shape[1] or s.data_ptr() % 4):
-        s = s.contiguous()
-    if n and s.stride(0) % 4:
-        raise ValueError("%s.scale must have rows of a multiple of 4 bytes" % name)
-    return KrScaled(q.data_ptr(), ld, room, s.data_ptr(), s.stride(0)), n, width, (q, s)
+                         % (name, blocks, _up(n, _SCALED), tuple(shape)))
+    lds = 0
+    if n:
+        lds, one = s.stride()
+        if one != 1 or lds % 4 or lds < shape[1] or s.data_ptr() % 4:
+            s = s.contiguous()
+            lds = s.stride(0)
+            if lds % 4:
+                raise ValueError("%s.scale must have rows of a multiple of 4 bytes" % name)
+    return KrScaled(q.data_ptr(), ld, room, s.data_ptr(), lds), n, width, (q, s)
 
 
 def scaled_hold(x, square: bool = False, plain: bool = True, crossed: bool = False) -> ScaledForms:
@@ -1302,7 +1314,8 @@ def scaled_values(h: Scaled, dtype=torch.float32) -> torch.Tensor:
     """The values that h holds, in dtype (kr_scaled_values)."""
     if dtype not in _TYPES:
         raise TypeError("dtype must be %s, got %s" % (" or ".join(map(str, _TYPES)), dtype))
-    _type(getattr(h, "q", h), "h.q", (torch.float8_e4m3fn,))
+    if not isinstance(h, Scaled) or not isinstance(h.q, torch.Tensor):
+        raise TypeError("h must be Scaled, got %s" % type(h).__name__)
     dev = _here(h.q, "h.q")
     k, n, width, keep = _held(h, "h", dev)
     out = _new(h.q.shape, dtype)
@@ -1317,13 +1330,14 @@ def scaled_matmul(a: Scaled, b: Scaled, dtype=torch.bfloat16) -> torch.Tensor:
     (kr_scaled_matmul).  It has no gradient."""
     if dtype not in _TYPES:
         raise TypeError("dtype must be %s, got %s" % (" or ".join(map(str, _TYPES)), dtype))
-    _type(getattr(a, "q", a), "a.q", (torch.float8_e4m3fn,))
+    if not isinstance(a, Scaled) or not isinstance(a.q, torch.Tensor):
+        raise TypeError("a must be Scaled, got %s" % type(a).__name__)
     dev = _here(a.q, "a.q")
     ak, m, k, keep_a = _held(a, "a", dev)
     bk, n, kb, keep_b = _held(b, "b", dev)
     if b.q.dim() != 2 or n < 1 or kb != k:
         raise ValueError("b.q must be [n][%d], got %s" % (k, tuple(b.q.shape)))
-    out = _new(a.q.shape[:-1] + (n,), dtype)
+    out = a.scale.new_empty(a.q.shape[:-1] + (n,), dtype=dtype)
     p = KrScaledProduct(m, n, k, ak, bk)
     wsb = _lib.kr_scaled_matmul_workspace(p)
     ws, at = _scratch(wsb)

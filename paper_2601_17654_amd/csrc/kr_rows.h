@@ -72,6 +72,16 @@ __device__ inline void store_part(T *row, int c, int width, const float *f)
     }
 }
 
+// The compiler knows nothing of x from here on: what was made of it before is made again.
+template <typename T>
+__device__ inline void anew(Pack<T, kVec<T>> &x)
+{
+    typedef int V4 __attribute__((ext_vector_type(4)));
+    V4 v = __builtin_bit_cast(V4, x);
+    asm("" : "+v"(v));
+    x = __builtin_bit_cast(Pack<T, kVec<T>>, v);
+}
+
 // Rows of one launch: a grid has fewer than 2^32 threads.
 constexpr int64_t kRowsPerLaunch = 1 << 21;
 

@@ -14,8 +14,6 @@ namespace kr {
 
 namespace {
 
-typedef int i32x4 __attribute__((ext_vector_type(4)));
-
 // x of the lane that is N before in its 16, in a ring.
 template <int N>
 __device__ inline float ring(float x)
@@ -185,15 +183,6 @@ __global__ __launch_bounds__(1024) void layer_norm_long_kernel(LayerNormArgs a)
         if (a.sum) store_row((T *)a.sum + row * a.lds, (int)c, a.width, s);
         store_row((T *)a.out + row * a.ldo, (int)c, a.width, n);
     }
-}
-
-// The compiler knows nothing of x from here on.
-template <typename T>
-__device__ inline void anew(Pack<T, kVec<T>> &x)
-{
-    i32x4 v = __builtin_bit_cast(i32x4, x);
-    asm("" : "+v"(v));
-    x = __builtin_bit_cast(Pack<T, kVec<T>>, v);
 }
 
 // Gradients, with h = (s - m) f, g = dn w:  ds = f (g - mean(g) - h mean(g h)) + dsum,

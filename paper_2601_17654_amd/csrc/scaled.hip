@@ -1,19 +1,113 @@
 // Holding a matrix in 8-bit floating point with a power of two for each 128 values, and its values back.
 #include <algorithm>
 
+#include "kr_rows.h"
 #include "kr_scaled.h"
 
 namespace kr {
 
 namespace {
 
+struct __attribute__((packed)) Loose8 {
+    uint32_t v[2];
+};
+
+// Eight held values to columns c .. c + 7 of a row of `bytes`.
+__device__ inline void store_q(char *row, int64_t c, int64_t bytes, uint32_t lo, uint32_t hi)
+{
+    if (c + 8 <= bytes) {
+        *(Loose8 *)(row + c) = Loose8{{lo, hi}};
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (c + e < bytes) row[c + e] = (char)((e < 4 ? lo : hi) >> (e % 4 * 8));
+    }
+}
+
+// Eight neighbours of a row, as they were loaded.
+template <typename T>
+struct Eight {
+    static constexpr int V = kVec<T>, NV = 8 / V;
+    Pack<T, V> x[NV];
+    // WHOLE: the row holds all of them.
+    template <bool WHOLE>
+    __device__ void load(const T *row, int64_t c, int64_t width)
+    {
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+            x[j] = WHOLE ? load16(row + c + j * V) : load_row(row, (int)c + j * V, (int)width);
+    }
+    __device__ void none()
+    {
+#pragma unroll
+        for (int j = 0; j < NV; ++j) x[j] = Pack<T, V>{};
+    }
+    __device__ void again()
+    {
+#pragma unroll
+        for (int j = 0; j < NV; ++j) anew(x[j]);
+    }
+    __device__ float at(int e) const { return (float)x[e / V].v[e % V]; }
+    __device__ uint32_t size(int e) const { return __float_as_uint(at(e)) & 0x7FFFFFFFu; }
+    // All eight times f; zeros where the block's byte is 255 (a NaN times 0 is no 0).
+    __device__ Loose8 held(float f, bool none) const
+    {
+        Loose8 q;
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+            q.v[h] = none ? 0u : hold4(at(h * 4) * f, at(h * 4 + 1) * f, at(h * 4 + 2) * f, at(h * 4 + 3) * f);
+        return q;
+    }
+};
+
+// Rows alone, each by itself: 16 lanes a block of k, eight values a lane, of the rows r, r + 16, ..
+// (ROWS of them), whose scale bytes are neighbours.
+template <typename T, int ROWS>
+__global__ __launch_bounds__(256) void hold_rows_kernel(HoldArgs a)
+{
+    const int lane = threadIdx.x % 16, r = threadIdx.x / 16;
+    const int64_t tile_r = blockIdx.x / a.tiles_c, tile_c = blockIdx.x - tile_r * a.tiles_c;
+    const int64_t r0 = tile_r * (16 * ROWS) + r, c0 = tile_c * kScaled + lane * 8;
+    Eight<T> x[ROWS];
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) {
+        const int64_t row = r0 + i * 16 < a.rows ? r0 + i * 16 : a.rows - 1;
+        x[i].template load<false>((const T *)a.x + row * a.ldx, c0, a.width);
+    }
+    uint32_t bytes = 0;
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) {
+        uint32_t top = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) top = max(top, x[i].size(e));
+#pragma unroll
+        for (int o = 8; o; o >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o));
+        if (r0 + i * 16 >= a.rows) continue;
+        const uint32_t byte = scale_byte(top);
+        bytes |= byte << (8 * i);
+        const Loose8 q = x[i].held(scale_inverse(byte), byte == 255);
+        store_q(a.plain.q + (r0 + i * 16) * a.plain.ld, c0, a.plain.bytes, q.v[0], q.v[1]);
+    }
+    if (lane == 0) {
+        uint8_t *to = a.plain.scale + tile_c * a.plain.lds + scale_place(r0);
+        if (ROWS == 4) *(uint32_t *)to = bytes;
+        else *(uint16_t *)to = (uint16_t)bytes;
+    }
+    // rows up to a multiple of 128 have bytes too: the last tile's
+    const int64_t all = (a.rows + kScaled - 1) / kScaled * kScaled;
+    if (lane == 0 && (tile_r + 1) * (16 * ROWS) >= a.rows) {
+        for (int64_t i = (tile_r + 1) * (16 * ROWS) + r; i < all; i += 16)
+            a.plain.scale[tile_c * a.plain.lds + scale_place(i)] = 0;
+    }
+}
+
 // A block of 256 threads takes a tile of 128 x 128: thread (cg, rg) eight columns from 8 cg on of the
 // eight rows from 8 rg on.  Both forms come of one read: the plain one's bytes go straight out, the
-// crossed one's through LDS, where 8-byte chunk rg of column c lies at place rg ^ c / 8.
+// crossed one's through LDS, where 8-byte chunk rg of column c lies at place rg ^ c / 8.  Values stay
+// as they were loaded and are converted twice, for the largest and to be held: half the registers.
 template <typename T, bool SQUARE, bool PLAIN, bool CROSSED>
 __global__ __launch_bounds__(256) void hold_kernel(HoldArgs a)
 {
-    constexpr int V = kVec<T>, NV = 8 / V;
     __shared__ uint32_t tops[CROSSED && !SQUARE ? 4 * kScaled : 4];
     __shared__ __align__(16) uint8_t bytes[2][kScaled];
     __shared__ __align__(16) uint8_t turned[CROSSED ? kScaled * kScaled : 16];
@@ -21,29 +115,30 @@ __global__ __launch_bounds__(256) void hold_kernel(HoldArgs a)
     const int64_t tile_r = blockIdx.x / a.tiles_c, tile_c = blockIdx.x - tile_r * a.tiles_c;
     const int64_t r0 = tile_r * kScaled + rg * 8, c0 = tile_c * kScaled + cg * 8;
 
-    float v[8][8];
-    uint32_t row_top[8], column_top[8] = {};
-    Pack<T, V> x[8][NV];
+    Eight<T> x[8];
+    if ((tile_r + 1) * kScaled <= a.rows && (tile_c + 1) * kScaled <= a.width) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
+        for (int i = 0; i < 8; ++i)
+            x[i].template load<true>((const T *)a.x + (r0 + i) * a.ldx, c0, a.width);
+    } else {
 #pragma unroll
-        for (int j = 0; j < NV; ++j) {
-            const int64_t r = r0 + i;
-            x[i][j] = load_row((const T *)a.x + (r < a.rows ? r : 0) * a.ldx, (int)c0 + j * V,
-                               r < a.rows ? (int)a.width : 0);
+        for (int i = 0; i < 8; ++i) {
+            if (r0 + i < a.rows) x[i].template load<false>((const T *)a.x + (r0 + i) * a.ldx, c0, a.width);
+            else x[i].none();
         }
+    }
+    uint32_t row_top[8], column_top[8] = {};
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         row_top[i] = 0;
 #pragma unroll
-        for (int j = 0; j < NV; ++j) floats(x[i][j], v[i] + j * V);
-#pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const uint32_t m = __float_as_uint(v[i][e]) & 0x7FFFFFFFu;
+            const uint32_t m = x[i].size(e);
             row_top[i] = max(row_top[i], m);
-            column_top[e] = max(column_top[e], m);
+            if (CROSSED && !SQUARE) column_top[e] = max(column_top[e], m);
         }
     }
+    uint32_t square_byte = 0;
     if (SQUARE) {
         uint32_t top = 0;
 #pragma unroll
@@ -52,75 +147,55 @@ __global__ __launch_bounds__(256) void hold_kernel(HoldArgs a)
         for (int o = 32; o; o >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o));
         if (t % 64 == 0) tops[wave] = top;
         __syncthreads();
-        top = max(max(tops[0], tops[1]), max(tops[2], tops[3]));
+        square_byte = scale_byte(max(max(tops[0], tops[1]), max(tops[2], tops[3])));
+    } else if (CROSSED) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) row_top[i] = column_top[i] = top;
-    } else {
-        if (PLAIN) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-#pragma unroll
-                for (int o = 8; o; o >>= 1)
-                    row_top[i] = max(row_top[i], (uint32_t)__shfl_xor((int)row_top[i], o));
-        }
-        if (CROSSED) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                column_top[e] = max(column_top[e], (uint32_t)__shfl_xor((int)column_top[e], 16));
-                column_top[e] = max(column_top[e], (uint32_t)__shfl_xor((int)column_top[e], 32));
-                if (rg % 4 == 0) tops[wave * kScaled + cg * 8 + e] = column_top[e];
-            }
-            __syncthreads();
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-#pragma unroll
-                for (int w = 0; w < 4; ++w)
-                    column_top[e] = max(column_top[e], tops[w * kScaled + cg * 8 + e]);
+        for (int e = 0; e < 8; ++e) {
+            column_top[e] = max(column_top[e], (uint32_t)__shfl_xor((int)column_top[e], 16));
+            column_top[e] = max(column_top[e], (uint32_t)__shfl_xor((int)column_top[e], 32));
+            if (rg % 4 == 0) tops[wave * kScaled + cg * 8 + e] = column_top[e];
         }
     }
     if (PLAIN) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const uint32_t byte = scale_byte(row_top[i]);
-            const float f = scale_inverse(byte);
-            // an infinite or NaN value times 0 is no 0: its block holds zeros
-            const bool none = byte == 255;
-            uint32_t q[2];
+            if (!SQUARE) {
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
-                q[h] = none ? 0 : hold4(v[i][h * 4] * f, v[i][h * 4 + 1] * f, v[i][h * 4 + 2] * f,
-                                        v[i][h * 4 + 3] * f);
-            if (cg == 0)
-                bytes[0][(rg * 8 + i) % 16 * 8 + (rg * 8 + i) / 16] = r0 + i < a.rows ? (uint8_t)byte : 0;
-            if (r0 + i >= a.rows) continue;
-            char *to = a.plain.q + (r0 + i) * a.plain.ld + c0;
-            if (c0 + 8 <= a.plain.bytes) {
-                struct __attribute__((packed)) Loose8 {
-                    uint32_t v[2];
-                };
-                *(Loose8 *)to = Loose8{{q[0], q[1]}};
-            } else {
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    if (c0 + e < a.plain.bytes) to[e] = (char)(q[e / 4] >> (e % 4 * 8));
+                for (int o = 8; o; o >>= 1)
+                    row_top[i] = max(row_top[i], (uint32_t)__shfl_xor((int)row_top[i], o));
             }
+            const uint32_t byte = SQUARE ? square_byte : scale_byte(row_top[i]);
+            const int row = rg * 8 + i;
+            if (cg == 0) bytes[0][row % 16 * 8 + row / 16] = r0 + i < a.rows ? (uint8_t)byte : 0;
+            x[i].again();
+            const Loose8 q = x[i].held(scale_inverse(byte), byte == 255);
+            if (r0 + i < a.rows)
+                store_q(a.plain.q + (r0 + i) * a.plain.ld, c0, a.plain.bytes, q.v[0], q.v[1]);
         }
     }
     if (CROSSED) {
+        if (!SQUARE) __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i].again();
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const uint32_t byte = scale_byte(column_top[e]);
+            uint32_t byte = square_byte;
+            if (!SQUARE) {
+                uint32_t top = 0;
+#pragma unroll
+                for (int w = 0; w < 4; ++w) top = max(top, tops[w * kScaled + cg * 8 + e]);
+                byte = scale_byte(top);
+            }
             const float f = scale_inverse(byte);
             const bool none = byte == 255;
+            const int column = cg * 8 + e;
             i32x2 q;
 #pragma unroll
             for (int h = 0; h < 2; ++h)
-                q[h] = none ? 0 : (int)hold4(v[h * 4][e] * f, v[h * 4 + 1][e] * f, v[h * 4 + 2][e] * f,
-                                             v[h * 4 + 3][e] * f);
-            if (rg == 0)
-                bytes[1][(cg * 8 + e) % 16 * 8 + (cg * 8 + e) / 16] =
-                    c0 + e < a.width ? (uint8_t)byte : 0;
-            *(i32x2 *)(turned + (cg * 8 + e) * kScaled + ((rg ^ cg) << 3)) = q;
+                q[h] = none ? 0 : (int)hold4(x[h * 4].at(e) * f, x[h * 4 + 1].at(e) * f,
+                                             x[h * 4 + 2].at(e) * f, x[h * 4 + 3].at(e) * f);
+            if (rg == 0) bytes[1][column % 16 * 8 + column / 16] = c0 + e < a.width ? (uint8_t)byte : 0;
+            *(i32x2 *)(turned + column * kScaled + ((rg ^ cg) << 3)) = q;
         }
     }
     __syncthreads();
@@ -131,26 +206,44 @@ __global__ __launch_bounds__(256) void hold_kernel(HoldArgs a)
         if (t >= 64 && t < 64 + kScaled / 4)
             *(uint32_t *)(a.crossed.scale + tile_r * a.crossed.lds + tile_c * kScaled + (t - 64) * 4) =
                 *(const uint32_t *)(bytes[1] + (t - 64) * 4);
-        // 16 lanes a column: 128 bytes
+        // 8 lanes a column: 128 bytes.  Chunks 2 i and 2 i + 1 lie side by side, in turn where c / 8
+        // is odd.
 #pragma unroll
-        for (int p = 0; p < 8; ++p) {
-            const int c = p * 16 + t / 16, chunk = t % 16;
-            const int64_t column = tile_c * kScaled + c, r = tile_r * kScaled + chunk * 8;
-            const i32x2 q = *(const i32x2 *)(turned + c * kScaled + ((chunk ^ c / 8) << 3));
+        for (int p = 0; p < 4; ++p) {
+            const int c = p * 32 + t / 8, pair = t % 8, odd = c / 8 % 2;
+            const int64_t column = tile_c * kScaled + c, r = tile_r * kScaled + pair * 16;
+            const Loose16 w = *(const Loose16 *)(turned + c * kScaled + ((pair ^ c / 16) << 4));
+            Loose16 q = w;
+            if (odd) q.v = w.v.zwxy;
             if (column >= a.width) continue;
-            char *to = a.crossed.q + column * a.crossed.ld + r;
-            if (r + 8 <= a.crossed.bytes) {
-                struct __attribute__((packed)) Loose8 {
-                    int v[2];
-                };
-                *(Loose8 *)to = Loose8{{q[0], q[1]}};
+            char *to = a.crossed.q + column * a.crossed.ld;
+            if (r + 16 <= a.crossed.bytes) {
+                *(Loose16 *)(to + r) = q;
             } else {
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    if (r + e < a.crossed.bytes) to[e] = (char)(q[e / 4] >> (e % 4 * 8));
+                store_q(to, r, a.crossed.bytes, q.v[0], q.v[1]);
+                store_q(to, r + 8, a.crossed.bytes, q.v[2], q.v[3]);
             }
         }
     }
+}
+
+template <typename T>
+hipError_t hold_rows(HoldArgs a, hipStream_t st)
+{
+    // four rows a thread, two where that leaves CUs without a second block
+    const int64_t rows = a.rows, tall = (rows + 63) / 64 * a.tiles_c >= 512 ? 64 : 32;
+    // a grid has fewer than 2^32 threads; whole groups of 128 rows, whose scale bytes are neighbours
+    const int64_t most = std::max<int64_t>(1, (1 << 22) / a.tiles_c) * kScaled;
+    for (int64_t done = 0; done < rows; done += most) {
+        a.rows = std::min(most, rows - done);
+        const unsigned blocks = (unsigned)((a.rows + tall - 1) / tall * a.tiles_c);
+        if (tall == 64) hold_rows_kernel<T, 4><<<blocks, 256, 0, st>>>(a);
+        else hold_rows_kernel<T, 2><<<blocks, 256, 0, st>>>(a);
+        a.x = (const T *)a.x + a.rows * a.ldx;
+        a.plain.q += a.rows * a.plain.ld;
+        a.plain.scale += a.rows;
+    }
+    return hipGetLastError();
 }
 
 template <typename T, bool SQUARE>
@@ -158,8 +251,9 @@ hipError_t hold(const HoldArgs &a, hipStream_t st)
 {
     const unsigned blocks = (unsigned)((a.rows + kScaled - 1) / kScaled * a.tiles_c);
     if (a.plain.q && a.crossed.q) hold_kernel<T, SQUARE, true, true><<<blocks, 256, 0, st>>>(a);
-    else if (a.plain.q) hold_kernel<T, SQUARE, true, false><<<blocks, 256, 0, st>>>(a);
-    else hold_kernel<T, SQUARE, false, true><<<blocks, 256, 0, st>>>(a);
+    else if (a.crossed.q) hold_kernel<T, SQUARE, false, true><<<blocks, 256, 0, st>>>(a);
+    else if constexpr (SQUARE) hold_kernel<T, true, true, false><<<blocks, 256, 0, st>>>(a);
+    else return hold_rows<T>(a, st);
     return hipGetLastError();
 }
 
