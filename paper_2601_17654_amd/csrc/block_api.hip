@@ -484,7 +484,7 @@ kr_status scaled_run(const kr_scaled_product *p, int32_t type, void *out, int64_
                      hipStream_t st)
 {
     ScaledArgs x{type, p->m, p->n, p->k, held(&p->a), held(&p->b), out, ldo, nullptr};
-    if (p->m <= kFewRows) return out ? said(launch_scaled_few(x, st)) : KR_OK;
+    if (p->m <= kScaledFew) return out ? said(launch_scaled_few(x, st)) : KR_OK;
     // rows to a multiple of 16 bytes: theirs, where they have that room
     const int64_t wide = padded(p->k);
     const Laid a(p->a.q, p->a.ld, p->m, p->a.room >= wide ? wide : p->k, c);

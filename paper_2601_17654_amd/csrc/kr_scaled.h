@@ -13,7 +13,8 @@
 
 namespace kr {
 
-constexpr int kScaled = 128;  // values that share a scale
+constexpr int kScaled = 128;   // values that share a scale
+constexpr int kScaledFew = 16;  // rows of a product that launch_scaled_few takes
 
 typedef int i32x2 __attribute__((ext_vector_type(2)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));

@@ -257,38 +257,50 @@ hipError_t hold(const HoldArgs &a, hipStream_t st)
     return hipGetLastError();
 }
 
-// Values back: a thread takes 16 neighbours.
+// Values back: a thread takes 16 neighbours, of 32-bit values 4, which are 16 bytes written.  (With 16 of
+// these, four stores 64 bytes apart, 8192 x 8192 took 96 us.)
+template <typename T>
+constexpr int kBack = sizeof(T) == 4 ? 4 : 16;
+
 template <typename T>
 __global__ __launch_bounds__(256) void held_values_kernel(HeldValuesArgs a, uint32_t log_tpr,
                                                           uint32_t chunks)
 {
+    constexpr int N = kBack<T>;
     const int64_t block = blockIdx.x / chunks;
     const uint32_t chunk = blockIdx.x - (uint32_t)block * chunks;
     const int64_t row = (block << (8 - log_tpr)) + (threadIdx.x >> log_tpr);
-    const int64_t c = (((int64_t)chunk << log_tpr) + (threadIdx.x & ((1u << log_tpr) - 1))) * 16;
+    const int64_t c = (((int64_t)chunk << log_tpr) + (threadIdx.x & ((1u << log_tpr) - 1))) * N;
     if (row >= a.rows || c >= a.width) return;
-    const Pack<char, 16> q = load_row(a.h.q + row * a.h.ld, (int)c, (int)a.width);
-    const uint32_t byte = a.h.scale[c / kScaled * a.h.lds + scale_place(row)];
-    const struct {
-        int v[4];
-    } w = __builtin_bit_cast(decltype(w), q);
-    float f[16];
+    struct __attribute__((packed)) Loose {
+        int v[N / 4];
+    } w = {};
+    const char *q = a.h.q + row * a.h.ld + c;
+    if (c + N <= a.width) {
+        w = *(const Loose *)q;
+    } else {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+        for (int e = 0; e < N; ++e)
+            if (c + e < a.width) w.v[e / 4] |= (int)(uint8_t)q[e] << (e % 4 * 8);
+    }
+    const uint32_t byte = a.h.scale[c / kScaled * a.h.lds + scale_place(row)];
+    float f[N];
+#pragma unroll
+    for (int i = 0; i < N / 4; ++i) {
         f[4 * i] = scale_times(__builtin_amdgcn_cvt_f32_fp8(w.v[i], 0), byte);
         f[4 * i + 1] = scale_times(__builtin_amdgcn_cvt_f32_fp8(w.v[i], 1), byte);
         f[4 * i + 2] = scale_times(__builtin_amdgcn_cvt_f32_fp8(w.v[i], 2), byte);
         f[4 * i + 3] = scale_times(__builtin_amdgcn_cvt_f32_fp8(w.v[i], 3), byte);
     }
 #pragma unroll
-    for (int j = 0; j < 16; j += kVec<T>)
+    for (int j = 0; j < N; j += kVec<T>)
         store_row((T *)a.out + row * a.ldo, (int)c + j, (int)a.width, f + j);
 }
 
 template <typename T>
 hipError_t values(HeldValuesArgs a, hipStream_t st)
 {
-    const int64_t groups = (a.width + 15) / 16;
+    const int64_t groups = (a.width + kBack<T> - 1) / kBack<T>;
     uint32_t log_tpr = 0;
     while (log_tpr < 8 && (1 << log_tpr) < groups) ++log_tpr;
     const uint32_t chunks = (uint32_t)((groups + (1 << log_tpr) - 1) >> log_tpr);

@@ -77,60 +77,47 @@ __device__ inline f32x4 mma_values(const Values<true> &a, const Values<true> &b,
     return c;
 }
 
-// Few rows (up to 32), out of the weights as they lie in memory: as few_kernel, 128 bytes of k of 16
-// rows a wave and step.
-template <int NW, int MT, typename T>
+// Few rows (up to 16), out of the weights as they lie in memory: as few_kernel, 128 bytes of k of 16
+// rows a wave and step.  (From 17 rows on tiles are faster: 32 x 8192 x 8192 17.8 us, 26.4 with two groups of
+// 16 rows here.)
+template <int NW, typename T>
 __global__ __launch_bounds__(NW * 64) void scaled_few_kernel(ScaledArgs a)
 {
     typedef Values<sizeof(T) == 4> V;
-    __shared__ __align__(16) float sums[NW][MT * 16][16];
+    __shared__ __align__(16) float sums[NW][16][16];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int r = lane % 16, part = lane / 16 * 32;
-    const int64_t n0 = (int64_t)blockIdx.x * 16;
+    // an XCD (every eighth block) takes neighbouring rows: eight groups of 16 share a line of scales
+    const int id = (int)blockIdx.x, all = (int)gridDim.x, xcd = id & 7;
+    const int64_t n0 = (int64_t)(xcd * (all >> 3) + min(xcd, all & 7) + (id >> 3)) * 16;
     // rows past the last take its place: their sums are not put
-    const int64_t wn = n0 + r < a.n ? n0 + r : a.n - 1;
-    const char *w = a.b.q + wn * a.b.ld;
-    const uint8_t *ws = a.b.scale + scale_place(wn);
-    const char *x[MT];
-    const uint8_t *xs[MT];
-#pragma unroll
-    for (int t = 0; t < MT; ++t) {
-        const int64_t m = t * 16 + r < a.m ? t * 16 + r : a.m - 1;
-        x[t] = a.a.q + m * a.a.ld;
-        xs[t] = a.a.scale + scale_place(m);
-    }
-    f32x4 acc[MT];
-#pragma unroll
-    for (int t = 0; t < MT; ++t) acc[t] = f32x4{0, 0, 0, 0};
+    const int64_t wn = n0 + r < a.n ? n0 + r : a.n - 1, xm = r < a.m ? r : a.m - 1;
+    const char *w = a.b.q + wn * a.b.ld, *x = a.a.q + xm * a.a.ld;
+    const uint8_t *ws = a.b.scale + scale_place(wn), *xs = a.a.scale + scale_place(xm);
+    f32x4 acc{0, 0, 0, 0};
     // the steps that are whole, some at a time: all of their loads are in flight at once
-    constexpr int AHEAD = MT > 1 ? 2 : 4;
+    constexpr int AHEAD = 4;
     const int whole = (int)(a.k / kScaled), steps = (int)((a.k + kScaled - 1) / kScaled);
     struct Raw {
         Pack<char, 16> v[2];
     };
     int s = wave;
     for (; s + (AHEAD - 1) * NW < whole; s += AHEAD * NW) {
-        Raw fw[AHEAD], fx[AHEAD][MT];
-        int sw[AHEAD], sx[AHEAD][MT];
+        Raw fw[AHEAD], fx[AHEAD];
+        int sw[AHEAD], sx[AHEAD];
 #pragma unroll
         for (int u = 0; u < AHEAD; ++u) {
             const int64_t b = s + u * NW;
             const int c = (int)b * kScaled + part;
             fw[u] = Raw{{load16(w + c), load16(w + c + 16)}};
             sw[u] = ws[b * a.b.lds];
-#pragma unroll
-            for (int t = 0; t < MT; ++t) {
-                fx[u][t] = Raw{{load16(x[t] + c), load16(x[t] + c + 16)}};
-                sx[u][t] = xs[t][b * a.a.lds];
-            }
+            fx[u] = Raw{{load16(x + c), load16(x + c + 16)}};
+            sx[u] = xs[b * a.a.lds];
         }
 #pragma unroll
-        for (int u = 0; u < AHEAD; ++u) {
-            const V vw(__builtin_bit_cast(i32x8, fw[u]), sw[u]);
-#pragma unroll
-            for (int t = 0; t < MT; ++t)
-                acc[t] = mma_values(vw, V(__builtin_bit_cast(i32x8, fx[u][t]), sx[u][t]), acc[t]);
-        }
+        for (int u = 0; u < AHEAD; ++u)
+            acc = mma_values(V(__builtin_bit_cast(i32x8, fw[u]), sw[u]),
+                             V(__builtin_bit_cast(i32x8, fx[u]), sx[u]), acc);
     }
     auto load = [&](const char *row, int c) {
         return __builtin_bit_cast(i32x8, Raw{{load_row(row, c, (int)a.k), load_row(row, c + 16, (int)a.k)}});
@@ -138,16 +125,12 @@ __global__ __launch_bounds__(NW * 64) void scaled_few_kernel(ScaledArgs a)
 #pragma unroll 1
     for (; s < steps; s += NW) {
         const int c = s * kScaled + part;
-        const V vw(load(w, c), ws[s * a.b.lds]);
-#pragma unroll
-        for (int t = 0; t < MT; ++t)
-            acc[t] = mma_values(vw, V(load(x[t], c), xs[t][s * a.a.lds]), acc[t]);
+        acc = mma_values(V(load(w, c), ws[s * a.b.lds]), V(load(x, c), xs[s * a.a.lds]), acc);
     }
-#pragma unroll
-    for (int t = 0; t < MT; ++t) *(f32x4 *)&sums[wave][t * 16 + r][lane / 16 * 4] = acc[t];
+    *(f32x4 *)&sums[wave][r][lane / 16 * 4] = acc;
     __syncthreads();
     const int token = (int)threadIdx.x / 2, h = (int)threadIdx.x % 2 * 8;
-    if (token >= a.m || n0 + h >= a.n) return;  // NW * 32 threads or more: a token each two
+    if (token >= a.m || n0 + h >= a.n) return;
     float v[8] = {};
 #pragma unroll 4
     for (int k = 0; k < NW; ++k)
@@ -170,14 +153,14 @@ struct TileArgs {
 // A block's copies to LDS: the operands' tiles as in mma_kernel, 16 bytes a lane, and the step's scale
 // bytes, 4 a lane: the first wave those of a's tile, the second of b's, each to 256 bytes of its own (the
 // others copy an empty buffer, so that every wave counts the same copies).
-template <int BM, int BN>
+template <int BM, int BN, int NW>
 struct Copies {
-    typedef TileLoader<false, BM, 4> LoadA;
-    typedef TileLoader<false, BN, 4> LoadB;
+    typedef TileLoader<false, BM, NW> LoadA;
+    typedef TileLoader<false, BN, NW> LoadB;
     static constexpr int N = LoadA::N + LoadB::N + 1;  // of a wave and step, the scales last
     struct Lds {
         char tile[2][(BM + BN) * kStep];
-        uint8_t scale[2][4][256];
+        uint8_t scale[2][NW][256];
     };
     LoadA la;
     LoadB lb;
@@ -198,7 +181,7 @@ struct Copies {
         la.aim(begin, 0);
         lb.aim(begin, 0);
         const bool odd = wave & 1;
-        const int64_t first = odd ? n0 : m0, left = (odd ? a.rows[1] : a.rows[0]) - first;
+        const int64_t first = (odd ? n0 : m0) / kScaled * kScaled, left = (odd ? a.rows[1] : a.rows[0]) - first;
         ld = odd ? a.lds[1] : a.lds[0];
         at = (uint64_t)((odd ? a.scale[1] : a.scale[0]) + begin * ld + first);
         records = wave < 2 ? (int)(left < 256 ? left : 256) : 0;
@@ -322,7 +305,7 @@ __global__ __launch_bounds__(256) void scaled_tile_kernel(TileArgs a, Out out)
     constexpr int WM = 2, WN = 2, RM = BM / WM, RN = BN / WN, TM = RM / 16, TN = RN / 16;
     constexpr int BLOCK = TM * TN, QUARTER = BLOCK / 4, HM = TM / 2, HN = TN / 2;
     typedef When<BLOCK> W;
-    typedef Copies<BM, BN> C;
+    typedef Copies<BM, BN, 4> C;
     static_assert(HM == HN && W::free >= 2 * HM * W::apart && W::next >= 2 * QUARTER &&
                       W::next + HM * W::apart >= 3 * QUARTER && W::next + 2 * HM * W::apart <= BLOCK &&
                       2 * HM * W::apart <= QUARTER * 2 && HM * W::apart <= QUARTER &&
@@ -418,13 +401,13 @@ __global__ __launch_bounds__(256) void scaled_tile_kernel(TileArgs a, Out out)
     put_tile<BM, BN, WM, WN>(E4m3(), a.p, out, acc, lds.tile[0], m0, n0, wave, split, lane);
 }
 
-// The same for outputs of 32 bits: a step's values go to bfloat16 on their way to the instructions.  The
-// compiler places these, and two blocks a CU fill each other's waits.
-template <typename Out>
-__global__ __launch_bounds__(256) void scaled_wide_kernel(TileArgs a, Out out)
+// The same for outputs of 32 bits, in tiles of 128 x BN: a step's values go to bfloat16 on their way to the
+// instructions, which the compiler places.  A lane's four sums are neighbours in a row and leave as they are.
+template <int BN>
+__global__ __launch_bounds__(256) void scaled_wide_kernel(TileArgs a, float *out, int64_t ldo)
 {
-    constexpr int BM = 128, BN = 128, WN = 2, TM = 4, TN = 4;
-    typedef Copies<BM, BN> C;
+    constexpr int BM = 128, WN = 2, TM = 4, TN = BN / WN / 16;
+    typedef Copies<BM, BN, 4> C;
     __shared__ __align__(1024) typename C::Lds lds;
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
@@ -453,41 +436,75 @@ __global__ __launch_bounds__(256) void scaled_wide_kernel(TileArgs a, Out out)
     for (int s = begin; s < end; ++s) {
         const int buf = (s - begin) & 1;
         arrived<C::N>();
-        const int sa = read_scales<64>(lds.scale[buf][0], wm, lane)[0];
-        const int sb = read_scales<64>(lds.scale[buf][1], wn, lane)[0];
+        // of 16-row tiles, side by side; a tile of 64 rows of b is half of its 128
+        const uint8_t *of_a = lds.scale[buf][0] + lane % 16 * 8 + wm * TM;
+        const uint8_t *of_b = lds.scale[buf][1] + lane % 16 * 8 + n0 % kScaled / 16 + wn * TN;
+        const uint32_t sa = *(const uint32_t *)of_a;
+        const uint32_t sb = TN == 4 ? *(const uint32_t *)of_b : *(const uint16_t *)of_b;
         i32x8 qa[TM], qb[TN];
 #pragma unroll
-        for (int i = 0; i < TM; ++i) qa[i] = tile(lds.tile[buf], wm * 64 + i * 16);
+        for (int i = 0; i < TM; ++i) qa[i] = tile(lds.tile[buf], (wm * TM + i) * 16);
 #pragma unroll
-        for (int j = 0; j < TN; ++j) qb[j] = tile(lds.tile[buf] + BM * kStep, wn * 64 + j * 16);
+        for (int j = 0; j < TN; ++j) qb[j] = tile(lds.tile[buf] + BM * kStep, (wn * TN + j) * 16);
         read_done();
 #pragma unroll
         for (int p = 0; p < C::PARTS; ++p) c.part(p);
         c.all(lds, buf);
-        auto byte = [](int x, int t) { return x >> (8 * t) & 255; };
+        auto byte = [](uint32_t x, int t) { return (int)(x >> (8 * t) & 255); };
         const Values<true> va[TM] = {{qa[0], byte(sa, 0)}, {qa[1], byte(sa, 1)}, {qa[2], byte(sa, 2)},
                                      {qa[3], byte(sa, 3)}};
 #pragma unroll
         for (int j = 0; j < TN; ++j) {
             const Values<true> vb(qb[j], byte(sb, j));
 #pragma unroll
-            for (int i = 0; i < TM; ++i) acc[i][j] = mma_values(vb, va[i], acc[i][j]);
+            for (int q = 0; q < 4; ++q)
+#pragma unroll
+                for (int i = 0; i < TM; ++i) acc[i][j] = mma(bf16(), vb.v[q], va[i].v[q], acc[i][j]);
         }
     }
-    read_done();
-    arrived<0>();  // the tiles' LDS is free, and no copy will write to it
-    put_tile<BM, BN, 2, WN>(E4m3(), a.p, out, acc, lds.tile[0], m0, n0, wave, split, lane);
+    if (a.p.splits > 1) {
+        out = a.p.part + (int64_t)split * a.p.m * a.p.n;
+        ldo = a.p.n;
+    }
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j) {
+            const int64_t m = m0 + (wm * TM + i) * 16 + lane % 16;
+            const int n = (int)n0 + (wn * TN + j) * 16 + lane / 16 * 4;
+            if (m < a.p.m) store_row(out + m * ldo, n, a.p.n, (const float *)&acc[i][j]);
+        }
+    arrived<0>();  // no copy is under way when the block's LDS is given up
 }
 
-MmaPlan plan_of(int out_type, int64_t m, int64_t n, int steps)
+// How a product is cut.  16-bit outputs: as the other products, whose steps take as long.  32-bit outputs:
+// tiles of 128 x 128 or 128 x 64 and up to 16 splits of the sum, by an estimate in microseconds: 1.05 and
+// 0.8 a step, a tile a CU at a time (two share the time), 5 around them, 5 for a split's join and its sums
+// at 4 TB/s.  Measured, 128 x 128 / 128 x 64 at the splits in brackets: 333 x 5001 x 2059 26.3 / 21.0 us (1),
+// 1000 x 4096 x 4096 46.5 / 49.3 (1), 32 x 8192 x 8192 26.4 (4) / 36.0 (2), 100 x 1000 x 16000 26.3 / 22.1 (8).
+struct Plan {
+    MmaPlan p;
+    bool narrow;  // of 32-bit outputs: tiles of 128 x 64
+};
+Plan plan_of(int out_type, int64_t m, int64_t n, int steps)
 {
-    MmaPlan p = mma_plan(m, n, 1, steps);
-    if (out_type == KR_F32 && p.large) {  // small tiles only
-        p.large = false;
-        p.tiles_m = (int)((m + 127) / 128);
-        p.tiles_n = (int)((n + 127) / 128);
+    if (out_type != KR_F32) return {mma_plan(m, n, 1, steps), false};
+    Plan best{};
+    double least = 0;
+    for (const bool narrow : {false, true}) {
+        const int64_t tm = (m + 127) / 128, tn = narrow ? (n + 63) / 64 : (n + 127) / 128;
+        for (int s = 1; s <= 16 && (s == 1 || (steps + s - 1) / s >= 4); ++s) {
+            const int per = (steps + s - 1) / s;
+            if ((steps + per - 1) / per != s) continue;
+            const int64_t part = s > 1 ? 4 * s * m * n : 0;
+            const double cost = (tm * tn * s + 255) / 256 * per * (narrow ? 0.8 : 1.05) +
+                                (s > 1 ? 5 + 2 * (double)part / 4e6 : 0);
+            if (best.p.tiles_m && cost >= least) continue;
+            least = cost;
+            best = {{false, (int)tm, (int)tn, s, per, part}, narrow};
+        }
     }
-    return p;
+    return best;
 }
 
 template <typename T>
@@ -501,7 +518,8 @@ hipError_t tiles(const ScaledArgs &a, hipStream_t st)
     x.p.k_bytes = a.a.bytes;
     x.p.steps = (int)((a.k + kScaled - 1) / kScaled);
     x.p.pairs = 1;
-    const MmaPlan p = plan_of(a.out_type, a.m, a.n, x.p.steps);
+    const Plan plan = plan_of(a.out_type, a.m, a.n, x.p.steps);
+    const MmaPlan &p = plan.p;
     x.p.tiles_m = p.tiles_m;
     x.p.tiles_n = p.tiles_n;
     x.p.splits = p.splits;
@@ -516,7 +534,8 @@ hipError_t tiles(const ScaledArgs &a, hipStream_t st)
     const PutAs<T> out{(T *)a.out, a.ldo, (int)a.n};
     const unsigned blocks = (unsigned)(p.tiles_m * p.tiles_n * p.splits);
     if constexpr (sizeof(T) == 4)
-        scaled_wide_kernel<<<blocks, 256, 0, st>>>(x, out);
+        plan.narrow ? scaled_wide_kernel<64><<<blocks, 256, 0, st>>>(x, out.out, out.ldo)
+                    : scaled_wide_kernel<128><<<blocks, 256, 0, st>>>(x, out.out, out.ldo);
     else if (p.large)
         scaled_tile_kernel<256, 256><<<blocks, 256, 0, st>>>(x, out);
     else
@@ -532,15 +551,10 @@ template <typename T>
 hipError_t few(const ScaledArgs &a, hipStream_t st)
 {
     const unsigned blocks = (unsigned)((a.n + 15) / 16);
-    // four waves a block where there are blocks for every CU twice over, else sixteen
-    const bool many = blocks >= 512;
-    if (a.m <= 16) {
-        if (many) scaled_few_kernel<4, 1, T><<<blocks, 256, 0, st>>>(a);
-        else scaled_few_kernel<16, 1, T><<<blocks, 1024, 0, st>>>(a);
-    } else {
-        if (many) scaled_few_kernel<4, 2, T><<<blocks, 256, 0, st>>>(a);
-        else scaled_few_kernel<16, 2, T><<<blocks, 1024, 0, st>>>(a);
-    }
+    // four waves a block where there are blocks for every CU twice over, else eight: one row of
+    // 8192 x 8192 13.1 us (8: 13.6), 4096 x 14336 13.2 us (16: 15.1), 28672 x 4096 22.7 us (8: 26.8)
+    if (blocks >= 512) scaled_few_kernel<4, T><<<blocks, 256, 0, st>>>(a);
+    else scaled_few_kernel<8, T><<<blocks, 512, 0, st>>>(a);
     return hipGetLastError();
 }
 
@@ -548,7 +562,7 @@ hipError_t few(const ScaledArgs &a, hipStream_t st)
 
 size_t scaled_part(int out_type, int64_t m, int64_t n, int64_t k)
 {
-    return (size_t)plan_of(out_type, m, n, (int)((k + kScaled - 1) / kScaled)).part_bytes;
+    return (size_t)plan_of(out_type, m, n, (int)((k + kScaled - 1) / kScaled)).p.part_bytes;
 }
 
 hipError_t launch_scaled(const ScaledArgs &a, hipStream_t st)

@@ -43,8 +43,8 @@ def test_tiles(kernels):
 def test_wide_copies(kernels):
     """The compiler places that kernel's matrix instructions; its copies are written out."""
     wide = {k: v for k, v in kernels.items() if "scaled_wide_kernel" in k}
-    assert len(wide) == 1
+    assert len(wide) == 2  # two tile sizes
     for name, code in wide.items():
-        assert sum(x.text.endswith(" lds") for x in code) == 3 * 9
+        assert sum(x.text.endswith(" lds") for x in code) in (3 * 9, 3 * 7)
         found = [f for f in faults(code) if "m0" in f]
         assert not found, found[:5]
