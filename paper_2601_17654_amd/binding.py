@@ -1241,11 +1241,11 @@ def _up(x: int, to: int) -> int:
     return -(-x // to) * to
 
 
-def _new_scaled(shape, rows: int, width: int):
-    """An empty Scaled, rows of a multiple of 16 bytes, and its kr_scaled."""
+def _new_scaled(x, shape, rows: int, width: int):
+    """An empty Scaled beside x, rows of a multiple of 16 bytes, and its kr_scaled."""
     room, lds = _up(width, 16), _up(rows, _SCALED)
-    q = _new(shape[:-1] + (room,), _E4M3)
-    scale = _new((_up(width, _SCALED) // _SCALED, lds), torch.uint8)
+    q = x.new_empty(shape if room == width else shape[:-1] + (room,), dtype=_E4M3)
+    scale = x.new_empty(((width + 127) // _SCALED, lds), dtype=torch.uint8)
     return (Scaled(q if room == width else q[..., :width], scale, room),
             KrScaled(q.data_ptr(), room, room, scale.data_ptr(), lds))
 
@@ -1302,8 +1302,8 @@ def scaled_hold(x, square: bool = False, plain: bool = True, crossed: bool = Fal
         raise ValueError("one of plain and crossed has to be asked for")
     xr, n, ldx = _rows(x, "x", dev)
     width = xr.shape[1]
-    p, pk = _new_scaled(x.shape, n, width) if plain else (None, None)
-    c, ck = _new_scaled((width, n), width, n) if crossed else (None, None)
+    p, pk = _new_scaled(x, x.shape, n, width) if plain else (None, None)
+    c, ck = _new_scaled(x, (width, n), width, n) if crossed else (None, None)
     _check("kr_scaled_hold",
            _lib.kr_scaled_hold(t, n, width, xr.data_ptr(), ldx, int(square), pk, ck,
                                _raw_stream(dev)))
