@@ -754,6 +754,37 @@ kr_status kr_scaled_matmul(const kr_scaled_product *p, int32_t type, void *out, 
 size_t kr_scaled_matmul_workspace(const kr_scaled_product *p);
 
 /*
+ * kr_scaled_linear -- out = x w^T, both held first: x by rows, w by squares (kr_scaled_hold), then
+ * their product (kr_scaled_matmul).  For a weight that stays, hold it once and call those two.
+ *   type          of x [rows][width], w [hidden][width] and out [rows][hidden]
+ * rows >= 0, width >= 1, hidden >= 1; KR_EUNSUPPORTED where one of the calls is.  out overlaps no
+ * input.  The workspace (16-byte aligned) holds the operands; 0: none needed, or an invalid argument.
+ */
+typedef struct kr_linear {
+    int32_t type;
+    int64_t rows, width, hidden;
+    const void *x, *w;
+    int64_t ldx, ldw;
+} kr_linear;
+kr_status kr_scaled_linear(const kr_linear *l, void *out, int64_t ldo, void *ws, size_t ws_bytes,
+                           void *stream);
+size_t kr_scaled_linear_workspace(const kr_linear *l);
+
+/*
+ * kr_scaled_linear_backward -- gradients of kr_scaled_linear from its inputs and the gradient dout of
+ * its output, holding taken as if it left values as they are.  Each product takes operands held
+ * along what it sums over:
+ *   dx = dout w       dout held by rows, w by squares (the values of the forward product)
+ *   dw = dout^T x     dout and x held by columns, blocks of 128 rows
+ * dx, dw   of the type, or NULL: not asked for; without rows dw is 0.  No output overlaps an input.
+ * KR_EUNSUPPORTED where one of the calls is (rows > 2^21 among them).
+ */
+kr_status kr_scaled_linear_backward(const kr_linear *l, const void *dout, int64_t lddo, void *dx,
+                                    int64_t lddx, void *dw, int64_t lddw, void *ws, size_t ws_bytes,
+                                    void *stream);
+size_t kr_scaled_linear_backward_workspace(const kr_linear *l);
+
+/*
  * kr_set_phase_events -- instrumentation for profilers and benchmarks (not part of the
  * method).  When both events are non-NULL, later calls record `start_event` on their
  * stream right before the phase's first kernel and `stop_event` right after its last

@@ -61,6 +61,12 @@ class KrScaledProduct(ctypes.Structure):
     _fields_ = [("m", _i64), ("n", _i64), ("k", _i64), ("a", KrScaled), ("b", KrScaled)]
 
 
+class KrLinear(ctypes.Structure):
+    _fields_ = [("type", _i32), ("rows", _i64), ("width", _i64), ("hidden", _i64), ("x", _vp),
+                ("w", _vp), ("ldx", _i64), ("ldw", _i64)]
+
+
+_LP = ctypes.POINTER(KrLinear)
 _HP, _PP = ctypes.POINTER(KrScaled), ctypes.POINTER(KrScaledProduct)
 _DP = ctypes.POINTER(KrDrop)
 _BP, _GP = ctypes.POINTER(KrBytes), ctypes.POINTER(KrGated)
@@ -125,6 +131,10 @@ _SIGS = {
     "kr_scaled_values": (_i32, [_i32, _i64, _i64, _HP, _vp, _i64, _vp]),
     "kr_scaled_matmul": (_i32, [_PP, _i32, _vp, _i64, _vp, _sz, _vp]),
     "kr_scaled_matmul_workspace": (_sz, [_PP]),
+    "kr_scaled_linear": (_i32, [_LP, _vp, _i64, _vp, _sz, _vp]),
+    "kr_scaled_linear_workspace": (_sz, [_LP]),
+    "kr_scaled_linear_backward": (_i32, [_LP, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _sz, _vp]),
+    "kr_scaled_linear_backward_workspace": (_sz, [_LP]),
     "kr_status_string": (ctypes.c_char_p, [_i32]),
     "kr_set_phase_events": (_i32, [_i32, _vp, _vp]),
 }
@@ -1358,52 +1368,59 @@ class _ScaledLinear(torch.autograd.Function):
         return scaled_linear_backward(dout, *ctx.saved_tensors, need=ctx.needs_input_grad)
 
 
-def _linear_weight(x, w):
+def _linear(x, w):
+    """kr_linear of x and w, the device, and what has to live."""
+    t = _type(x, "x")
     if not isinstance(w, torch.Tensor) or w.dtype != x.dtype:
         raise TypeError("w must be Scaled or a tensor of %s like x" % x.dtype)
     if w.dim() != 2 or w.shape[0] < 1 or w.shape[1] != x.shape[-1]:
         raise ValueError("w must be [hidden][%d], got %s" % (x.shape[-1], tuple(w.shape)))
+    dev = _here(x, "x")
+    xr, n, ldx = _rows(x, "x", dev)
+    width = xr.shape[1]
+    wr, hidden, ldw = _rows(w, "w", dev, width)
+    return KrLinear(t, n, width, hidden, xr.data_ptr(), wr.data_ptr(), ldx, ldw), dev, (xr, wr)
 
 
 def scaled_linear(x, w) -> torch.Tensor:
     """x w^T of x [..., width] and w [hidden][width], both held in 8-bit floating point first: x by
-    rows, w by squares; the result in x's type.  w may be Scaled (a weight that is held once, by
-    scaled_hold(w, square=True).plain); then there is no gradient.  Else the gradient reaches both,
-    holding taken as if it left values as they are."""
+    rows, w by squares; the result in x's type (kr_scaled_linear).  w may be Scaled (a weight that is
+    held once, by scaled_hold(w, square=True).plain); then there is no gradient.  Else the gradient
+    reaches both, holding taken as if it left values as they are."""
     if isinstance(w, Scaled):
         _no_gradient("scaled_linear with a weight that is held", x)
-    elif _tracked(x, w):
+        _type(x, "x")
+        return scaled_matmul(scaled_hold(x.detach()).plain, w, x.dtype)
+    if _tracked(x, w):
         return _ScaledLinear.apply(x, w)
-    _type(x, "x")
-    if not isinstance(w, Scaled):
-        _linear_weight(x, w)
-        w = scaled_hold(w.detach(), square=True).plain
-    return scaled_matmul(scaled_hold(x.detach()).plain, w, x.dtype)
+    l, dev, keep = _linear(x, w)
+    out = x.new_empty(x.shape[:-1] + (l.hidden,))
+    wsb = _lib.kr_scaled_linear_workspace(l)
+    ws, at = _scratch(wsb)
+    _check("kr_scaled_linear",
+           _lib.kr_scaled_linear(l, out.data_ptr(), l.hidden, at, wsb, _raw_stream(dev)))
+    return out
 
 
 def scaled_linear_backward(dout, x, w, need=(True, True)):
     """(dx, dw) of scaled_linear from its inputs and the gradient dout of its output.  Each of the two
     products takes operands held along what it sums over: dx = dout w, dout held by rows and w by
     squares, as forward; dw = dout^T x, both held by columns, 128 rows a block.  None where `need`
-    is false."""
-    _type(x, "x")
-    _linear_weight(x, w)
+    is false (kr_scaled_linear_backward)."""
+    l, dev, keep = _linear(x, w)
     if not isinstance(dout, torch.Tensor) or dout.dtype != x.dtype:
         raise TypeError("dout must be a tensor of %s" % x.dtype)
-    if dout.shape != x.shape[:-1] + (w.shape[0],):
-        raise ValueError("dout must be %s, got %s" % (tuple(x.shape[:-1]) + (w.shape[0],),
+    if dout.shape != x.shape[:-1] + (l.hidden,):
+        raise ValueError("dout must be %s, got %s" % (tuple(x.shape[:-1]) + (l.hidden,),
                                                       tuple(dout.shape)))
-    if x.numel() == 0:
-        return torch.empty_like(x) if need[0] else None, torch.zeros_like(w) if need[1] else None
-    x, w, dout = x.detach(), w.detach(), dout.detach()
-    if not need[0] and not need[1]:
-        return None, None
-    d = scaled_hold(dout, plain=bool(need[0]), crossed=bool(need[1]))
-    dx = dw = None
-    if need[0]:
-        wt = scaled_hold(w, square=True, plain=False, crossed=True).crossed
-        dx = scaled_matmul(d.plain, wt, x.dtype)
-    if need[1]:
-        xt = scaled_hold(x, plain=False, crossed=True).crossed
-        dw = scaled_matmul(d.crossed, xt, x.dtype)
+    dr, _, ldd = _rows(dout, "dout", dev, l.hidden)
+    dx = _new_like(x) if need[0] else None
+    dw = _new_like(w) if need[1] else None
+    wsb = _lib.kr_scaled_linear_backward_workspace(l)
+    ws, at = _scratch(wsb)
+    _check("kr_scaled_linear_backward",
+           _lib.kr_scaled_linear_backward(l, dr.data_ptr(), ldd,
+                                          None if dx is None else dx.data_ptr(), l.width,
+                                          None if dw is None else dw.data_ptr(), l.width, at, wsb,
+                                          _raw_stream(dev)))
     return dx, dw

@@ -475,9 +475,17 @@ bool scaled_ok(const kr_scaled_product *p)
            held_ok(&p->b, p->n, p->k);
 }
 
-bool scaled_fits(const kr_scaled_product *p)
+bool product_fits(int64_t m, int64_t n, int64_t k)
 {
-    return p->m <= kRowsMost && p->n <= kChannelsMost && p->k <= kRowMost && tiles_fit(p->m, p->n);
+    return m <= kRowsMost && n <= kChannelsMost && k <= kRowMost && tiles_fit(m, n);
+}
+
+bool scaled_fits(const kr_scaled_product *p) { return product_fits(p->m, p->n, p->k); }
+
+bool hold_fits(int64_t rows, int64_t width)
+{
+    return rows <= kHeldMost && width <= kHeldMost &&
+           up(rows, kScaled) / kScaled * (up(width, kScaled) / kScaled) <= kTilesMost;
 }
 
 kr_status scaled_run(const kr_scaled_product *p, int32_t type, void *out, int64_t ldo, Carve &c,
@@ -511,9 +519,7 @@ extern "C" kr_status kr_scaled_hold(int32_t type, int64_t rows, int64_t width, c
 {
     if (!type_ok(type) || rows < 0 || width < 1 || (square != 0 && square != 1) || (!plain && !crossed))
         return KR_EINVAL;
-    if (rows > kHeldMost || width > kHeldMost ||
-        up(rows, kScaled) / kScaled * (up(width, kScaled) / kScaled) > kTilesMost)
-        return KR_EUNSUPPORTED;
+    if (!hold_fits(rows, width)) return KR_EUNSUPPORTED;
     if (rows == 0) return KR_OK;
     if (!matrix_ok(x, ldx, width, size_of(type)) ||
         (plain && (!held_ok(plain, rows, width) || plain->room > up(width, kScaled))) ||
@@ -558,4 +564,136 @@ extern "C" kr_status kr_scaled_matmul(const kr_scaled_product *p, int32_t type, 
     if (!ws_ok(ws, ws_bytes, kr_scaled_matmul_workspace(p))) return KR_ECAPACITY;
     Carve c{(char *)ws};
     return scaled_run(p, type, out, ldo, c, (hipStream_t)stream);
+}
+
+namespace {
+
+bool linear_ok(const kr_linear *l)
+{
+    return l && type_ok(l->type) && l->rows >= 0 && l->width >= 1 && l->hidden >= 1 &&
+           (l->rows == 0 || matrix_ok(l->x, l->ldx, l->width, size_of(l->type))) &&
+           matrix_ok(l->w, l->ldw, l->width, size_of(l->type));
+}
+
+bool linear_fits(const kr_linear *l)
+{
+    return product_fits(l->rows, l->hidden, l->width) && hold_fits(l->rows, l->width) &&
+           hold_fits(l->hidden, l->width);
+}
+
+bool linear_back_fits(const kr_linear *l)
+{
+    return linear_fits(l) && product_fits(l->rows, l->width, l->hidden) &&
+           product_fits(l->hidden, l->width, l->rows) && hold_fits(l->rows, l->hidden);
+}
+
+// Room for a held matrix, rows of a multiple of 16 bytes, in a workspace.
+kr_scaled held_room(int64_t rows, int64_t width, Carve &c)
+{
+    const int64_t room = padded(width), lds = up(rows, kScaled);
+    kr_scaled h{};
+    h.ld = h.room = room;
+    h.lds = lds;
+    h.q = c.take(rows * room);
+    h.scale = c.take(up(width, kScaled) / kScaled * lds);
+    return h;
+}
+
+hipError_t hold_into(int32_t type, int64_t rows, int64_t width, const void *x, int64_t ldx, bool square,
+                     const kr_scaled *plain, const kr_scaled *crossed, hipStream_t st)
+{
+    HoldArgs a{rows, width, x, ldx, {}, {}, up(width, kScaled) / kScaled};
+    if (plain) a.plain = held(plain);
+    if (crossed) a.crossed = held(crossed);
+    return launch_hold(type, square, a, st);
+}
+
+// c.base null: sizes alone.
+kr_status linear_run(const kr_linear *l, void *out, int64_t ldo, Carve &c, hipStream_t st)
+{
+    const kr_scaled x = held_room(l->rows, l->width, c), w = held_room(l->hidden, l->width, c);
+    const kr_scaled_product p{l->rows, l->hidden, l->width, x, w};
+    if (!c.base) return scaled_run(&p, l->type, nullptr, 0, c, st);
+    hipError_t e = hold_into(l->type, l->rows, l->width, l->x, l->ldx, false, &x, nullptr, st);
+    if (e == hipSuccess)
+        e = hold_into(l->type, l->hidden, l->width, l->w, l->ldw, true, &w, nullptr, st);
+    return e == hipSuccess ? scaled_run(&p, l->type, out, ldo, c, st) : said(e);
+}
+
+kr_status linear_back_run(const kr_linear *l, const void *dout, int64_t ldd, void *dx, int64_t lddx,
+                          void *dw, int64_t lddw, Carve &c, hipStream_t st)
+{
+    const bool for_x = !c.base || dx, for_w = !c.base || dw;
+    kr_scaled d{}, dt{}, wt{}, xt{};
+    if (for_x) {
+        d = held_room(l->rows, l->hidden, c);
+        wt = held_room(l->width, l->hidden, c);
+    }
+    if (for_w) {
+        dt = held_room(l->hidden, l->rows, c);
+        xt = held_room(l->width, l->rows, c);
+    }
+    const kr_scaled_product px{l->rows, l->width, l->hidden, d, wt}, pw{l->hidden, l->width, l->rows, dt, xt};
+    if (!c.base) {
+        scaled_run(&px, l->type, nullptr, 0, c, st);
+        return scaled_run(&pw, l->type, nullptr, 0, c, st);
+    }
+    hipError_t e = hold_into(l->type, l->rows, l->hidden, dout, ldd, false, for_x ? &d : nullptr,
+                             for_w ? &dt : nullptr, st);
+    if (e == hipSuccess && for_x)
+        e = hold_into(l->type, l->hidden, l->width, l->w, l->ldw, true, nullptr, &wt, st);
+    if (e == hipSuccess && for_w)
+        e = hold_into(l->type, l->rows, l->width, l->x, l->ldx, false, nullptr, &xt, st);
+    kr_status s = said(e);
+    if (s == KR_OK && for_x) s = scaled_run(&px, l->type, dx, lddx, c, st);
+    if (s == KR_OK && for_w) s = scaled_run(&pw, l->type, dw, lddw, c, st);
+    return s;
+}
+
+}  // namespace
+
+extern "C" size_t kr_scaled_linear_workspace(const kr_linear *l)
+{
+    if (!linear_ok(l) || !linear_fits(l) || l->rows == 0) return 0;
+    Carve c{nullptr};
+    linear_run(l, nullptr, 0, c, nullptr);
+    return c.used;
+}
+
+extern "C" kr_status kr_scaled_linear(const kr_linear *l, void *out, int64_t ldo, void *ws,
+                                      size_t ws_bytes, void *stream)
+{
+    if (!linear_ok(l)) return KR_EINVAL;
+    if (!linear_fits(l)) return KR_EUNSUPPORTED;
+    if (l->rows == 0) return KR_OK;
+    if (!matrix_ok(out, ldo, l->hidden, size_of(l->type)) || (uintptr_t)ws % 16) return KR_EINVAL;
+    if (!ws_ok(ws, ws_bytes, kr_scaled_linear_workspace(l))) return KR_ECAPACITY;
+    Carve c{(char *)ws};
+    return linear_run(l, out, ldo, c, (hipStream_t)stream);
+}
+
+extern "C" size_t kr_scaled_linear_backward_workspace(const kr_linear *l)
+{
+    if (!linear_ok(l) || !linear_back_fits(l) || l->rows == 0) return 0;
+    Carve c{nullptr};
+    linear_back_run(l, nullptr, 0, nullptr, 0, nullptr, 0, c, nullptr);
+    return c.used;
+}
+
+extern "C" kr_status kr_scaled_linear_backward(const kr_linear *l, const void *dout, int64_t lddo, void *dx,
+                                               int64_t lddx, void *dw, int64_t lddw, void *ws,
+                                               size_t ws_bytes, void *stream)
+{
+    if (!linear_ok(l)) return KR_EINVAL;
+    if (!linear_back_fits(l)) return KR_EUNSUPPORTED;
+    const size_t es = size_of(l->type);
+    if ((l->rows > 0 && (!matrix_ok(dout, lddo, l->hidden, es) || (dx && !matrix_ok(dx, lddx, l->width, es)))) ||
+        (dw && !matrix_ok(dw, lddw, l->width, es)) || (uintptr_t)ws % 16)
+        return KR_EINVAL;
+    if (l->rows == 0) return dw ? said(launch_zeros(dw, lddw * es, l->hidden, l->width * es, (hipStream_t)stream))
+                               : KR_OK;
+    if (!dx && !dw) return KR_OK;
+    if (!ws_ok(ws, ws_bytes, kr_scaled_linear_backward_workspace(l))) return KR_ECAPACITY;
+    Carve c{(char *)ws};
+    return linear_back_run(l, dout, lddo, dx, lddx, dw, lddw, c, (hipStream_t)stream);
 }

@@ -81,6 +81,9 @@ struct HeldValuesArgs {
 };
 hipError_t launch_held_values(int dtype, const HeldValuesArgs &a, hipStream_t st);
 
+// Zeros to rows of `bytes` bytes.
+hipError_t launch_zeros(void *p, int64_t ld, int64_t rows, int64_t bytes, hipStream_t st);
+
 struct ScaledArgs {
     int out_type;
     int64_t m, n, k;

@@ -319,7 +319,19 @@ hipError_t values(HeldValuesArgs a, hipStream_t st)
     return hipGetLastError();
 }
 
+__global__ __launch_bounds__(256) void zeros_kernel(char *p, int64_t ld, int64_t rows, int64_t bytes)
+{
+    for (int64_t r = blockIdx.x; r < rows; r += gridDim.x)
+        for (int64_t c = threadIdx.x * 2; c < bytes; c += 512) *(uint16_t *)(p + r * ld + c) = 0;
+}
+
 }  // namespace
+
+hipError_t launch_zeros(void *p, int64_t ld, int64_t rows, int64_t bytes, hipStream_t st)
+{
+    zeros_kernel<<<(unsigned)std::min<int64_t>(rows, 4096), 256, 0, st>>>((char *)p, ld, rows, bytes);
+    return hipGetLastError();
+}
 
 hipError_t launch_hold(int dtype, bool square, const HoldArgs &a, hipStream_t st)
 {

@@ -104,13 +104,12 @@ def test_binding():
     for call in (lambda: b.scaled_hold(x.double()), lambda: b.scaled_hold([1.0]),
                  lambda: b.scaled_values(x), lambda: b.scaled_values(good, torch.int8),
                  lambda: b.scaled_matmul(x, good), lambda: b.scaled_matmul(good, good, torch.float64),
-                 lambda: b.scaled_linear(x, x.half()), lambda: b.scaled_linear(x.long(), x.long()),
-                 lambda: b.scaled_linear_backward(x.half(), x, x)):
+                 lambda: b.scaled_linear(x, x.half()), lambda: b.scaled_linear(x.long(), x.long())):
         with pytest.raises(TypeError):
             call()
     for call in (lambda: b.scaled_hold(x), lambda: b.scaled_matmul(good, good),
                  lambda: b.scaled_linear(x, x[:, :299]), lambda: b.scaled_linear(x, x[0]),
-                 lambda: b.scaled_linear_backward(x, x, x)):
+                 lambda: b.scaled_linear(x, x), lambda: b.scaled_linear_backward(x, x, x[:, 1:])):
         with pytest.raises(ValueError):
             call()
 
@@ -121,3 +120,47 @@ def test_one_row_with_room():
     scale = torch.zeros(3, 128, dtype=torch.uint8)
     k = b._held(b.Scaled(store[:, :300], scale, 304), "h", -1)[0]
     assert (k.ld, k.room) == (304, 304)
+
+
+def linear(**bad):
+    v = dict(type=BF16, rows=40, width=72, hidden=56, x=16, w=16, ldx=72, ldw=72)
+    return b.KrLinear(*{**v, **bad}.values())
+
+
+LINEAR_BAD = [dict(type=3), dict(rows=-1), dict(width=0), dict(hidden=0), dict(x=0), dict(w=0), dict(x=17),
+              dict(w=17), dict(ldx=71), dict(ldw=71)]
+
+
+@pytest.mark.parametrize("bad", LINEAR_BAD)
+def test_linear(bad):
+    l = linear(**bad)
+    assert L.kr_scaled_linear_workspace(l) == 0 and L.kr_scaled_linear_backward_workspace(l) == 0
+    assert L.kr_scaled_linear(l, 16, 56, 16, 1 << 30, None) == b.KR_EINVAL
+    assert L.kr_scaled_linear_backward(l, 16, 56, 16, 72, 16, 72, 16, 1 << 30, None) == b.KR_EINVAL
+
+
+def test_linear_arguments():
+    l = linear()
+    need, back = L.kr_scaled_linear_workspace(l), L.kr_scaled_linear_backward_workspace(l)
+    # the operands, a byte a value and a byte for each block of a row
+    assert need >= 40 * 80 + 128 + 56 * 80 + 128 and back >= 2 * (40 * 64 + 72 * 64)
+    for out, ldo, ws in ((None, 56, 16), (17, 56, 16), (16, 55, 16), (16, 56, 24)):
+        assert L.kr_scaled_linear(l, out, ldo, ws, need, None) == b.KR_EINVAL
+    assert L.kr_scaled_linear(l, 16, 56, 16, need - 1, None) == b.KR_ECAPACITY
+    assert L.kr_scaled_linear(l, 16, 56, None, need, None) == b.KR_ECAPACITY
+    good = [16, 56, 16, 72, 16, 72, 16, back]
+    for at, value, says in ((0, None, b.KR_EINVAL), (0, 17, b.KR_EINVAL), (1, 55, b.KR_EINVAL),
+                            (2, 17, b.KR_EINVAL), (3, 71, b.KR_EINVAL), (4, 17, b.KR_EINVAL),
+                            (5, 71, b.KR_EINVAL), (6, 24, b.KR_EINVAL), (6, None, b.KR_ECAPACITY),
+                            (7, back - 1, b.KR_ECAPACITY)):
+        bad = list(good)
+        bad[at] = value
+        assert L.kr_scaled_linear_backward(l, *bad, None) == says, (at, value)
+    none = linear(rows=0, x=0)
+    assert L.kr_scaled_linear(none, None, 0, None, 0, None) == b.KR_OK
+    assert L.kr_scaled_linear_backward(none, None, 0, None, 0, None, 0, None, 0, None) == b.KR_OK
+    wide = linear(width=(1 << 21) + 1, ldx=1 << 22, ldw=1 << 22)
+    assert L.kr_scaled_linear(wide, 16, 56, 16, 1 << 40, None) == b.KR_EUNSUPPORTED
+    tall = linear(rows=(1 << 21) + 1)
+    assert L.kr_scaled_linear_workspace(tall) > 0 and L.kr_scaled_linear_backward_workspace(tall) == 0
+    assert L.kr_scaled_linear_backward(tall, *good, None) == b.KR_EUNSUPPORTED
