@@ -101,35 +101,40 @@ __global__ __launch_bounds__(256) void hold_rows_kernel(HoldArgs a)
     }
 }
 
-// A block of 256 threads takes a tile of 128 x 128: thread (cg, rg) eight columns from 8 cg on of the
-// eight rows from 8 rg on.  Both forms come of one read: the plain one's bytes go straight out, the
-// crossed one's through LDS, where 8-byte chunk rg of column c lies at place rg ^ c / 8.  Values stay
-// as they were loaded and are converted twice, for the largest and to be held: half the registers.
+// A block of 512 threads takes a tile of 128 x 128: thread (cg, rg) eight columns from 8 cg on of the four
+// rows from 4 rg on.  Both forms come of one read: the plain one's bytes go straight out, the crossed
+// one's through LDS, where 4-byte chunk rg of column c lies at place rg ^ 2 (c / 8).  Values stay as they
+// were loaded and are converted twice, for the largest and to be held: half the registers.  (With eight
+// rows a thread a block alone on its CU, which small matrices have, waited for its instructions: 1000 x
+// 1500 both forms 12.7 us, now 8.)
+constexpr int kHoldThreads = 512;
+
 template <typename T, bool SQUARE, bool PLAIN, bool CROSSED>
-__global__ __launch_bounds__(256) void hold_kernel(HoldArgs a)
+__global__ __launch_bounds__(kHoldThreads) void hold_kernel(HoldArgs a)
 {
-    __shared__ uint32_t tops[CROSSED && !SQUARE ? 4 * kScaled : 4];
-    __shared__ __align__(16) uint8_t bytes[2][kScaled];
+    constexpr int WAVES = kHoldThreads / 64, ROWS = 4;
+    __shared__ uint32_t tops[CROSSED && !SQUARE ? WAVES * kScaled : WAVES];
+    __shared__ __align__(16) uint8_t bytes[2][kScaled], of_column[kScaled];
     __shared__ __align__(16) uint8_t turned[CROSSED ? kScaled * kScaled : 16];
     const int t = threadIdx.x, cg = t % 16, rg = t / 16, wave = t / 64;
     const int64_t tile_r = blockIdx.x / a.tiles_c, tile_c = blockIdx.x - tile_r * a.tiles_c;
-    const int64_t r0 = tile_r * kScaled + rg * 8, c0 = tile_c * kScaled + cg * 8;
+    const int64_t r0 = tile_r * kScaled + rg * ROWS, c0 = tile_c * kScaled + cg * 8;
 
-    Eight<T> x[8];
+    Eight<T> x[ROWS];
     if ((tile_r + 1) * kScaled <= a.rows && (tile_c + 1) * kScaled <= a.width) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
+        for (int i = 0; i < ROWS; ++i)
             x[i].template load<true>((const T *)a.x + (r0 + i) * a.ldx, c0, a.width);
     } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < ROWS; ++i) {
             if (r0 + i < a.rows) x[i].template load<false>((const T *)a.x + (r0 + i) * a.ldx, c0, a.width);
             else x[i].none();
         }
     }
-    uint32_t row_top[8], column_top[8] = {};
+    uint32_t row_top[ROWS], column_top[8] = {};
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < ROWS; ++i) {
         row_top[i] = 0;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
@@ -142,30 +147,33 @@ __global__ __launch_bounds__(256) void hold_kernel(HoldArgs a)
     if (SQUARE) {
         uint32_t top = 0;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) top = max(top, row_top[i]);
+        for (int i = 0; i < ROWS; ++i) top = max(top, row_top[i]);
 #pragma unroll
         for (int o = 32; o; o >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o));
         if (t % 64 == 0) tops[wave] = top;
         __syncthreads();
-        square_byte = scale_byte(max(max(tops[0], tops[1]), max(tops[2], tops[3])));
+        top = tops[t % WAVES];
+#pragma unroll
+        for (int o = WAVES / 2; o; o >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o));
+        square_byte = scale_byte(top);
     } else if (CROSSED) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             column_top[e] = max(column_top[e], (uint32_t)__shfl_xor((int)column_top[e], 16));
             column_top[e] = max(column_top[e], (uint32_t)__shfl_xor((int)column_top[e], 32));
-            if (rg % 4 == 0) tops[wave * kScaled + cg * 8 + e] = column_top[e];
+            if (t % 64 < 16) tops[wave * kScaled + cg * 8 + e] = column_top[e];
         }
     }
     if (PLAIN) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < ROWS; ++i) {
             if (!SQUARE) {
 #pragma unroll
                 for (int o = 8; o; o >>= 1)
                     row_top[i] = max(row_top[i], (uint32_t)__shfl_xor((int)row_top[i], o));
             }
             const uint32_t byte = SQUARE ? square_byte : scale_byte(row_top[i]);
-            const int row = rg * 8 + i;
+            const int row = rg * ROWS + i;
             if (cg == 0) bytes[0][row % 16 * 8 + row / 16] = r0 + i < a.rows ? (uint8_t)byte : 0;
             x[i].again();
             const Loose8 q = x[i].held(scale_inverse(byte), byte == 255);
@@ -175,27 +183,28 @@ __global__ __launch_bounds__(256) void hold_kernel(HoldArgs a)
     }
     if (CROSSED) {
         if (!SQUARE) __syncthreads();
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[i].again();
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
+        if (t < kScaled) {
             uint32_t byte = square_byte;
             if (!SQUARE) {
                 uint32_t top = 0;
 #pragma unroll
-                for (int w = 0; w < 4; ++w) top = max(top, tops[w * kScaled + cg * 8 + e]);
+                for (int w = 0; w < WAVES; ++w) top = max(top, tops[w * kScaled + t]);
                 byte = scale_byte(top);
+                of_column[t] = (uint8_t)byte;
             }
-            const float f = scale_inverse(byte);
-            const bool none = byte == 255;
-            const int column = cg * 8 + e;
-            i32x2 q;
+            bytes[1][t % 16 * 8 + t / 16] = tile_c * kScaled + t < a.width ? (uint8_t)byte : 0;
+        }
+        if (!SQUARE) __syncthreads();
+        const i32x2 mine = SQUARE ? i32x2{0, 0} : *(const i32x2 *)(of_column + cg * 8);
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
-                q[h] = none ? 0 : (int)hold4(x[h * 4].at(e) * f, x[h * 4 + 1].at(e) * f,
-                                             x[h * 4 + 2].at(e) * f, x[h * 4 + 3].at(e) * f);
-            if (rg == 0) bytes[1][column % 16 * 8 + column / 16] = c0 + e < a.width ? (uint8_t)byte : 0;
-            *(i32x2 *)(turned + column * kScaled + ((rg ^ cg) << 3)) = q;
+        for (int i = 0; i < ROWS; ++i) x[i].again();
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const uint32_t byte = SQUARE ? square_byte : (uint32_t)mine[e / 4] >> (e % 4 * 8) & 255;
+            const float f = scale_inverse(byte);
+            const uint32_t q = byte == 255 ? 0 : hold4(x[0].at(e) * f, x[1].at(e) * f, x[2].at(e) * f,
+                                                       x[3].at(e) * f);
+            *(uint32_t *)(turned + (cg * 8 + e) * kScaled + ((rg ^ 2 * cg) << 2)) = q;
         }
     }
     __syncthreads();
@@ -206,15 +215,13 @@ __global__ __launch_bounds__(256) void hold_kernel(HoldArgs a)
         if (t >= 64 && t < 64 + kScaled / 4)
             *(uint32_t *)(a.crossed.scale + tile_r * a.crossed.lds + tile_c * kScaled + (t - 64) * 4) =
                 *(const uint32_t *)(bytes[1] + (t - 64) * 4);
-        // 8 lanes a column: 128 bytes.  Chunks 2 i and 2 i + 1 lie side by side, in turn where c / 8
-        // is odd.
+        // 8 lanes a column: 128 bytes.  Of 16 bytes the halves are in turn where c / 8 is odd.
 #pragma unroll
-        for (int p = 0; p < 4; ++p) {
-            const int c = p * 32 + t / 8, pair = t % 8, odd = c / 8 % 2;
-            const int64_t column = tile_c * kScaled + c, r = tile_r * kScaled + pair * 16;
-            const Loose16 w = *(const Loose16 *)(turned + c * kScaled + ((pair ^ c / 16) << 4));
-            Loose16 q = w;
-            if (odd) q.v = w.v.zwxy;
+        for (int p = 0; p < kScaled * 8 / kHoldThreads; ++p) {
+            const int c = p * (kHoldThreads / 8) + t / 8, part = t % 8;
+            const int64_t column = tile_c * kScaled + c, r = tile_r * kScaled + part * 16;
+            Loose16 q = *(const Loose16 *)(turned + c * kScaled + ((part ^ c / 16) << 4));
+            if (c / 8 % 2) q.v = q.v.zwxy;
             if (column >= a.width) continue;
             char *to = a.crossed.q + column * a.crossed.ld;
             if (r + 16 <= a.crossed.bytes) {
@@ -250,9 +257,9 @@ template <typename T, bool SQUARE>
 hipError_t hold(const HoldArgs &a, hipStream_t st)
 {
     const unsigned blocks = (unsigned)((a.rows + kScaled - 1) / kScaled * a.tiles_c);
-    if (a.plain.q && a.crossed.q) hold_kernel<T, SQUARE, true, true><<<blocks, 256, 0, st>>>(a);
-    else if (a.crossed.q) hold_kernel<T, SQUARE, false, true><<<blocks, 256, 0, st>>>(a);
-    else if constexpr (SQUARE) hold_kernel<T, true, true, false><<<blocks, 256, 0, st>>>(a);
+    if (a.plain.q && a.crossed.q) hold_kernel<T, SQUARE, true, true><<<blocks, kHoldThreads, 0, st>>>(a);
+    else if (a.crossed.q) hold_kernel<T, SQUARE, false, true><<<blocks, kHoldThreads, 0, st>>>(a);
+    else if constexpr (SQUARE) hold_kernel<T, true, true, false><<<blocks, kHoldThreads, 0, st>>>(a);
     else return hold_rows<T>(a, st);
     return hipGetLastError();
 }
