@@ -5,8 +5,11 @@ addition, gated projection), backward (their gradients) and the forward form in 
 (norm held in bytes, byte product) -- times each, expands the times to the planner's tables and
 plans two steps: training (forward and backward) and a forward step in 8 bits.  For either it
 prints the time-energy frontier's size and the schedule of its fastest and its cheapest point.
+With --block layer_norm the block is of the other common kind, in 8-bit floating point: layer norm
+with dropout and the residual's addition, a linear layer, and their gradients; one training step.
 
     python examples/plan_block.py [--rows 8192] [--width 4096] [--hidden 14336] [--layers 16]
+                                  [--block rms_norm|layer_norm]
 
 What is measured is each kernel's time with all compute units at the clock of the moment.  How a
 time changes with frequency and with units given to communication is the table generator's
@@ -85,9 +88,39 @@ def run_block(rows, width, hidden, repeats=10):
     return {k: (t[k], per_byte[k]) for k in t}, r
 
 
+def run_layer_norm_block(rows, width, hidden, repeats=10, p=0.1):
+    """The same of a block with layer norm, dropout and a linear layer in 8-bit floating point."""
+    gen = torch.Generator(device="cuda").manual_seed(0)
+
+    def normal(*shape):
+        return torch.randn(*shape, generator=gen, device="cuda").to(torch.bfloat16)
+
+    x, residual, dout, dsum = (normal(rows, width), normal(rows, width), normal(rows, hidden),
+                               normal(rows, width))
+    weight, bias = torch.ones_like(x[0]), torch.zeros_like(x[0])
+    w = normal(hidden, width) / width ** 0.5
+    drop = dict(p=p, seed=1, offset=0)
+    t, r = {}, {}
+    t["layer_norm"], r["layer_norm"] = measure(
+        lambda: kr.add_layer_norm(x, weight, bias, residual, **drop), repeats)
+    n = r["layer_norm"]
+    t["linear"], r["linear"] = measure(lambda: kr.scaled_linear(n.out, w), repeats)
+    t["linear_back"], r["linear_back"] = measure(
+        lambda: kr.scaled_linear_backward(dout, n.out, w), repeats)
+    dn = r["linear_back"][0]
+    t["layer_norm_back"], r["layer_norm_back"] = measure(
+        lambda: kr.add_layer_norm_backward(dn, n.sum, weight, n.mean, n.rstd, dsum, **drop), repeats)
+    mw, wh, mh = rows * width, width * hidden, rows * hidden
+    per_byte = {"layer_norm": 8 * mw / (8.0 * mw), "layer_norm_back": 14 * mw / (10.0 * mw),
+                "linear": mw * hidden / (2.0 * (mw + wh + mh)),  # 8 bits: half the cost each
+                "linear_back": 2.0 * mw * hidden / (2.0 * (2 * mw + 2 * wh + mh))}
+    return {k: (t[k], per_byte[k]) for k in t}, r
+
+
 # The block's partitions: kernels that run beside one collective each.
 PARTITIONS = (("norm", "gated"), ("gated_back", "norm_back"), ("norm_bytes", "bytes"))
 TRAINING, BYTES_FORWARD = PARTITIONS[:2], PARTITIONS[2:]  # those of one step
+LAYER_NORM = (("layer_norm", "linear"), ("linear_back", "layer_norm_back"))
 
 
 def tables(times, layers, rows, width, partitions=PARTITIONS):
@@ -128,12 +161,18 @@ def main(argv=None):
     ap.add_argument("--width", type=int, default=4096)
     ap.add_argument("--hidden", type=int, default=14336)
     ap.add_argument("--layers", type=int, default=16)
+    ap.add_argument("--block", choices=("rms_norm", "layer_norm"), default="rms_norm")
     a = ap.parse_args(argv)
-    times, _ = run_block(a.rows, a.width, a.hidden)
+    if a.block == "rms_norm":
+        times, _ = run_block(a.rows, a.width, a.hidden)
+        steps = (("training step", TRAINING), ("forward step in 8 bits", BYTES_FORWARD))
+    else:
+        times, _ = run_layer_norm_block(a.rows, a.width, a.hidden)
+        steps = (("training step", LAYER_NORM),)
     for name, (s, per_byte) in times.items():
-        print("%-11s %9.1f us   %7.1f operations a byte" % (name, s * 1e6, per_byte))
+        print("%-16s %9.1f us   %7.1f operations a byte" % (name, s * 1e6, per_byte))
     plans = []
-    for name, partitions in (("training step", TRAINING), ("forward step in 8 bits", BYTES_FORWARD)):
+    for name, partitions in steps:
         space, tabs = tables(times, a.layers, a.rows, a.width, partitions)
         T, E, sched = plan(space, tabs)
         plans.append((T, E, sched))

@@ -18,8 +18,9 @@
  *  - the launch-timing frontier of two operation sequences (Appendix B);
  *  - the evaluation's frontier comparison metrics (Section 6.1);
  *  - the compute kernels of a transformer block's partition on this card, so that a plan
- *    can be made from measured times: norm with the residual's addition, gated
- *    projection, their backward passes, and the forward form in 8-bit integers.
+ *    can be made from measured times: norms (root-mean-square, layer) with the residual's
+ *    addition, dropout, gated projection, products of values held in 8-bit floating point,
+ *    their backward passes, and a forward form in 8-bit integers.
  *
  * Conventions for every entry point
  *  - Array arguments are DEVICE pointers unless marked "host".  The caller owns and
@@ -612,7 +613,7 @@ kr_status kr_add_layer_norm(int32_t type, int64_t rows, int64_t width, const voi
  *   dweight = sum over rows of dout * h,  dbias = sum over rows of dout
  *   dsum       gradient that reaches s by the residual's path, or NULL: 0
  *   drop       as it was forward
- *   dresidual  may be dout or dsum itself
+ *   dresidual, dx   may be dout or dsum themselves, not each other
  *   dx         NULL where nothing is dropped (drop NULL or p below 2^-17): dresidual is x's gradient
  *              too.  D is taken of the unrounded dresidual.
  *   dweight    float [width]; 0 where there are no rows
@@ -699,6 +700,8 @@ size_t kr_gated_projection_backward_workspace(const kr_gated *g);
  * rows.  With t a block's largest magnitude,
  *   e = the least whole number >= -127 with t <= 448 * 2^e,  q = x * 2^-e to the nearest, ties to even
  * and the value held is q * 2^e.  A block with a NaN or an infinity holds q = 0 and has the scale NaN.
+ * (A power of two costs nothing against a scale in 32 bits: a floating-point value keeps its relative
+ * precision under any scale.  It makes holding one rounding, and the matrix cores apply it.)
  *   q       [rows][width], a byte a value, rows `ld` bytes apart
  *   room    bytes of each row, width or more and at most ld, that are written when values are held
  *           and may be read by a product: those past width are 0.  (A product copies operands whose
@@ -738,7 +741,8 @@ kr_status kr_scaled_values(int32_t type, int64_t rows, int64_t width, const kr_s
  * round as 32-bit sums do; where it is of 16 bits, the matrix cores' 8-bit instruction adds, which
  * brings eight neighbouring products to the largest one's exponent and cuts off what is below 2^-13 of
  * that power of two: sums are off by up to 2^-10 of their terms' magnitudes (1.5e-5 relative on
- * normal values), before a rounding of 2^-12 or 2^-9.
+ * normal values), before a rounding of 2^-11 or 2^-8.  What is below 2^-126, a value, a product or a sum,
+ * may be taken as 0.
  *   a [m][k], b [n][k]   m >= 0, n >= 1, k >= 1
  *   type                 of out
  * KR_EUNSUPPORTED for m >= 2^31, n > 2^27, k > 2^21 or an output of more than 2^23 tiles of 128 x 64.

@@ -1,20 +1,17 @@
 // Dropout: out = kept x / (1 - p) (+ residual), the mask computed from counters (kr_drop.h) and stored
-// nowhere; of a gradient the same call gives the gradient.
+// nowhere; of a gradient the same call gives the gradient.  A thread takes eight neighbours, whose random
+// bits come of one counter.
+//
+// Bound by memory: 8192 x 14336 in bfloat16 81 us (5.8 TB/s of its 470 MB), in float32 161 us (5.9 TB/s).
 #include "kr_drop.h"
+#include "kr_rows.h"
 
 namespace kr {
 
 namespace {
 
-// TPR threads share a row, one group of eight values each, and take its groups in turn.
-struct DropoutShape {
-    int log_tpr;      // threads a row: 1, 2, .. 256
-    uint32_t groups;  // of a row
-    uint32_t chunks;  // blocks a row
-};
-
 template <typename T, bool RES, bool DROP>
-__global__ __launch_bounds__(256) void dropout_kernel(DropoutArgs a, DropoutShape s)
+__global__ __launch_bounds__(256) void dropout_kernel(DropoutArgs a, Dealt s)
 {
     constexpr int V = kVec<T>, NV = kDropGroup / V;
     const int64_t block = blockIdx.x / s.chunks;
@@ -57,10 +54,7 @@ __global__ __launch_bounds__(256) void dropout_kernel(DropoutArgs a, DropoutShap
 template <typename T>
 hipError_t typed(DropoutArgs a, hipStream_t st)
 {
-    DropoutShape s{};
-    s.groups = (uint32_t)((a.width + kDropGroup - 1) / kDropGroup);
-    while (s.log_tpr < 8 && (1u << s.log_tpr) < s.groups) ++s.log_tpr;
-    s.chunks = (s.groups + (1u << s.log_tpr) - 1) >> s.log_tpr;
+    const Dealt s = dealt((a.width + kDropGroup - 1) / kDropGroup);
     // a grid has fewer than 2^32 threads
     const int64_t most = std::max<int64_t>(1, (1 << 23) / s.chunks) << (8 - s.log_tpr);
     const int64_t rows = a.rows;

@@ -270,14 +270,13 @@ template <typename T>
 constexpr int kBack = sizeof(T) == 4 ? 4 : 16;
 
 template <typename T>
-__global__ __launch_bounds__(256) void held_values_kernel(HeldValuesArgs a, uint32_t log_tpr,
-                                                          uint32_t chunks)
+__global__ __launch_bounds__(256) void held_values_kernel(HeldValuesArgs a, Dealt s)
 {
     constexpr int N = kBack<T>;
-    const int64_t block = blockIdx.x / chunks;
-    const uint32_t chunk = blockIdx.x - (uint32_t)block * chunks;
-    const int64_t row = (block << (8 - log_tpr)) + (threadIdx.x >> log_tpr);
-    const int64_t c = (((int64_t)chunk << log_tpr) + (threadIdx.x & ((1u << log_tpr) - 1))) * N;
+    const int64_t block = blockIdx.x / s.chunks;
+    const uint32_t chunk = blockIdx.x - (uint32_t)block * s.chunks;
+    const int64_t row = (block << (8 - s.log_tpr)) + (threadIdx.x >> s.log_tpr);
+    const int64_t c = (((int64_t)chunk << s.log_tpr) + (threadIdx.x & ((1u << s.log_tpr) - 1))) * N;
     if (row >= a.rows || c >= a.width) return;
     struct __attribute__((packed)) Loose {
         int v[N / 4];
@@ -307,18 +306,15 @@ __global__ __launch_bounds__(256) void held_values_kernel(HeldValuesArgs a, uint
 template <typename T>
 hipError_t values(HeldValuesArgs a, hipStream_t st)
 {
-    const int64_t groups = (a.width + kBack<T> - 1) / kBack<T>;
-    uint32_t log_tpr = 0;
-    while (log_tpr < 8 && (1 << log_tpr) < groups) ++log_tpr;
-    const uint32_t chunks = (uint32_t)((groups + (1 << log_tpr) - 1) >> log_tpr);
+    const Dealt s = dealt((a.width + kBack<T> - 1) / kBack<T>);
     // a grid has fewer than 2^32 threads; whole groups of 128 rows, whose scale bytes are neighbours
-    const int64_t per = std::max<int64_t>(1, (1 << 23) / chunks) << (8 - log_tpr);
+    const int64_t per = std::max<int64_t>(1, (1 << 23) / s.chunks) << (8 - s.log_tpr);
     const int64_t most = std::max<int64_t>(kScaled, per / kScaled * kScaled);
     const int64_t rows = a.rows;
     for (int64_t done = 0; done < rows; done += most) {
         a.rows = std::min(most, rows - done);
-        const int64_t blocks = ((a.rows + (256 >> log_tpr) - 1) >> (8 - log_tpr)) * chunks;
-        held_values_kernel<T><<<(unsigned)blocks, 256, 0, st>>>(a, log_tpr, chunks);
+        const int64_t blocks = ((a.rows + (256 >> s.log_tpr) - 1) >> (8 - s.log_tpr)) * s.chunks;
+        held_values_kernel<T><<<(unsigned)blocks, 256, 0, st>>>(a, s);
         a.h.q += a.rows * a.h.ld;
         a.h.scale += a.rows;
         a.out = (T *)a.out + a.rows * a.ldo;
