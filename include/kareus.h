@@ -724,7 +724,7 @@ typedef struct kr_scaled {
  *   square    0, or 1: the 128 rows (columns) of an aligned 128 x 128 square share t, so that both forms
  *             hold the same values; each row still has its own byte
  * Rooms are at most the width of the form rounded up to 128.  KR_EUNSUPPORTED for more than 2^30 rows or
- * columns or 2^23 squares.  No workspace.
+ * columns or 2^22 squares.  No workspace.
  */
 kr_status kr_scaled_hold(int32_t type, int64_t rows, int64_t width, const void *x, int64_t ldx,
                          int32_t square, const kr_scaled *plain, const kr_scaled *crossed,
@@ -781,6 +781,7 @@ size_t kr_scaled_linear_workspace(const kr_linear *l);
  *   dx = dout w       dout held by rows, w by squares (the values of the forward product)
  *   dw = dout^T x     dout and x held by columns, blocks of 128 rows
  * dx, dw   of the type, or NULL: not asked for; without rows dw is 0.  No output overlaps an input.
+ *          (One that is asked for alone may add its sum in another order than both together.)
  * KR_EUNSUPPORTED where one of the calls is (rows > 2^21 among them).
  */
 kr_status kr_scaled_linear_backward(const kr_linear *l, const void *dout, int64_t lddo, void *dx,

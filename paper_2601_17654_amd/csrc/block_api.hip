@@ -2,7 +2,6 @@
 // order.  Declarations and contracts: include/kareus.h.
 #include <algorithm>
 #include <cmath>
-#include <utility>
 
 #include "kr_drop.h"
 #include "kr_gated.h"
@@ -485,30 +484,51 @@ bool scaled_fits(const kr_scaled_product *p) { return product_fits(p->m, p->n, p
 bool hold_fits(int64_t rows, int64_t width)
 {
     return rows <= kHeldMost && width <= kHeldMost &&
-           up(rows, kScaled) / kScaled * (up(width, kScaled) / kScaled) <= kTilesMost;
+           up(rows, kScaled) / kScaled * (up(width, kScaled) / kScaled) <= kHoldTilesMost;
 }
+
+// A product's arguments: its part in the workspace, and operands that are laid out anew.
+struct ScaledLaid {
+    ScaledArgs x;
+    bool few;
+    Laid a, b;
+    ScaledLaid(const kr_scaled_product *p, int32_t type, void *out, int64_t ldo, Carve &c)
+        : x{type, p->m, p->n, p->k, held(&p->a), held(&p->b), out, ldo, nullptr},
+          few(p->m <= kScaledFew),
+          // rows to a multiple of 16 bytes: theirs, where they have that room
+          a(p->a.q, p->a.ld, few ? 0 : p->m, room_of(p->a, p->k), c),
+          b(p->b.q, p->b.ld, few ? 0 : p->n, room_of(p->b, p->k), c)
+    {
+        if (few) return;
+        x.part = c.take((int64_t)scaled_part(type, p->m, p->n, p->k));
+        set(x.a, a);
+        set(x.b, b);
+    }
+    static int64_t room_of(const kr_scaled &h, int64_t k) { return h.room >= padded(k) ? padded(k) : k; }
+    static void set(HeldMatrix &h, const Laid &l)
+    {
+        h.q = (char *)l.op.p;
+        h.ld = l.op.ld;
+        h.bytes = l.op.bytes;
+    }
+    kr_status fill(hipStream_t st) const
+    {
+        if (few) return KR_OK;
+        PadArgs pads{};
+        a.add_to(pads);
+        b.add_to(pads);
+        return said(launch_pad(pads, st));
+    }
+};
 
 kr_status scaled_run(const kr_scaled_product *p, int32_t type, void *out, int64_t ldo, Carve &c,
                      hipStream_t st)
 {
-    ScaledArgs x{type, p->m, p->n, p->k, held(&p->a), held(&p->b), out, ldo, nullptr};
-    if (p->m <= kScaledFew) return out ? said(launch_scaled_few(x, st)) : KR_OK;
-    // rows to a multiple of 16 bytes: theirs, where they have that room
-    const int64_t wide = padded(p->k);
-    const Laid a(p->a.q, p->a.ld, p->m, p->a.room >= wide ? wide : p->k, c);
-    const Laid b(p->b.q, p->b.ld, p->n, p->b.room >= wide ? wide : p->k, c);
-    x.part = c.take((int64_t)scaled_part(type, p->m, p->n, p->k));
+    const ScaledLaid l(p, type, out, ldo, c);
     if (!out) return KR_OK;
-    PadArgs pads{};
-    a.add_to(pads);
-    b.add_to(pads);
-    if (const hipError_t e = launch_pad(pads, st); e != hipSuccess) return said(e);
-    for (const auto &to : {std::make_pair(&x.a, &a), std::make_pair(&x.b, &b)}) {
-        to.first->q = (char *)to.second->op.p;
-        to.first->ld = to.second->op.ld;
-        to.first->bytes = to.second->op.bytes;
-    }
-    return said(launch_scaled(x, st));
+    const kr_status s = l.fill(st);
+    if (s != KR_OK) return s;
+    return said(l.few ? launch_scaled_few(l.x, st) : launch_scaled(l.x, st));
 }
 
 }  // namespace
@@ -599,13 +619,13 @@ kr_scaled held_room(int64_t rows, int64_t width, Carve &c)
     return h;
 }
 
-hipError_t hold_into(int32_t type, int64_t rows, int64_t width, const void *x, int64_t ldx, bool square,
-                     const kr_scaled *plain, const kr_scaled *crossed, hipStream_t st)
+HoldArgs hold_args(int64_t rows, int64_t width, const void *x, int64_t ldx, const kr_scaled *plain,
+                   const kr_scaled *crossed)
 {
     HoldArgs a{rows, width, x, ldx, {}, {}, up(width, kScaled) / kScaled};
     if (plain) a.plain = held(plain);
     if (crossed) a.crossed = held(crossed);
-    return launch_hold(type, square, a, st);
+    return a;
 }
 
 // c.base null: sizes alone.
@@ -613,11 +633,13 @@ kr_status linear_run(const kr_linear *l, void *out, int64_t ldo, Carve &c, hipSt
 {
     const kr_scaled x = held_room(l->rows, l->width, c), w = held_room(l->hidden, l->width, c);
     const kr_scaled_product p{l->rows, l->hidden, l->width, x, w};
-    if (!c.base) return scaled_run(&p, l->type, nullptr, 0, c, st);
-    hipError_t e = hold_into(l->type, l->rows, l->width, l->x, l->ldx, false, &x, nullptr, st);
-    if (e == hipSuccess)
-        e = hold_into(l->type, l->hidden, l->width, l->w, l->ldw, true, &w, nullptr, st);
-    return e == hipSuccess ? scaled_run(&p, l->type, out, ldo, c, st) : said(e);
+    if (c.base) {
+        const hipError_t e = launch_hold_linear(
+            l->type, hold_args(l->rows, l->width, l->x, l->ldx, &x, nullptr),
+            hold_args(l->hidden, l->width, l->w, l->ldw, &w, nullptr), st);
+        if (e != hipSuccess) return said(e);
+    }
+    return scaled_run(&p, l->type, c.base ? out : nullptr, ldo, c, st);
 }
 
 kr_status linear_back_run(const kr_linear *l, const void *dout, int64_t ldd, void *dx, int64_t lddx,
@@ -634,20 +656,22 @@ kr_status linear_back_run(const kr_linear *l, const void *dout, int64_t ldd, voi
         xt = held_room(l->width, l->rows, c);
     }
     const kr_scaled_product px{l->rows, l->width, l->hidden, d, wt}, pw{l->hidden, l->width, l->rows, dt, xt};
-    if (!c.base) {
-        scaled_run(&px, l->type, nullptr, 0, c, st);
-        return scaled_run(&pw, l->type, nullptr, 0, c, st);
+    if (c.base) {
+        const hipError_t e = launch_hold_linear_back(
+            l->type, hold_args(l->rows, l->hidden, dout, ldd, for_x ? &d : nullptr, for_w ? &dt : nullptr),
+            hold_args(l->hidden, l->width, l->w, l->ldw, nullptr, &wt),
+            hold_args(l->rows, l->width, l->x, l->ldx, nullptr, &xt), st);
+        if (e != hipSuccess) return said(e);
     }
-    hipError_t e = hold_into(l->type, l->rows, l->hidden, dout, ldd, false, for_x ? &d : nullptr,
-                             for_w ? &dt : nullptr, st);
-    if (e == hipSuccess && for_x)
-        e = hold_into(l->type, l->hidden, l->width, l->w, l->ldw, true, nullptr, &wt, st);
-    if (e == hipSuccess && for_w)
-        e = hold_into(l->type, l->rows, l->width, l->x, l->ldx, false, nullptr, &xt, st);
-    kr_status s = said(e);
-    if (s == KR_OK && for_x) s = scaled_run(&px, l->type, dx, lddx, c, st);
-    if (s == KR_OK && for_w) s = scaled_run(&pw, l->type, dw, lddw, c, st);
-    return s;
+    if (!for_x || !for_w) {
+        return for_x ? scaled_run(&px, l->type, dx, lddx, c, st) : scaled_run(&pw, l->type, dw, lddw, c, st);
+    }
+    // (held_room's rows need no laying out anew)
+    const ScaledLaid x(&px, l->type, dx, lddx, c), w(&pw, l->type, dw, lddw, c);
+    if (!c.base) return KR_OK;
+    if (!x.few && !w.few) return said(launch_scaled_pair(x.x, w.x, st));
+    const hipError_t e = x.few ? launch_scaled_few(x.x, st) : launch_scaled(x.x, st);
+    return said(e != hipSuccess ? e : w.few ? launch_scaled_few(w.x, st) : launch_scaled(w.x, st));
 }
 
 }  // namespace

@@ -293,13 +293,13 @@ struct MmaArgs {
     float *part;         // splits > 1: [split][plane][m][n] (int32 for bytes)
 };
 
-// The tile of a block.  Blocks go to the 8 XCDs in turn: each XCD takes a run of consecutive
+// The tile of block id.  Blocks go to the 8 XCDs in turn: each XCD takes a run of consecutive
 // tiles, and a run covers 4 tiles of m before it moves on in n, so that the tiles of an XCD
 // share rows of both operands in its L2.
-__device__ inline void tile_of(const MmaArgs &a, int *tm, int *tn, int *split)
+__device__ inline void tile_of(const MmaArgs &a, int id, int *tm, int *tn, int *split)
 {
     const int per = a.tiles_m * a.tiles_n, all = per * a.splits;
-    const int id = (int)blockIdx.x, x = id & 7, q = all >> 3, r = all & 7;
+    const int x = id & 7, q = all >> 3, r = all & 7;
     int t = x * q + min(x, r) + (id >> 3);
     *split = t / per;
     t -= *split * per;
@@ -499,7 +499,7 @@ __global__ __launch_bounds__(WM *WN * 64) void mma_kernel(MmaArgs a, Out out)
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int wm = wave / WN, wn = wave % WN;
     int tm, tn, split;
-    tile_of(a, &tm, &tn, &split);
+    tile_of(a, (int)blockIdx.x, &tm, &tn, &split);
     const int64_t m0 = (int64_t)tm * BM;
     const int64_t n0 = (int64_t)tn * (TWO ? BN / 2 : BN);
 

@@ -71,7 +71,13 @@ struct HoldArgs {
     HeldMatrix plain, crossed;  // q null: not asked for
     int64_t tiles_c;
 };
+constexpr int64_t kHoldTilesMost = 1 << 22;  // a grid has fewer than 2^32 threads, 512 a tile
 hipError_t launch_hold(int dtype, bool square, const HoldArgs &a, hipStream_t st);
+// A linear layer's operands in one launch: x's rows and w's squares (plain);  the gradient's rows and
+// columns, either null, and what their products take: w's squares and x's columns (crossed).
+hipError_t launch_hold_linear(int dtype, const HoldArgs &x, const HoldArgs &w, hipStream_t st);
+hipError_t launch_hold_linear_back(int dtype, const HoldArgs &d, const HoldArgs &w, const HoldArgs &x,
+                                   hipStream_t st);
 
 struct HeldValuesArgs {
     int64_t rows, width;
@@ -96,6 +102,8 @@ struct ScaledArgs {
 size_t scaled_part(int out_type, int64_t m, int64_t n, int64_t k);
 // a, b: 16-byte aligned, rows of a multiple of 16 bytes, zeros past k.
 hipError_t launch_scaled(const ScaledArgs &a, hipStream_t st);
+// Two products of one output type, in one launch where both are cut into tiles of one size.
+hipError_t launch_scaled_pair(const ScaledArgs &a, const ScaledArgs &b, hipStream_t st);
 // Up to 32 rows, any alignment, k bytes of each row; no part.
 hipError_t launch_scaled_few(const ScaledArgs &a, hipStream_t st);
 

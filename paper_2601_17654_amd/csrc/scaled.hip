@@ -109,15 +109,22 @@ __global__ __launch_bounds__(256) void hold_rows_kernel(HoldArgs a)
 // 1500 both forms 12.7 us, now 8.)
 constexpr int kHoldThreads = 512;
 
-template <typename T, bool SQUARE, bool PLAIN, bool CROSSED>
-__global__ __launch_bounds__(kHoldThreads) void hold_kernel(HoldArgs a)
+// What a block shares; of forms that are not asked for, a word.
+template <bool COLUMNS, bool CROSSED>
+struct HoldLds {
+    uint8_t turned[CROSSED ? kScaled * kScaled : 16];
+    uint8_t bytes[2][kScaled], of_column[kScaled];
+    uint32_t tops[kHoldThreads / 64 * (COLUMNS ? kScaled : 1)];
+};
+
+template <typename T, bool SQUARE, bool PLAIN, bool CROSSED, typename Lds>
+__device__ __attribute__((always_inline)) inline void hold_tile(const HoldArgs &a, int64_t block, Lds &lds)
 {
     constexpr int WAVES = kHoldThreads / 64, ROWS = 4;
-    __shared__ uint32_t tops[CROSSED && !SQUARE ? WAVES * kScaled : WAVES];
-    __shared__ __align__(16) uint8_t bytes[2][kScaled], of_column[kScaled];
-    __shared__ __align__(16) uint8_t turned[CROSSED ? kScaled * kScaled : 16];
+    uint32_t *tops = lds.tops;
+    uint8_t(*bytes)[kScaled] = lds.bytes, *of_column = lds.of_column, *turned = lds.turned;
     const int t = threadIdx.x, cg = t % 16, rg = t / 16, wave = t / 64;
-    const int64_t tile_r = blockIdx.x / a.tiles_c, tile_c = blockIdx.x - tile_r * a.tiles_c;
+    const int64_t tile_r = block / a.tiles_c, tile_c = block - tile_r * a.tiles_c;
     const int64_t r0 = tile_r * kScaled + rg * ROWS, c0 = tile_c * kScaled + cg * 8;
 
     Eight<T> x[ROWS];
@@ -234,6 +241,35 @@ __global__ __launch_bounds__(kHoldThreads) void hold_kernel(HoldArgs a)
     }
 }
 
+template <typename T, bool SQUARE, bool PLAIN, bool CROSSED>
+__global__ __launch_bounds__(kHoldThreads) void hold_kernel(HoldArgs a)
+{
+    __shared__ __align__(16) HoldLds<CROSSED && !SQUARE, CROSSED> lds;
+    hold_tile<T, SQUARE, PLAIN, CROSSED>(a, blockIdx.x, lds);
+}
+
+// What a linear layer holds, in one launch: forward x by rows and the weight by squares; backward
+// the output's gradient by rows and by columns, the weight's transpose by squares and x by columns.
+struct HoldMany {
+    HoldArgs a[3];
+    uint32_t first[2];  // blocks of the first, of the first two
+};
+
+template <typename T, bool BACK>
+__global__ __launch_bounds__(kHoldThreads) void hold_many_kernel(HoldMany m)
+{
+    __shared__ __align__(16) HoldLds<BACK, BACK> lds;
+    const uint32_t b = blockIdx.x;
+    if (!BACK) {
+        if (b < m.first[0]) hold_tile<T, false, true, false>(m.a[0], b, lds);
+        else hold_tile<T, true, true, false>(m.a[1], b - m.first[0], lds);
+    } else {
+        if (b < m.first[0]) hold_tile<T, false, true, true>(m.a[0], b, lds);
+        else if (b < m.first[1]) hold_tile<T, true, false, true>(m.a[1], b - m.first[0], lds);
+        else hold_tile<T, false, false, true>(m.a[2], b - m.first[1], lds);
+    }
+}
+
 template <typename T>
 hipError_t hold_rows(HoldArgs a, hipStream_t st)
 {
@@ -253,10 +289,12 @@ hipError_t hold_rows(HoldArgs a, hipStream_t st)
     return hipGetLastError();
 }
 
+int64_t hold_tiles(const HoldArgs &a) { return (a.rows + kScaled - 1) / kScaled * a.tiles_c; }
+
 template <typename T, bool SQUARE>
 hipError_t hold(const HoldArgs &a, hipStream_t st)
 {
-    const unsigned blocks = (unsigned)((a.rows + kScaled - 1) / kScaled * a.tiles_c);
+    const unsigned blocks = (unsigned)hold_tiles(a);
     if (a.plain.q && a.crossed.q) hold_kernel<T, SQUARE, true, true><<<blocks, kHoldThreads, 0, st>>>(a);
     else if (a.crossed.q) hold_kernel<T, SQUARE, false, true><<<blocks, kHoldThreads, 0, st>>>(a);
     else if constexpr (SQUARE) hold_kernel<T, true, true, false><<<blocks, kHoldThreads, 0, st>>>(a);
@@ -341,6 +379,36 @@ hipError_t launch_hold(int dtype, bool square, const HoldArgs &a, hipStream_t st
     if (dtype == KR_F32) return square ? hold<float, true>(a, st) : hold<float, false>(a, st);
     if (dtype == KR_F16) return square ? hold<f16, true>(a, st) : hold<f16, false>(a, st);
     return square ? hold<bf16, true>(a, st) : hold<bf16, false>(a, st);
+}
+
+hipError_t launch_hold_linear(int dtype, const HoldArgs &x, const HoldArgs &w, hipStream_t st)
+{
+    const int64_t n0 = hold_tiles(x), n = n0 + hold_tiles(w);
+    if (n > kHoldTilesMost) {
+        const hipError_t e = launch_hold(dtype, false, x, st);
+        return e == hipSuccess ? launch_hold(dtype, true, w, st) : e;
+    }
+    const HoldMany m{{x, w, {}}, {(uint32_t)n0, 0}};
+    if (dtype == KR_F32) hold_many_kernel<float, false><<<(unsigned)n, kHoldThreads, 0, st>>>(m);
+    else if (dtype == KR_F16) hold_many_kernel<f16, false><<<(unsigned)n, kHoldThreads, 0, st>>>(m);
+    else hold_many_kernel<bf16, false><<<(unsigned)n, kHoldThreads, 0, st>>>(m);
+    return hipGetLastError();
+}
+
+hipError_t launch_hold_linear_back(int dtype, const HoldArgs &d, const HoldArgs &w, const HoldArgs &x,
+                                   hipStream_t st)
+{
+    const int64_t n0 = hold_tiles(d), n1 = n0 + hold_tiles(w), n = n1 + hold_tiles(x);
+    if (!d.plain.q || !d.crossed.q || n > kHoldTilesMost) {  // one gradient alone, or more than a grid
+        hipError_t e = launch_hold(dtype, false, d, st);
+        if (e == hipSuccess && d.plain.q) e = launch_hold(dtype, true, w, st);
+        return e == hipSuccess && d.crossed.q ? launch_hold(dtype, false, x, st) : e;
+    }
+    const HoldMany m{{d, w, x}, {(uint32_t)n0, (uint32_t)n1}};
+    if (dtype == KR_F32) hold_many_kernel<float, true><<<(unsigned)n, kHoldThreads, 0, st>>>(m);
+    else if (dtype == KR_F16) hold_many_kernel<f16, true><<<(unsigned)n, kHoldThreads, 0, st>>>(m);
+    else hold_many_kernel<bf16, true><<<(unsigned)n, kHoldThreads, 0, st>>>(m);
+    return hipGetLastError();
 }
 
 hipError_t launch_held_values(int dtype, const HeldValuesArgs &a, hipStream_t st)

@@ -9,6 +9,8 @@
 // neighbours differ by powers of two up to 2^10); a 16-bit output's rounding alone is up to 4.9e-4 or
 // 3.9e-3.  Outputs of 32 bits take the values to bfloat16, which holds them and their scales exactly,
 // and the instruction of that type, whose sums are off by 1e-7 (8192^3: 944 us, against 381).
+#include <algorithm>
+
 #include "kr_few.h"
 #include "kr_scaled.h"
 
@@ -148,6 +150,14 @@ struct TileArgs {
     const uint8_t *scale[2];  // of a, of b
     int64_t lds[2];           // bytes from one block's to the next
     int64_t rows[2];          // of a block that may be read
+};
+
+// One product, or two whose blocks share a launch: those from `first` on are the second's.
+template <typename Out>
+struct Two {
+    TileArgs a[2];
+    Out out[2];
+    uint32_t first;
 };
 
 // A block's copies to LDS: the operands' tiles as in mma_kernel, 16 bytes a lane, and the step's scale
@@ -300,8 +310,12 @@ struct When<16> {
 // In a step's first quarter come the reads of its second b half and of a1, from `next` on those of the next
 // step's a0 and of its first b half.
 template <int BM, int BN, typename Out>
-__global__ __launch_bounds__(256) void scaled_tile_kernel(TileArgs a, Out out)
+__global__ __launch_bounds__(256) void scaled_tile_kernel(Two<Out> two)
 {
+    const bool second = blockIdx.x >= two.first;
+    const TileArgs &a = two.a[second];
+    const Out &out = two.out[second];
+    const int block = (int)(second ? blockIdx.x - two.first : blockIdx.x);
     constexpr int WM = 2, WN = 2, RM = BM / WM, RN = BN / WN, TM = RM / 16, TN = RN / 16;
     constexpr int BLOCK = TM * TN, QUARTER = BLOCK / 4, HM = TM / 2, HN = TN / 2;
     typedef When<BLOCK> W;
@@ -316,7 +330,7 @@ __global__ __launch_bounds__(256) void scaled_tile_kernel(TileArgs a, Out out)
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int wm = wave / WN, wn = wave % WN;
     int tm, tn, split;
-    tile_of(a.p, &tm, &tn, &split);
+    tile_of(a.p, block, &tm, &tn, &split);
     const int64_t m0 = (int64_t)tm * BM, n0 = (int64_t)tn * BN;
     const int begin = split * a.p.per_split, end = min(begin + a.p.per_split, a.p.steps);
 
@@ -404,8 +418,13 @@ __global__ __launch_bounds__(256) void scaled_tile_kernel(TileArgs a, Out out)
 // The same for outputs of 32 bits, in tiles of 128 x BN: a step's values go to bfloat16 on their way to the
 // instructions, which the compiler places.  A lane's four sums are neighbours in a row and leave as they are.
 template <int BN>
-__global__ __launch_bounds__(256) void scaled_wide_kernel(TileArgs a, float *out, int64_t ldo)
+__global__ __launch_bounds__(256) void scaled_wide_kernel(Two<PutAs<float>> two)
 {
+    const bool second = blockIdx.x >= two.first;
+    const TileArgs &a = two.a[second];
+    float *out = two.out[second].out;
+    int64_t ldo = two.out[second].ldo;
+    const int block = (int)(second ? blockIdx.x - two.first : blockIdx.x);
     constexpr int BM = 128, WN = 2, TM = 4, TN = BN / WN / 16;
     typedef Copies<BM, BN, 4> C;
     __shared__ __align__(1024) typename C::Lds lds;
@@ -413,7 +432,7 @@ __global__ __launch_bounds__(256) void scaled_wide_kernel(TileArgs a, float *out
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int wm = wave / WN, wn = wave % WN;
     int tm, tn, split;
-    tile_of(a.p, &tm, &tn, &split);
+    tile_of(a.p, block, &tm, &tn, &split);
     const int64_t m0 = (int64_t)tm * BM, n0 = (int64_t)tn * BN;
     const int begin = split * a.p.per_split, end = min(begin + a.p.per_split, a.p.steps);
     C c;
@@ -507,8 +526,7 @@ Plan plan_of(int out_type, int64_t m, int64_t n, int steps)
     return best;
 }
 
-template <typename T>
-hipError_t tiles(const ScaledArgs &a, hipStream_t st)
+TileArgs tile_args(const ScaledArgs &a, const MmaPlan &p)
 {
     TileArgs x{};
     x.p.a[0] = Operand{a.a.q, a.a.ld, a.m, a.a.bytes};
@@ -518,8 +536,6 @@ hipError_t tiles(const ScaledArgs &a, hipStream_t st)
     x.p.k_bytes = a.a.bytes;
     x.p.steps = (int)((a.k + kScaled - 1) / kScaled);
     x.p.pairs = 1;
-    const Plan plan = plan_of(a.out_type, a.m, a.n, x.p.steps);
-    const MmaPlan &p = plan.p;
     x.p.tiles_m = p.tiles_m;
     x.p.tiles_n = p.tiles_n;
     x.p.splits = p.splits;
@@ -531,20 +547,106 @@ hipError_t tiles(const ScaledArgs &a, hipStream_t st)
         x.lds[i] = h.lds;
         x.rows[i] = ((i ? a.n : a.m) + kScaled - 1) / kScaled * kScaled;
     }
-    const PutAs<T> out{(T *)a.out, a.ldo, (int)a.n};
-    const unsigned blocks = (unsigned)(p.tiles_m * p.tiles_n * p.splits);
+    return x;
+}
+
+// b: null, or a second product whose plan has a's tile size.
+template <typename T>
+hipError_t tiles(const ScaledArgs &a, const Plan &pa, const ScaledArgs *b, const Plan *pb, hipStream_t st)
+{
+    typedef PutAs<T> Out;
+    Two<Out> two{{tile_args(a, pa.p), {}}, {{(T *)a.out, a.ldo, (int)a.n}, {}}, 0};
+    two.first = (uint32_t)(pa.p.tiles_m * pa.p.tiles_n * pa.p.splits);
+    unsigned blocks = two.first;
+    if (b) {
+        two.a[1] = tile_args(*b, pb->p);
+        two.out[1] = Out{(T *)b->out, b->ldo, (int)b->n};
+        blocks += (unsigned)(pb->p.tiles_m * pb->p.tiles_n * pb->p.splits);
+    }
     if constexpr (sizeof(T) == 4)
-        plan.narrow ? scaled_wide_kernel<64><<<blocks, 256, 0, st>>>(x, out.out, out.ldo)
-                    : scaled_wide_kernel<128><<<blocks, 256, 0, st>>>(x, out.out, out.ldo);
-    else if (p.large)
-        scaled_tile_kernel<256, 256><<<blocks, 256, 0, st>>>(x, out);
+        pa.narrow ? scaled_wide_kernel<64><<<blocks, 256, 0, st>>>(two)
+                  : scaled_wide_kernel<128><<<blocks, 256, 0, st>>>(two);
+    else if (pa.p.large)
+        scaled_tile_kernel<256, 256><<<blocks, 256, 0, st>>>(two);
     else
-        scaled_tile_kernel<128, 128><<<blocks, 256, 0, st>>>(x, out);
-    if (p.splits > 1) {
-        const int64_t threads = a.m * ((a.n + 7) / 8);
-        mma_join_kernel<E4m3><<<(unsigned)((threads + 255) / 256), 256, 0, st>>>(x.p, out);
+        scaled_tile_kernel<128, 128><<<blocks, 256, 0, st>>>(two);
+    for (int i = 0; i < (b ? 2 : 1); ++i) {
+        const MmaArgs &p = two.a[i].p;
+        if (p.splits == 1) continue;
+        const int64_t threads = (int64_t)p.m * ((p.n + 7) / 8);
+        mma_join_kernel<E4m3><<<(unsigned)((threads + 255) / 256), 256, 0, st>>>(p, two.out[i]);
     }
     return hipGetLastError();
+}
+
+template <typename T>
+hipError_t one(const ScaledArgs &a, hipStream_t st)
+{
+    return tiles<T>(a, plan_of(a.out_type, a.m, a.n, (int)((a.k + kScaled - 1) / kScaled)), nullptr, nullptr, st);
+}
+
+// What one tile takes of the chip's 256 CUs, and by itself, in microseconds (of mma_plan and plan_of).
+struct TileCost {
+    double share, alone;
+};
+TileCost cost_of(const Plan &x, bool f32)
+{
+    const int per = x.p.per_split;
+    if (f32) return {per * (x.narrow ? 0.8 : 1.05), per * (x.narrow ? 0.8 : 1.05) + 5};
+    if (x.p.large) return {1.3 * per + 9, 1.3 * per + 9};
+    return {0.47 * per + 2, 0.94 * per + 4};  // two a CU
+}
+int64_t blocks_of(const Plan &x) { return (int64_t)x.p.tiles_m * x.p.tiles_n * x.p.splits; }
+double join_of(const Plan &x) { return x.p.splits > 1 ? 4 + 2 * (double)x.p.part_bytes / 4e6 : 0; }
+
+// Both in one launch, whose tiles fill the chip together; alone, by rounds of 256.
+double cost_together(const Plan &a, const Plan &b, bool f32)
+{
+    const TileCost x = cost_of(a, f32), y = cost_of(b, f32);
+    const double all = (blocks_of(a) * x.share + blocks_of(b) * y.share) / 256;
+    const double longest = std::max(x.alone, y.alone);
+    return std::max(all + 0.5 * std::min(x.alone, y.alone), longest) + join_of(a) + join_of(b);
+}
+double cost_alone(const Plan &a, bool f32)
+{
+    return (blocks_of(a) + 255) / 256 * cost_of(a, f32).share + (f32 ? 5 : 0) + join_of(a);
+}
+
+// Tiles of one size, whole sums.
+Plan plan_whole(int64_t m, int64_t n, int steps, bool f32, bool other)
+{
+    const int bm = !f32 && other ? 256 : 128, bn = f32 ? (other ? 64 : 128) : bm;
+    return {{!f32 && other, (int)((m + bm - 1) / bm), (int)((n + bn - 1) / bn), 1, steps, 0}, f32 && other};
+}
+
+// Two products (a linear layer's gradients), whose sums differ in length: one launch where that is
+// cheaper by the estimate, with their own plans or with whole sums in tiles of one size.  4917 x 5056 x 832,
+// 400 large tiles of 7 steps and 273 small ones of 40: 86 us alone one after the other, 62 together.
+template <typename T>
+hipError_t pair(const ScaledArgs &a, const ScaledArgs &b, hipStream_t st)
+{
+    constexpr bool F32 = sizeof(T) == 4;
+    const int sa = (int)((a.k + kScaled - 1) / kScaled), sb = (int)((b.k + kScaled - 1) / kScaled);
+    const Plan pa = plan_of(a.out_type, a.m, a.n, sa), pb = plan_of(b.out_type, b.m, b.n, sb);
+    Plan best[2] = {pa, pb};
+    bool together = pa.p.large == pb.p.large && pa.narrow == pb.narrow;
+    double least = together ? cost_together(pa, pb, F32) : cost_alone(pa, F32) + cost_alone(pb, F32) + 3;
+    for (const bool other : {false, true}) {
+        const Plan x = plan_whole(a.m, a.n, sa, F32, other), y = plan_whole(b.m, b.n, sb, F32, other);
+        const double cost = cost_together(x, y, F32);
+        if (cost >= least || blocks_of(x) + blocks_of(y) > 1 << 23) continue;
+        least = cost;
+        best[0] = x;
+        best[1] = y;
+        together = true;
+    }
+    if (!together || blocks_of(best[0]) + blocks_of(best[1]) > 1 << 23) {
+        const hipError_t e = tiles<T>(a, best[0], nullptr, nullptr, st);
+        return e == hipSuccess ? tiles<T>(b, best[1], nullptr, nullptr, st) : e;
+    }
+    // the longer sums first, so that the shorter ones fill the end
+    return best[0].p.per_split >= best[1].p.per_split ? tiles<T>(a, best[0], &b, &best[1], st)
+                                                      : tiles<T>(b, best[1], &a, &best[0], st);
 }
 
 template <typename T>
@@ -567,9 +669,16 @@ size_t scaled_part(int out_type, int64_t m, int64_t n, int64_t k)
 
 hipError_t launch_scaled(const ScaledArgs &a, hipStream_t st)
 {
-    if (a.out_type == KR_F32) return tiles<float>(a, st);
-    if (a.out_type == KR_F16) return tiles<f16>(a, st);
-    return tiles<bf16>(a, st);
+    if (a.out_type == KR_F32) return one<float>(a, st);
+    if (a.out_type == KR_F16) return one<f16>(a, st);
+    return one<bf16>(a, st);
+}
+
+hipError_t launch_scaled_pair(const ScaledArgs &a, const ScaledArgs &b, hipStream_t st)
+{
+    if (a.out_type == KR_F32) return pair<float>(a, b, st);
+    if (a.out_type == KR_F16) return pair<f16>(a, b, st);
+    return pair<bf16>(a, b, st);
 }
 
 hipError_t launch_scaled_few(const ScaledArgs &a, hipStream_t st)
