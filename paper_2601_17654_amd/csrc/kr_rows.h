@@ -62,7 +62,7 @@ inline Dealt dealt(int64_t groups)
 }
 
 // load_row and store_row for rows of a whole number of vectors (WHOLE), which need no shifts and no
-// element by element end: the layer norm's gradient below takes 30 registers less with them.
+// element by element end.
 template <bool WHOLE, typename T>
 __device__ inline Pack<T, kVec<T>> load_part(const T *row, int c, int width)
 {

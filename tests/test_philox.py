@@ -1,5 +1,5 @@
-"""The tests' generator against the known answers that are published with it (Random123's file of
-them), and the share of values that it keeps."""
+"""The tests' generator against the known answers that are published for it, and the share of values that
+it keeps."""
 
 import pytest
 
