@@ -757,12 +757,10 @@ def launch_timing_frontier(kind1, kind2, ops, p_static: float, kmax: int, out_ca
 # streams may overlap.  A single token's call takes about as long here as on the device, so
 # these functions hand over plain integers and ask for each thing once.
 #
-# While torch records a graph and an input requires a gradient, add_rms_norm and gated_projection
-# are nodes of it, whose backward passes are add_rms_norm_backward and
-# gated_projection_backward.  The forms in 8-bit integers have no gradient and refuse such
+# While torch records a graph and an input requires a gradient, add_rms_norm, add_layer_norm, dropout,
+# gated_projection and scaled_linear are nodes of it, whose backward passes are the functions
+# named so (dropout's is dropout).  The other forms in 8 bits have no gradient and refuse such
 # inputs.  The backward functions themselves return plain tensors: they are not differentiated again.
-
-# (scaled_hold, scaled_values and scaled_matmul have none either; scaled_linear has.)
 
 _TYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (

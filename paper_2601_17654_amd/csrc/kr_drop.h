@@ -13,8 +13,9 @@ namespace kr {
 // Philox4x32-10 (Salmon et al., "Parallel random numbers: as easy as 1, 2, 3", 2011) at the counter
 // (c / 8, row, offset) under the key `seed`, are `cut` or more; kept values are taken times `factor`.
 // Sixteen bits a value: the ten rounds (20 products of 32 x 32 bits, each at a quarter of the
-// rate, and 40 exclusive ors) cost eight values 480 cycles a wave.  With 32 bits a value they would
-// cost twice that and 16-bit tensors would wait for them instead of for memory.
+// rate, and 40 exclusive ors) cost eight values a lane some 480 cycles a wave: 67 million values 26 us of the
+// chip's vector units, a quarter of what their memory takes in a norm.  With 32 bits a value it would be half,
+// and dropout alone of a 16-bit tensor would wait for them.
 struct Drop {
     uint64_t seed, offset;
     const uint64_t *seed_at;  // read when the kernel runs, in place of seed; or null

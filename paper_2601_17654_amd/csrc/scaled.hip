@@ -108,8 +108,8 @@ __global__ __launch_bounds__(256) void hold_rows_kernel(HoldArgs a)
 // rows from 4 rg on.  Both forms come of one read: the plain one's bytes go straight out, the crossed
 // one's through LDS, where 4-byte chunk rg of column c lies at place rg ^ 2 (c / 8).  Values stay as they
 // were loaded and are converted twice, for the largest and to be held: half the registers.  (With eight
-// rows a thread a block alone on its CU, which small matrices have, waited for its instructions: 1000 x
-// 1500 both forms 12.7 us, now 8.)
+// rows a thread and 256 threads a block alone on its CU, which small matrices have, waited for its
+// instructions: 1000 x 1500, both forms, 12.7 us instead of 8.)
 constexpr int kHoldThreads = 512;
 
 // What a block shares; of forms that are not asked for, a word.

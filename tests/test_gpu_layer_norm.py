@@ -312,3 +312,54 @@ def test_captured(kr):
         want = step()
         assert all(torch.equal(p, q) for p, q in zip(got, want)), k
         torch.cuda.synchronize()
+
+
+def test_past_32_bit_offsets(kr):
+    """More than 2^32 elements, rows of a repeated pattern: forward and backward as from the pattern alone, but
+    for the sums over rows, which are the pattern's many times."""
+    part, w, b = make(64, 2100, torch.bfloat16, 12)
+    n = 64 * 33000
+    x, g = (v.cuda().repeat(n // 64, 1) for v in part[:2])
+    w, b = w.cuda(), b.cuda()
+    small = kr.add_layer_norm(x[:64], w, b)
+    got = kr.add_layer_norm(x, w, b)
+    for row0 in (0, n // 2 - 32, n - 64):
+        row0 = row0 // 64 * 64
+        assert torch.equal(got.out[row0:row0 + 64], small.out)
+        assert torch.equal(got.rstd[row0:row0 + 64], small.rstd)
+    del got.out
+    few = kr.add_layer_norm_backward(g[:64], x[:64], w, small.mean, small.rstd)
+    many = kr.add_layer_norm_backward(g, x, w, got.mean, got.rstd)
+    for row0 in (0, n // 2 // 64 * 64, n - 64):
+        assert torch.equal(many[1][row0:row0 + 64], few[1])
+    # A sum of n terms in 32 bits, each added to what there is, is off by at most n 2^-24 of the terms' sizes
+    # together (and by n^2 2^-48: the 1.01).  Here a block, one row at a time at this width, adds
+    # rows / blocks of them, its share goes into one of 32 runs of blocks / 32, and these are added; h and
+    # the product are 4 roundings.  The few rows' sums are off by WORK.
+    from paper_2601_17654_amd.binding import _lib, _TYPES
+
+    blocks = _lib.kr_add_layer_norm_backward_workspace(_TYPES[torch.bfloat16], n, 2100) // (8 * 2100)
+    adds = -(-n // blocks) + -(-blocks // 32) + 32 + 4
+    gd = g[:64].double()
+    h = (x[:64].double() - small.mean.double()[:, None]) * small.rstd.double()[:, None]
+    for k, size in ((2, (gd * h).abs().sum(0)), (3, gd.abs().sum(0))):
+        off = (many[k].double() - few[k].double() * (n // 64)).abs()
+        assert (off <= (adds * 2.0 ** -24 + WORK) * 1.01 * size * (n // 64)).all()
+
+
+def test_past_32_bit_offsets_every_row(kr):
+    """The same size with whole numbers of at most 2 for h, dout and weight: sums over rows are whole numbers below
+    2^24, exact in any order, so that a row left out or taken twice shows."""
+    gen = torch.Generator().manual_seed(13)
+    n = 64 * 33000
+    s, g = (torch.randint(-2, 3, (64, 2100), generator=gen).to(torch.bfloat16) for _ in range(2))
+    assert ((s * g).double().abs().sum(0) * (n // 64) < 2 ** 24).all()
+    want = [(s.double() * g.double()).sum(0) * (n // 64), g.double().sum(0) * (n // 64)]
+    s, g = (v.cuda().repeat(n // 64, 1) for v in (s, g))
+    # the last row alone, past 2^32 elements, differs
+    want[0] += (2 - s[-1].double().cpu()) * g[-1].double().cpu()
+    s[-1] = 2
+    stats = torch.zeros(n, device="cuda"), torch.ones(n, device="cuda")
+    w = torch.ones(2100, dtype=torch.bfloat16, device="cuda")
+    _, _, dw, db = kr.add_layer_norm_backward(g, s, w, *stats)
+    assert torch.equal(dw.double().cpu(), want[0]) and torch.equal(db.double().cpu(), want[1])

@@ -97,6 +97,62 @@ def test_step_against_the_formulas(kr):
         assert float((got - v).norm() / v.norm()) < 1e-3, k
 
 
+def test_captured_step(kr):
+    """Forward and backward through torch's graph in one captured graph, replayed with new inputs and seeds,
+    beside eager steps on another stream."""
+    t = {k: v.detach() for k, v in leaves(200, 264, torch.bfloat16).items()}
+    d = normal(3, 50, 200, seed=7, dtype=torch.bfloat16).cuda()
+    seed = torch.zeros(1, dtype=torch.int64, device="cuda")
+
+    def step(s):
+        own = {k: v.clone().requires_grad_() for k, v in t.items()}
+        y = block(kr, own, 0.2, s)
+        return (y.detach(), *torch.autograd.grad(y, list(own.values()), d))
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step(seed)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step(seed)
+    for k in range(4):
+        seed.fill_(5 + k)
+        t["x"].copy_(normal(3, 50, 200, seed=30 + k, dtype=torch.bfloat16))
+        t["up"].mul_(0.9)
+        side.wait_stream(torch.cuda.current_stream())
+        graph.replay()
+        with torch.cuda.stream(side):
+            want = step(5 + k)
+        torch.cuda.current_stream().wait_stream(side)
+        assert all(torch.equal(a, b) for a, b in zip(got, want)), k
+        torch.cuda.synchronize()
+
+
+def test_two_streams_at_once(kr):
+    """The same calls on two streams, interleaved: neither touches what the other uses."""
+    t = {k: v.detach() for k, v in leaves(520, 1032, torch.bfloat16, (4, 150)).items()}
+    d = normal(4, 150, 520, seed=7, dtype=torch.bfloat16).cuda()
+
+    def step():
+        own = {k: v.clone().requires_grad_() for k, v in t.items()}
+        y = block(kr, own, 0.2, 3)
+        return (y.detach(), *torch.autograd.grad(y, list(own.values()), d))
+
+    want = step()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    got = []
+    for s in streams:
+        s.wait_stream(torch.cuda.current_stream())
+    for k in range(6):
+        with torch.cuda.stream(streams[k % 2]):
+            got.append(step())
+    torch.cuda.synchronize()
+    for g in got:
+        assert all(torch.equal(a, b) for a, b in zip(g, want))
+
+
 def test_linear_to_rows_apart(kr):
     """The C calls to rows apart, each gradient alone and both: gaps and rows behind stay; without rows the
     weight's gradient is zeros."""

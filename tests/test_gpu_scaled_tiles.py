@@ -41,6 +41,30 @@ def test_whole_numbers(kr, shape, dtype):
     assert torch.equal(got, want)
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("rows,width,hidden", [
+    (4917, 5056, 832), (2048, 2304, 4352), (1000, 2000, 1500), (16, 4100, 600), (17, 300, 5000), (100, 130, 16000),
+    (9000, 140, 150), (300, 6000, 700), (1, 512, 640)])
+def test_linear_gradients(kr, rows, width, hidden, dtype):
+    """Both gradients' products, alone and in one launch, in tiles of either size, whole and split sums: whole
+    numbers to 4 are held as they are, their sums (16 * 16000 < 2^18) are exact in 32 bits, a block's products
+    within 2^4 of each other."""
+    g = torch.Generator().manual_seed(rows)
+    x, w, d = (torch.randint(-4, 5, s, generator=g).to(dtype).cuda()
+               for s in ((rows, width), (hidden, width), (rows, hidden)))
+    size = 0.0625 if dtype == torch.float16 else 1.0  # sums of float16 stay below 65,504
+    y = kr.scaled_linear(x, w * size)
+    assert torch.equal(y, (x.double() @ w.double().t() * size).to(dtype))
+    want = ((d.double() @ w.double() * size).to(dtype), (d.double().t() @ x.double() * size).to(dtype))
+    both = kr.scaled_linear_backward(d * size, x, w)
+    one, none = kr.scaled_linear_backward(d * size, x, w, need=(True, False))
+    assert none is None
+    none, two = kr.scaled_linear_backward(d * size, x, w, need=(False, True))
+    assert none is None
+    for a, b in zip((*both, one, two), (*want, *want)):
+        assert torch.equal(a, b)
+
+
 def test_same_bits_again(kr):
     """Twice, and on another stream at the same time: the same bits (no order changes)."""
     g = torch.Generator().manual_seed(3)
