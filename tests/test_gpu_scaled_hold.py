@@ -149,3 +149,30 @@ def test_large(kr):
     back = kr.scaled_values(both.plain, torch.bfloat16)
     assert torch.equal(back[rows // 128 * 128 - 128:rows // 128 * 128],
                        kr.scaled_values(want.plain, torch.bfloat16))
+
+
+@pytest.mark.parametrize("square", [False, True])
+def test_past_32_bit_offsets(kr, square):
+    """More than 2^32 values, one pattern of 128 rows over and over, strided: each form is the pattern's over
+    and over, and so are the values that it holds."""
+    width, n = 8200, 4097
+    part = make(128, width, torch.bfloat16, 6).cuda()
+    x = torch.empty(n * 128, width + 3, dtype=torch.bfloat16, device="cuda")[:, 1:-2]
+    x.copy_(part.repeat(n, 1))
+    one = kr.scaled_hold(part, square, crossed=True)
+    many = kr.scaled_hold(x, square, crossed=True)
+    del x
+    for k in range(0, n, 241):
+        rows = slice(k * 128, k * 128 + 128)
+        assert torch.equal(many.plain.q[rows].view(torch.uint8), one.plain.q.view(torch.uint8)), k
+        assert torch.equal(many.crossed.q[:, rows].view(torch.uint8), one.crossed.q.view(torch.uint8)), k
+        assert torch.equal(many.plain.scale[:, rows], one.plain.scale[:, :128]), k
+        assert torch.equal(many.crossed.scale[k], one.crossed.scale[0]), k
+    rows = slice((n - 1) * 128, n * 128)
+    assert torch.equal(many.plain.q[rows].view(torch.uint8), one.plain.q.view(torch.uint8))
+    assert torch.equal(many.crossed.q[:, rows].view(torch.uint8), one.crossed.q.view(torch.uint8))
+    assert torch.equal(many.crossed.scale[n - 1], one.crossed.scale[0])
+    small = kr.scaled_values(one.plain, torch.bfloat16)
+    back = kr.scaled_values(many.plain, torch.bfloat16)
+    for k in (0, n // 2, n - 1):
+        assert torch.equal(back[k * 128:k * 128 + 128], small), k
