@@ -730,7 +730,10 @@ kr_status kr_scaled_hold(int32_t type, int64_t rows, int64_t width, const void *
                          int32_t square, const kr_scaled *plain, const kr_scaled *crossed,
                          void *stream);
 
-/* kr_scaled_values -- the values held, rounded to the type: out [rows][width]. */
+/*
+ * kr_scaled_values -- the values held, rounded to the type: out [rows][width].  KR_EUNSUPPORTED for more
+ * than 2^30 rows or columns.  No workspace.
+ */
 kr_status kr_scaled_values(int32_t type, int64_t rows, int64_t width, const kr_scaled *h, void *out,
                            int64_t ldo, void *stream);
 

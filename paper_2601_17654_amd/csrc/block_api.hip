@@ -558,7 +558,7 @@ extern "C" kr_status kr_scaled_values(int32_t type, int64_t rows, int64_t width,
     if (rows > kHeldMost || width > kHeldMost) return KR_EUNSUPPORTED;
     if (rows == 0) return KR_OK;
     if (!matrix_ok(out, ldo, width, size_of(type))) return KR_EINVAL;
-    const HeldValuesArgs a{rows, width, held(h), out, ldo};
+    const HeldValuesArgs a{rows, width, held(h), out, ldo, 0};
     return said(launch_held_values(type, a, (hipStream_t)stream));
 }
 

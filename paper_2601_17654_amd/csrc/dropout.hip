@@ -55,12 +55,10 @@ template <typename T>
 hipError_t typed(DropoutArgs a, hipStream_t st)
 {
     const Dealt s = dealt((a.width + kDropGroup - 1) / kDropGroup);
-    // a grid has fewer than 2^32 threads
-    const int64_t most = std::max<int64_t>(1, (1 << 23) / s.chunks) << (8 - s.log_tpr);
-    const int64_t rows = a.rows;
+    const int64_t most = dealt_rows(s), rows = a.rows;
     for (int64_t done = 0; done < rows; done += most) {
         a.rows = std::min(most, rows - done);
-        const unsigned blocks = (unsigned)(((a.rows + (256 >> s.log_tpr) - 1) >> (8 - s.log_tpr)) * s.chunks);
+        const unsigned blocks = (unsigned)dealt_blocks(s, a.rows);
         if (a.res && a.drop.cut) dropout_kernel<T, true, true><<<blocks, 256, 0, st>>>(a, s);
         else if (a.res) dropout_kernel<T, true, false><<<blocks, 256, 0, st>>>(a, s);
         else if (a.drop.cut) dropout_kernel<T, false, true><<<blocks, 256, 0, st>>>(a, s);

@@ -5,6 +5,7 @@
 #include <type_traits>
 
 #include "kr_block.h"
+#include "kr_dealt.h"
 
 namespace kr {
 
@@ -43,22 +44,6 @@ inline bool with_shape(Shape s, F f)
     KR_SHAPE(1024, 16);
 #undef KR_SHAPE
     return false;
-}
-
-// How a row's groups of neighbours, one a thread, are dealt to blocks of 256 threads: 2^log_tpr threads
-// a row, the rows side by side, or `chunks` blocks to a row; of one to four waves those that leave the fewest
-// threads without a group (258 groups: 64 threads five times, not 256 twice).
-struct Dealt {
-    uint32_t log_tpr, groups, chunks;
-};
-inline Dealt dealt(int64_t groups)
-{
-    uint32_t log = 0;
-    while (log < 8 && ((int64_t)1 << log) < groups) ++log;
-    auto chunks = [&](uint32_t l) { return (groups + (1 << l) - 1) >> l; };
-    for (uint32_t l = log; l-- > 6;)
-        if (chunks(l) << l < chunks(log) << log) log = l;
-    return {log, (uint32_t)groups, (uint32_t)chunks(log)};
 }
 
 // load_row and store_row for rows of a whole number of vectors (WHOLE), which need no shifts and no

@@ -81,9 +81,10 @@ hipError_t launch_hold_linear_back(int dtype, const HoldArgs &d, const HoldArgs 
 
 struct HeldValuesArgs {
     int64_t rows, width;
-    HeldMatrix h;
+    HeldMatrix h;  // q of the launch's first row, the scale bytes of them all
     void *out;
     int64_t ldo;
+    int64_t row0;  // of the first row, among the scale bytes
 };
 hipError_t launch_held_values(int dtype, const HeldValuesArgs &a, hipStream_t st);
 

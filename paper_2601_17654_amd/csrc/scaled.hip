@@ -330,7 +330,7 @@ __global__ __launch_bounds__(256) void held_values_kernel(HeldValuesArgs a, Deal
         for (int e = 0; e < N; ++e)
             if (c + e < a.width) w.v[e / 4] |= (int)(uint8_t)q[e] << (e % 4 * 8);
     }
-    const uint32_t byte = a.h.scale[c / kScaled * a.h.lds + scale_place(row)];
+    const uint32_t byte = a.h.scale[c / kScaled * a.h.lds + scale_place(a.row0 + row)];
     float f[N];
 #pragma unroll
     for (int i = 0; i < N / 4; ++i) {
@@ -348,19 +348,15 @@ template <typename T>
 hipError_t values(HeldValuesArgs a, hipStream_t st)
 {
     const Dealt s = dealt((a.width + kBack<T> - 1) / kBack<T>);
-    // a grid has fewer than 2^32 threads; whole groups of 128 rows, whose scale bytes are neighbours
-    const int64_t per = std::max<int64_t>(1, (1 << 23) / s.chunks) << (8 - s.log_tpr);
-    const int64_t most = std::max<int64_t>(kScaled, per / kScaled * kScaled);
-    const int64_t rows = a.rows;
-    for (int64_t done = 0; done < rows; done += most) {
-        a.rows = std::min(most, rows - done);
-        const int64_t blocks = ((a.rows + (256 >> s.log_tpr) - 1) >> (8 - s.log_tpr)) * s.chunks;
-        held_values_kernel<T><<<(unsigned)blocks, 256, 0, st>>>(a, s);
+    const int64_t most = dealt_rows(s), rows = a.rows;
+    for (; a.row0 < rows; a.row0 += a.rows) {
+        a.rows = std::min(most, rows - a.row0);
+        held_values_kernel<T><<<(unsigned)dealt_blocks(s, a.rows), 256, 0, st>>>(a, s);
+        if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
         a.h.q += a.rows * a.h.ld;
-        a.h.scale += a.rows;
         a.out = (T *)a.out + a.rows * a.ldo;
     }
-    return hipGetLastError();
+    return hipSuccess;
 }
 
 __global__ __launch_bounds__(256) void zeros_kernel(char *p, int64_t ld, int64_t rows, int64_t bytes)
