@@ -745,7 +745,7 @@ kr_status kr_scaled_values(int32_t type, int64_t rows, int64_t width, const kr_s
  * brings eight neighbouring products to the largest one's exponent and cuts off what is below 2^-13 of
  * that power of two: sums are off by up to 2^-10 of their terms' magnitudes (1.5e-5 relative on
  * normal values), before a rounding of 2^-11 or 2^-8.  What is below 2^-126, a value, a product or a sum,
- * may be taken as 0.
+ * may be taken as 0, or rounded to a multiple of 2^-133.
  *   a [m][k], b [n][k]   m >= 0, n >= 1, k >= 1
  *   type                 of out
  * KR_EUNSUPPORTED for m >= 2^31, n > 2^27, k > 2^21 or an output of more than 2^23 tiles of 128 x 64.
