@@ -1,11 +1,12 @@
-"""Rows past one launch: the values of a held matrix go on where the launch before ended, at either side of
-its edge (tests/dealt.py says where that is)."""
+"""Rows past one launch: dropout and the values of a held matrix go on where the launch before ended, at
+either side of its edge (tests/dealt.py says where that is)."""
 
 import pytest
 import torch
 
 from tests.dealt import rows_a_launch
-from tests.scaled_form import in_order
+from tests.philox import factor
+from tests.scaled_form import hold, in_order, values
 
 pytestmark = pytest.mark.gpu
 
@@ -16,6 +17,57 @@ def kr():
     from paper_2601_17654_amd import binding
 
     return binding
+
+
+def places(edge, rows, n):
+    """First rows of runs of n: at the beginning, before, across and after the edge, at the end."""
+    return sorted({0, edge // 2, edge - n, edge - n // 2, edge, rows - n})
+
+
+@pytest.mark.parametrize("width,residual", [(1, True), (17, False), (2048, False)])
+def test_dropout(kr, width, residual):
+    """Kept values are whole numbers times 2: exact."""
+    edge = rows_a_launch(-(-width // 8))
+    rows, n = edge + 40, 16
+    # a row's values from its number: a row taken for another shows
+    part = torch.arange(1, 252, dtype=torch.bfloat16, device="cuda")[:, None].expand(251, width)
+    x = torch.empty(rows, width, dtype=torch.bfloat16, device="cuda")
+    whole = rows // 251 * 251
+    x[:whole].view(-1, 251, width).copy_(part.expand(whole // 251, 251, width))
+    x[whole:] = part[:rows - whole]
+    r = None
+    if residual:
+        r = torch.empty_like(x)
+        r[:rows // 2] = 3
+        r[rows // 2:] = 5
+    got = kr.dropout(x, 0.5, 11, 5, r)
+    for row0 in places(edge, rows, n):
+        f = factor(n, width, 0.5, 11, 5, row0)
+        want = x[row0:row0 + n].double().cpu() * f
+        if residual:
+            want = want + r[row0:row0 + n].double().cpu()
+        assert torch.equal(got[row0:row0 + n].double().cpu(), want.bfloat16().double()), row0
+
+
+def test_values_of_many_rows(kr):
+    """Narrow rows, 2^29 a launch: 253 rows of different scales over and over."""
+    width = 9
+    edge = rows_a_launch(-(-width // 4))
+    rows, n = edge + 300, 140
+    g = torch.Generator().manual_seed(1)
+    x = torch.randn(253, width, generator=g) * torch.exp2(torch.randint(-20, 20, (253, 1), generator=g))
+    q, byte = hold(x)
+    many = -(-rows // 253)
+    held = q.to(torch.float8_e4m3fn).view(torch.uint8).cuda().repeat(many, 1)[:rows]
+    flat = torch.zeros(-(-rows // 128) * 128, dtype=torch.uint8, device="cuda")
+    flat[:rows] = byte[:, 0].to(torch.uint8).cuda().repeat(many)[:rows]
+    scale = flat.view(-1, 8, 16).transpose(1, 2).reshape(1, -1)
+    del flat
+    assert torch.equal(scale[:, :128].cpu(), in_order(byte[:128]))
+    got = kr.scaled_values(kr.Scaled(held.view(torch.float8_e4m3fn), scale), torch.float32)
+    want = values(q, byte)
+    for row0 in places(edge, rows, n):
+        assert torch.equal(got[row0:row0 + n].double().cpu(), want[torch.arange(row0, row0 + n) % 253]), row0
 
 
 @pytest.mark.parametrize("rows,width", [(130, (1 << 26) + 261), (128, 1 << 27)])
