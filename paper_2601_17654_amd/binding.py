@@ -15,6 +15,7 @@ from typing import NamedTuple, Optional
 
 import numpy as np
 import torch
+import torch.autograd.forward_ad as _forward_ad
 
 _LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libkareus_mi355x.so")
 if not os.path.exists(_LIB_PATH):
@@ -761,6 +762,7 @@ def launch_timing_frontier(kind1, kind2, ops, p_static: float, kmax: int, out_ca
 # gated_projection and scaled_linear are nodes of it, whose backward passes are the functions
 # named so (dropout's is dropout).  The other forms in 8 bits have no gradient and refuse such
 # inputs.  The backward functions themselves return plain tensors: they are not differentiated again.
+# None has a forward-mode derivative, and all refuse inputs that carry a tangent.
 
 _TYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
@@ -867,8 +869,19 @@ def _norm_inputs(x, weight, residual):
     return t, dev, xr, n, ldx, width, w, rr, ldr
 
 
+def _no_tangent(*tensors) -> None:
+    """Refuses tensors with a forward-mode tangent, which a call by address would lose without a word."""
+    if _forward_ad._current_level < 0:  # outside of torch.autograd.forward_ad.dual_level()
+        return
+    for t in tensors:
+        if isinstance(t, torch.Tensor) and _forward_ad.unpack_dual(t).tangent is not None:
+            raise ValueError("the operators have no forward-mode derivative: call them on tensors without "
+                             "a tangent")
+
+
 def _tracked(*tensors) -> bool:
     """Whether a graph is recorded that one of these belongs to."""
+    _no_tangent(*tensors)
     if torch.is_grad_enabled():
         for t in tensors:
             if getattr(t, "requires_grad", False):
@@ -944,6 +957,7 @@ def add_rms_norm_backward(dout, sum, weight, rstd, dsum=None):
     """(dx, dweight) of add_rms_norm from its sum and rstd; dsum is the gradient that reaches
     the sum by the residual's path.  dx, like dout, is the gradient of x and of residual;
     dweight is float32 (kr_add_rms_norm_backward)."""
+    _no_tangent(dout, sum, weight, rstd, dsum)
     t = _type(dout, "dout")
     _like(sum, dout, "sum", "dout")
     dev = _here(dout, "dout")
@@ -1098,6 +1112,7 @@ def add_layer_norm_backward(dout, sum, weight, mean, rstd, dsum=None, p: float =
     """(dx, dresidual, dweight, dbias) of add_layer_norm from its sum, mean and rstd; dsum is the
     gradient that reaches the sum by the residual's path.  dx is dresidual itself where p is 0;
     dweight and dbias are float32 (kr_add_layer_norm_backward)."""
+    _no_tangent(dout, sum, weight, mean, rstd, dsum)
     t = _type(dout, "dout")
     _like(sum, dout, "sum", "dout")
     dev = _here(dout, "dout")
@@ -1208,6 +1223,7 @@ def gated_projection(x, wg, wu, act: str = "silu") -> torch.Tensor:
 def gated_projection_backward(dh, x, wg, wu, act: str = "silu"):
     """(dx, dwg, dwu) of gated_projection from its inputs and the gradient dh of its output
     (kr_gated_projection_backward)."""
+    _no_tangent(dh, x, wg, wu)
     g, dev, keep = _gated(x, wg, wu, act)
     if not isinstance(dh, torch.Tensor) or dh.dtype != x.dtype:
         raise TypeError("dh must be a tensor of %s" % x.dtype)
@@ -1324,6 +1340,7 @@ def scaled_values(h: Scaled, dtype=torch.float32) -> torch.Tensor:
         raise TypeError("dtype must be %s, got %s" % (" or ".join(map(str, _TYPES)), dtype))
     if not isinstance(h, Scaled) or not isinstance(h.q, torch.Tensor):
         raise TypeError("h must be Scaled, got %s" % type(h).__name__)
+    _no_tangent(h.q)
     dev = _here(h.q, "h.q")
     k, n, width, keep = _held(h, "h", dev)
     out = _new(h.q.shape, dtype)
@@ -1340,6 +1357,7 @@ def scaled_matmul(a: Scaled, b: Scaled, dtype=torch.bfloat16) -> torch.Tensor:
         raise TypeError("dtype must be %s, got %s" % (" or ".join(map(str, _TYPES)), dtype))
     if not isinstance(a, Scaled) or not isinstance(a.q, torch.Tensor):
         raise TypeError("a must be Scaled, got %s" % type(a).__name__)
+    _no_tangent(a.q, b.q if isinstance(b, Scaled) else None)
     dev = _here(a.q, "a.q")
     ak, m, k, keep_a = _held(a, "a", dev)
     bk, n, kb, keep_b = _held(b, "b", dev)
@@ -1387,6 +1405,7 @@ def scaled_linear(x, w) -> torch.Tensor:
     reaches both, holding taken as if it left values as they are."""
     if isinstance(w, Scaled):
         _no_gradient("scaled_linear with a weight that is held", x)
+        _no_tangent(w.q)
         _type(x, "x")
         return scaled_matmul(scaled_hold(x.detach()).plain, w, x.dtype)
     if _tracked(x, w):
@@ -1405,6 +1424,7 @@ def scaled_linear_backward(dout, x, w, need=(True, True)):
     products takes operands held along what it sums over: dx = dout w, dout held by rows and w by
     squares, as forward; dw = dout^T x, both held by columns, 128 rows a block.  None where `need`
     is false (kr_scaled_linear_backward)."""
+    _no_tangent(dout, x, w)
     l, dev, keep = _linear(x, w)
     if not isinstance(dout, torch.Tensor) or dout.dtype != x.dtype:
         raise TypeError("dout must be a tensor of %s" % x.dtype)
