@@ -1335,12 +1335,12 @@ def scaled_hold(x, square: bool = False, plain: bool = True, crossed: bool = Fal
 
 
 def scaled_values(h: Scaled, dtype=torch.float32) -> torch.Tensor:
-    """The values that h holds, in dtype (kr_scaled_values)."""
+    """The values that h holds, in dtype (kr_scaled_values).  It has no gradient."""
     if dtype not in _TYPES:
         raise TypeError("dtype must be %s, got %s" % (" or ".join(map(str, _TYPES)), dtype))
     if not isinstance(h, Scaled) or not isinstance(h.q, torch.Tensor):
         raise TypeError("h must be Scaled, got %s" % type(h).__name__)
-    _no_tangent(h.q)
+    _no_gradient("scaled_values", h.q)
     dev = _here(h.q, "h.q")
     k, n, width, keep = _held(h, "h", dev)
     out = _new(h.q.shape, dtype)
@@ -1357,7 +1357,7 @@ def scaled_matmul(a: Scaled, b: Scaled, dtype=torch.bfloat16) -> torch.Tensor:
         raise TypeError("dtype must be %s, got %s" % (" or ".join(map(str, _TYPES)), dtype))
     if not isinstance(a, Scaled) or not isinstance(a.q, torch.Tensor):
         raise TypeError("a must be Scaled, got %s" % type(a).__name__)
-    _no_tangent(a.q, b.q if isinstance(b, Scaled) else None)
+    _no_gradient("scaled_matmul", a.q, b.q if isinstance(b, Scaled) else None)
     dev = _here(a.q, "a.q")
     ak, m, k, keep_a = _held(a, "a", dev)
     bk, n, kb, keep_b = _held(b, "b", dev)
@@ -1404,8 +1404,7 @@ def scaled_linear(x, w) -> torch.Tensor:
     held once, by scaled_hold(w, square=True).plain); then there is no gradient.  Else the gradient
     reaches both, holding taken as if it left values as they are."""
     if isinstance(w, Scaled):
-        _no_gradient("scaled_linear with a weight that is held", x)
-        _no_tangent(w.q)
+        _no_gradient("scaled_linear with a weight that is held", x, w.q)
         _type(x, "x")
         return scaled_matmul(scaled_hold(x.detach()).plain, w, x.dtype)
     if _tracked(x, w):
