@@ -105,7 +105,7 @@ size_t scaled_part(int out_type, int64_t m, int64_t n, int64_t k);
 hipError_t launch_scaled(const ScaledArgs &a, hipStream_t st);
 // Two products of one output type, in one launch where both are cut into tiles of one size.
 hipError_t launch_scaled_pair(const ScaledArgs &a, const ScaledArgs &b, hipStream_t st);
-// Up to 32 rows, any alignment, k bytes of each row; no part.
+// Up to kScaledFew rows (hipErrorInvalidValue of more), any alignment, k bytes of each row; no part.
 hipError_t launch_scaled_few(const ScaledArgs &a, hipStream_t st);
 
 }  // namespace kr

@@ -683,6 +683,7 @@ hipError_t launch_scaled_pair(const ScaledArgs &a, const ScaledArgs &b, hipStrea
 
 hipError_t launch_scaled_few(const ScaledArgs &a, hipStream_t st)
 {
+    if (a.m > kScaledFew) return hipErrorInvalidValue;
     if (a.out_type == KR_F32) return few<float>(a, st);
     if (a.out_type == KR_F16) return few<f16>(a, st);
     return few<bf16>(a, st);
