@@ -274,21 +274,14 @@ __global__ __launch_bounds__(kHoldThreads) void hold_many_kernel(HoldMany m)
 }
 
 template <typename T>
-hipError_t hold_rows(HoldArgs a, hipStream_t st)
+hipError_t hold_rows(const HoldArgs &a, hipStream_t st)
 {
-    // four rows a thread, two where that leaves CUs without a second block
-    const int64_t rows = a.rows, tall = (rows + 63) / 64 * a.tiles_c >= 512 ? 64 : 32;
-    // a grid has fewer than 2^32 threads; whole groups of 128 rows, whose scale bytes are neighbours
-    const int64_t most = std::max<int64_t>(1, (1 << 22) / a.tiles_c) * kScaled;
-    for (int64_t done = 0; done < rows; done += most) {
-        a.rows = std::min(most, rows - done);
-        const unsigned blocks = (unsigned)((a.rows + tall - 1) / tall * a.tiles_c);
-        if (tall == 64) hold_rows_kernel<T, 4><<<blocks, 256, 0, st>>>(a);
-        else hold_rows_kernel<T, 2><<<blocks, 256, 0, st>>>(a);
-        a.x = (const T *)a.x + a.rows * a.ldx;
-        a.plain.q += a.rows * a.plain.ld;
-        a.plain.scale += a.rows;
-    }
+    // four rows a thread, two where that leaves CUs without a second block.  In one launch: kHoldTilesMost
+    // tiles are 2^23 blocks of 64 rows at most, 2^31 threads.
+    const bool tall = (a.rows + 63) / 64 * a.tiles_c >= 512;
+    const int64_t blocks = (a.rows + (tall ? 63 : 31)) / (tall ? 64 : 32) * a.tiles_c;
+    if (tall) hold_rows_kernel<T, 4><<<(unsigned)blocks, 256, 0, st>>>(a);
+    else hold_rows_kernel<T, 2><<<(unsigned)blocks, 256, 0, st>>>(a);
     return hipGetLastError();
 }
 

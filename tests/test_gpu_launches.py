@@ -91,3 +91,26 @@ def test_values_of_wide_rows(kr, rows, width):
             want = every[i, c % 1000] * torch.ldexp(torch.ones(3000, dtype=torch.float64),
                                                     byte[i, c // 128 % 500] - 127)
             assert torch.equal(got[i, c0:c0 + 3000].double().cpu(), want), (i, c0)
+
+
+@pytest.mark.parametrize("square", [False, True])
+def test_hold_of_the_most_rows(kr, square):
+    """2^22 squares, the most that is taken, in one launch: three blocks of rows over and over, to the last."""
+    rows, width, n = 1 << 29, 3, 384
+    g = torch.Generator().manual_seed(3)
+    part = (torch.randn(n, width, generator=g) * torch.exp2(torch.randint(-9, 9, (n, 1), generator=g))).bfloat16()
+    x = part.cuda().repeat(-(-rows // n), 1)[:rows]
+    plain, crossed = hold(part, square), hold(part.t(), square)
+    byte, turned = in_order(plain[1]), in_order(crossed[1])
+    for forms in (dict(), dict(crossed=True), dict(plain=False, crossed=True)):
+        got = kr.scaled_hold(x, square, **forms)
+        for block in (0, 1, 1 << 21, (1 << 22) - 2, (1 << 22) - 1):
+            i, k = block * 128, block % 3 * 128
+            if got.plain is not None:
+                assert torch.equal(got.plain.q[i:i + 128].float().cpu().double(), plain[0][k:k + 128]), block
+                assert torch.equal(got.plain.scale[:, i:i + 128].cpu(), byte[:, k:k + 128]), block
+            if got.crossed is not None:
+                assert torch.equal(got.crossed.q[:, i:i + 128].float().cpu().double(),
+                                   crossed[0][:, k:k + 128]), block
+                assert torch.equal(got.crossed.scale[block].cpu(), turned[block % 3]), block
+        del got
