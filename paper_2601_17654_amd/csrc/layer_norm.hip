@@ -440,10 +440,12 @@ hipError_t back_long(LayerNormBackArgs a, int slots, hipStream_t st)
     // dw and db first: an output may take dout's place
     const dim3 grid((unsigned)((a.width + 255) / 256), slots);
     layer_norm_back_long_weight_kernel<T><<<grid, 256, 0, st>>>(a);
+    if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     const int64_t rows = a.rows;
     for (int64_t done = 0; done < rows; done += kRowsPerLaunch) {
         a.rows = rows - done < kRowsPerLaunch ? rows - done : kRowsPerLaunch;
         layer_norm_back_long_kernel<T, DROP><<<(unsigned)a.rows, 1024, 0, st>>>(a);
+        if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
         a.s = (const T *)a.s + a.rows * a.lds;
         a.dout = (const T *)a.dout + a.rows * a.ldo;
         if (a.dsum) a.dsum = (const T *)a.dsum + a.rows * a.ldd;
@@ -453,7 +455,7 @@ hipError_t back_long(LayerNormBackArgs a, int slots, hipStream_t st)
         a.rstd += a.rows;
         a.row0 += a.rows;
     }
-    return hipGetLastError();
+    return hipSuccess;
 }
 
 template <typename T, bool DROP>

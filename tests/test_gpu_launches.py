@@ -114,3 +114,39 @@ def test_hold_of_the_most_rows(kr, square):
                                    crossed[0][:, k:k + 128]), block
                 assert torch.equal(got.crossed.scale[block].cpu(), turned[block % 3]), block
         del got
+
+
+def test_layer_norm_gradient_of_long_rows(kr):
+    """Rows too long for registers, 2^21 a launch, the gradient over dout: as the first rows alone, and whole
+    numbers whose sums over rows are exact below 2^24, so that a row left out or taken twice shows."""
+    import ctypes
+
+    rows, width, n, ld = (1 << 21) + 40, 16385, 64, 16392
+    t = kr._TYPES[torch.bfloat16]
+    g = torch.Generator().manual_seed(4)
+    s, d = (torch.randint(-2, 3, (n, width), generator=g).to(torch.bfloat16).cuda() for _ in range(2))
+    w = torch.ones(width, dtype=torch.bfloat16, device="cuda")
+    mean, rstd = torch.zeros(rows, device="cuda"), torch.ones(rows, device="cuda")
+    few = kr.add_layer_norm_backward(d, s, w, mean[:n], rstd[:n])
+    big = [torch.empty(rows, ld, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    whole = rows // n * n
+    for b, part in zip(big, (s, d)):
+        b[:whole].view(-1, n, ld)[:, :, :width] = part
+        b[whole:, :width] = part[:rows - whole]
+        b[:, width:] = 7
+    times = torch.full((n, 1), float(rows // n), dtype=torch.float64, device="cuda")
+    times[:rows - whole] += 1
+    want = [(s.double() * d.double() * times).sum(0), (d.double() * times).sum(0)]
+    assert max(float((v.abs().double() * times).sum(0).max()) for v in (s.double() * d.double(), d)) < 2 ** 24
+    dw, db = torch.empty(width, device="cuda"), torch.empty(width, device="cuda")
+    wsb = kr._lib.kr_add_layer_norm_backward_workspace(t, rows, width)
+    ws = torch.empty(wsb, dtype=torch.uint8, device="cuda")
+    at = big[1].data_ptr()
+    assert kr._lib.kr_add_layer_norm_backward(
+        t, rows, width, at, ld, big[0].data_ptr(), ld, w.data_ptr(), mean.data_ptr(), rstd.data_ptr(), None, 0,
+        None, at, ld, None, 0, dw.data_ptr(), db.data_ptr(), ws.data_ptr(), wsb, kr._raw_stream(0)) == kr.KR_OK
+    edge = 1 << 21
+    for row0 in (0, edge - n, edge, rows // n * n - n):
+        assert torch.equal(big[1][row0:row0 + n, :width], few[1][:big[1][row0:row0 + n].shape[0]]), row0
+        assert (big[1][row0:row0 + n, width:] == 7).all()
+    assert torch.equal(dw.double(), want[0]) and torch.equal(db.double(), want[1])
