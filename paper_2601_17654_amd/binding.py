@@ -1308,10 +1308,9 @@ def _held(h: Scaled, name: str, dev: int):
     if n:
         lds, one = s.stride()
         if one != 1 or lds % 4 or lds < shape[1] or s.data_ptr() % 4:
-            s = s.contiguous()
-            lds = s.stride(0)
-            if lds % 4:
-                raise ValueError("%s.scale must have rows of a multiple of 4 bytes" % name)
+            # a copy at an address of its own, which contiguous() does not always make
+            s = s[:, :_up(n, _SCALED)].clone(memory_format=torch.contiguous_format)
+            lds = _up(n, _SCALED)
     return KrScaled(q.data_ptr(), ld, room, s.data_ptr(), lds), n, width, (q, s)
 
 
