@@ -81,3 +81,37 @@ def test_every_byte_at_every_scale(kr, which, m, n, blocks, dtype):
         assert len(ea[:, block][seen].unique()) >= 240
     if which == "every b":
         assert len(eb[j, block][seen.any(0)].unique()) >= 240
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("m,n,k", [(1, 40, 700), (16, 40, 700), (100, 300, 700), (4096, 4096, 300)])
+def test_what_is_no_number(kr, m, n, k, dtype):
+    """The byte of a NaN and the scale of a NaN, beside any value, a 0 or a value at the other operand's end: NaN
+    through the whole row or column, and nowhere else."""
+    g = torch.Generator().manual_seed(3)
+    blocks = -(-k // 128)
+    a, b = (torch.randint(0, 0x7F, (r, k), generator=g, dtype=torch.uint8) for r in (m, n))
+    ea, eb = (torch.randint(110, 130, (r, blocks), generator=g) for r in (m, n))
+    a[:, 5], b[:, 6] = 0, 0
+    good = [t.clone() for t in (a, ea, b, eb)]
+    bad = torch.zeros(m, n, dtype=torch.bool)
+    a[m // 2, k - 1] = 0xFF
+    bad[m // 2] = True
+    b[3, 5], b[n - 1, 7] = 0x7F, 0xFF  # against zeros, too
+    eb[7, 1], eb[8, blocks - 1] = 255, 255
+    bad[:, [3, 7, 8, n - 1]] = True
+    if m > 1:
+        ea[m - 1, 0] = 255
+        bad[m - 1] = True
+
+    def product(a, ea, b, eb):
+        return kr.scaled_matmul(kr.Scaled(a.view(torch.float8_e4m3fn).cuda(), in_order(ea).cuda()),
+                                kr.Scaled(b.view(torch.float8_e4m3fn).cuda(), in_order(eb).cuda()), dtype).cpu()
+
+    got, want = product(a, ea, b, eb), product(*good)
+    assert torch.equal(got.isnan(), bad) and not want.isnan().any()
+    assert torch.equal(got[~bad], want[~bad])
+    for q, e in ((a, ea), (b, eb)):
+        v = kr.scaled_values(kr.Scaled(q.view(torch.float8_e4m3fn).cuda(), in_order(e).cuda()), dtype).cpu()
+        no = (q & 0x7F == 0x7F) | (e == 255).repeat_interleave(128, 1)[:, :k]
+        assert torch.equal(v.isnan(), no)
