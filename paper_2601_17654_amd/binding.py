@@ -871,17 +871,17 @@ def _norm_inputs(x, weight, residual):
 
 def _no_tangent(*tensors) -> None:
     """Refuses tensors with a forward-mode tangent, which a call by address would lose without a word."""
-    if _forward_ad._current_level < 0:  # outside of torch.autograd.forward_ad.dual_level()
-        return
-    for t in tensors:
-        if isinstance(t, torch.Tensor) and _forward_ad.unpack_dual(t).tangent is not None:
-            raise ValueError("the operators have no forward-mode derivative: call them on tensors without "
-                             "a tangent")
+    if _forward_ad._current_level >= 0:  # inside of torch.autograd.forward_ad.dual_level()
+        for t in tensors:
+            if isinstance(t, torch.Tensor) and _forward_ad.unpack_dual(t).tangent is not None:
+                raise ValueError("the operators have no forward-mode derivative: call them on tensors "
+                                 "without a tangent")
 
 
 def _tracked(*tensors) -> bool:
     """Whether a graph is recorded that one of these belongs to."""
-    _no_tangent(*tensors)
+    if _forward_ad._current_level >= 0:
+        _no_tangent(*tensors)
     if torch.is_grad_enabled():
         for t in tensors:
             if getattr(t, "requires_grad", False):
