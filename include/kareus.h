@@ -762,7 +762,8 @@ size_t kr_scaled_matmul_workspace(const kr_scaled_product *p);
 
 /*
  * kr_scaled_linear -- out = x w^T, both held first: x by rows, w by squares (kr_scaled_hold), then
- * their product (kr_scaled_matmul).  For a weight that stays, hold it once and call those two.
+ * their product (kr_scaled_matmul), to the type.  For a weight that stays, or sums in 32 bits of operands in
+ * 16, hold and call those two.
  *   type          of x [rows][width], w [hidden][width] and out [rows][hidden]
  * rows >= 0, width >= 1, hidden >= 1; KR_EUNSUPPORTED where one of the calls is.  out overlaps no
  * input.  The workspace (16-byte aligned) holds the operands; 0: none needed, or an invalid argument.

@@ -2,7 +2,8 @@
 // nowhere; of a gradient the same call gives the gradient.  A thread takes eight neighbours, whose random
 // bits come of one counter.
 //
-// Bound by memory: 8192 x 14336 in bfloat16 81 us (5.8 TB/s of its 470 MB), in float32 161 us (5.9 TB/s).
+// Bound by memory: 8192 x 14336 in bfloat16 81 us (5.8 TB/s of its 470 MB), in float32 161 us (5.9 TB/s);
+// with a residual 120 and 243 us (5.9, 5.8 TB/s).
 #include "kr_drop.h"
 #include "kr_rows.h"
 

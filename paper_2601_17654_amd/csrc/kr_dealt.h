@@ -1,5 +1,5 @@
-// How rows are dealt to blocks by kernels that take them in groups of neighbours, and to launches.  Host
-// code alone, plain C++.
+// How rows are dealt to blocks by kernels that take them in groups of neighbours, and to launches.  Plain C++:
+// the functions run on the host alone.
 #pragma once
 
 #include <stdint.h>
